@@ -18,12 +18,15 @@ SR_KERNEL_AUTO, SR_KERNEL_GENERIC, SR_KERNEL_MFMA = 0, 1, 2
 SR_COEFF_PLANAR, SR_COEFF_PRE_SHUFFLE, SR_COEFF_PIXEL_MAJOR, SR_COEFF_BLOCKED = 0, 1, 2, 3
 SR_COEFF_VALUES, SR_COEFF_LOGITS = 0, 1
 SR_RUNS_NOTHING, SR_RUNS_GENERIC, SR_RUNS_STREAMING, SR_RUNS_SLOTS = 0, 1, 2, 3
+SR_ROUTE_SOFTMAX, SR_ROUTE_CHOSEN, SR_ROUTE_VALUES = 0, 1, 2
 SR_MAX_ATOMS = 256
 
 EXPORTS = ("sr_dict_assemble", "sr_dict_assemble_selective", "sr_dict_assemble_ex", "sr_dict_assemble_list", "sr_dict_assemble_list_ex",
            "sr_bicubic_upsample", "sr_dict_assemble_plan", "sr_dict_assemble_tile", "sr_dict_assemble_launch_shape", "sr_dict_assemble_walk", "sr_dict_assemble_runs", "sr_dict_assemble_list_walk", "sr_strerror", "sr_version",
            "sr_probe_read", "sr_probe_mix", "sr_probe_mix_tiled", "sr_probe_mix_tiled_bytes", "sr_probe_mix_tiled_paced", "sr_probe_stream", "sr_probe_pattern", "sr_probe_policy", "sr_probe_policy_bits",
-           "sr_atom_gram_workspace_bytes", "sr_atom_gram", "sr_atom_gram_static", "sr_select_atoms")
+           "sr_atom_gram_workspace_bytes", "sr_atom_gram", "sr_atom_gram_static", "sr_select_atoms",
+           "sr_list_route", "sr_list_route_workspace_bytes", "sr_list_route_balance", "sr_list_route_grad",
+           "sr_dict_assemble_list_grad_workspace_bytes", "sr_dict_assemble_list_grad")
 
 
 class sr_tensor(ctypes.Structure):
@@ -90,12 +93,18 @@ def load():
     lib.sr_atom_gram_static.argtypes = [T, T, T, T, i, i, i, i, vp, vp]
     lib.sr_select_atoms.argtypes = [dp, i, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                     ip, ip, fp, dp]
+    sz = ctypes.c_size_t
+    lib.sr_list_route.argtypes = [T, i, i, i, i, i, T, T, T, vp]
+    lib.sr_list_route_workspace_bytes.argtypes = [i]
+    lib.sr_list_route_balance.argtypes = [T, i, i, i, i, i, T, T, T, vp, vp, vp, vp, sz, vp]
+    lib.sr_list_route_grad.argtypes = [T, T, T, i, i, i, i, i, T, vp, vp, T, vp]
+    lib.sr_dict_assemble_list_grad_workspace_bytes.argtypes = [i, i]
+    lib.sr_dict_assemble_list_grad.argtypes = [T, T, T, T, i, i, i, i, i, T, T, T, T, vp, sz, vp]
     lib.sr_strerror.restype = ctypes.c_char_p
     lib.sr_version.argtypes = []
     for name in EXPORTS:
-        if name not in ("sr_strerror", "sr_atom_gram_workspace_bytes"):
-            getattr(lib, name).restype = i
-    lib.sr_atom_gram_workspace_bytes.restype = ctypes.c_size_t
+        if name not in ("sr_strerror",):
+            getattr(lib, name).restype = sz if name.endswith("_workspace_bytes") else i
     _lib = lib
     return lib
 
@@ -407,3 +416,100 @@ def sr_select_atoms(normal, L, alpha, delta_alpha=0.1, lambda0=1e-6, eps=0.0):
                                   lambda0, eps, kept.ctypes.data_as(ctypes.POINTER(ctypes.c_int)), ctypes.byref(n),
                                   gamma.ctypes.data_as(ctypes.POINTER(ctypes.c_float)), ctypes.byref(lam)))
     return kept[:n.value].copy(), gamma[:n.value].copy(), lam.value
+
+
+def _here(*tensors):
+    """Refuses tensors that are not on the current device: the calls below run there, on its current stream."""
+    import torch
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != torch.cuda.current_device()):
+            raise ValueError(f"a tensor is on {t.device}: expected the current device")
+
+
+def _maybe(t):
+    return None if t is None else describe(t)
+
+
+def _logits(t, layout) -> sr_tensor:
+    d = describe(t)
+    if layout == SR_COEFF_PIXEL_MAJOR:                                       # [N][H][W][L], described with c = L
+        d.c, d.h, d.w = int(t.shape[3]), int(t.shape[1]), int(t.shape[2])
+    return d
+
+
+def _plain(t, dtype, count, what):
+    """The address of a small contiguous result or scalar tensor."""
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor of {count} values of {dtype}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _scratch(workspace, need, like):
+    import torch
+    if workspace is None:
+        workspace = torch.empty(max(need, 16), device=like.device, dtype=torch.uint8)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace
+
+
+def sr_list_route(coeff, L, scale, entries, kind, coeff_layout, mask, index, value, stream=None):
+    """The ``entries`` largest of every pixel's L logits as (atom, value) lists (include/sr_route.h)."""
+    _here(coeff, mask, index, value)
+    _check(load().sr_list_route(_logits(coeff, coeff_layout), L, scale, entries, kind, coeff_layout, _maybe(mask),
+                                describe(index), describe(value), _stream(stream)))
+    return index, value
+
+
+def sr_list_route_workspace_bytes(L: int) -> int:
+    return int(load().sr_list_route_workspace_bytes(int(L)))
+
+
+def sr_list_route_balance(coeff, L, scale, entries, kind, coeff_layout, mask, index, value, counts, share, loss,
+                          workspace=None, stream=None):
+    """sr_list_route with the atoms' counts (int64, L + 1) and shares (float32, L) and the two losses (float32, 2);
+    scratch is made here unless the caller passes it."""
+    import torch
+    workspace = _scratch(workspace, sr_list_route_workspace_bytes(L), coeff)
+    _here(coeff, mask, index, value, counts, share, loss, workspace)
+    _check(load().sr_list_route_balance(_logits(coeff, coeff_layout), L, scale, entries, kind, coeff_layout, _maybe(mask),
+                                        describe(index), describe(value), _plain(counts, torch.int64, L + 1, "counts"),
+                                        _plain(share, torch.float32, L, "share"), _plain(loss, torch.float32, 2, "loss"),
+                                        ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(),
+                                        _stream(stream)))
+    return index, value, counts, share, loss
+
+
+def sr_list_route_grad(coeff, index, dvalue, L, scale, entries, kind, coeff_layout, mask, counts, dloss, dcoeff, stream=None):
+    """Gradient of sr_list_route (``dvalue``, or None) and of the losses of sr_list_route_balance (``counts`` and ``dloss``,
+    both or neither None) with respect to the logits."""
+    import torch
+    _here(coeff, index, dvalue, mask, counts, dloss, dcoeff)
+    _check(load().sr_list_route_grad(_logits(coeff, coeff_layout), describe(index), _maybe(dvalue), L, scale, entries, kind,
+                                     coeff_layout, _maybe(mask),
+                                     None if counts is None else _plain(counts, torch.int64, L + 1, "counts"),
+                                     None if dloss is None else _plain(dloss, torch.float32, 2, "dloss"),
+                                     _logits(dcoeff, coeff_layout), _stream(stream)))
+    return dcoeff
+
+
+def sr_dict_assemble_list_grad_workspace_bytes(L: int, k: int) -> int:
+    return int(load().sr_dict_assemble_list_grad_workspace_bytes(int(L), int(k)))
+
+
+def sr_dict_assemble_list_grad(lr, index, value, dict, L, k, scale, channels, entries, mask, dout, dvalue, ddict,
+                               workspace=None, stream=None):
+    """Gradient of sr_dict_assemble_list with respect to the values (``dvalue``) and the dictionary (``ddict``, of the
+    dictionary's shape), either of which may be None; scratch is made here unless the caller passes it."""
+    if ddict is not None:
+        workspace = _scratch(workspace, sr_dict_assemble_list_grad_workspace_bytes(L, k), lr)
+    _here(lr, index, value, dict, mask, dout, dvalue, ddict, workspace)
+    if ddict is not None and not ddict.is_contiguous():
+        raise ValueError("ddict must be contiguous")
+    _check(load().sr_dict_assemble_list_grad(describe(lr), describe(index), describe(value), describe(_dict4(dict)),
+                                             L, k, scale, channels, entries, _maybe(mask), describe(dout), _maybe(dvalue),
+                                             None if ddict is None else describe(_dict4(ddict)),
+                                             None if workspace is None else ctypes.c_void_p(workspace.data_ptr()),
+                                             0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                             _stream(stream)))
+    return dvalue, ddict
