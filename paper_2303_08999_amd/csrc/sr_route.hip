@@ -4,7 +4,7 @@
 // found `entries` times over by a reduction of 64-bit keys (order of the logit, then the lower atom).
 #include <stdint.h>
 
-#include "sr_route.h"
+#include "sr_route_lanes.h"
 
 namespace srd {
 namespace {
@@ -348,6 +348,31 @@ hipError_t launch_route_grad(const RouteArgs& a, sr_dtype z, sr_dtype v, int gri
     return hipGetLastError();
 }
 
+// The kernels for many pixels (sr_route_lanes.h): lists of at most 16 entries, a pixel's logits within 32-bit offsets of one another.
+constexpr int64_t LANES_FROM = 2048;     // pixels
+int lanes_of(LaneArgs& a, const RouteArgs& r, sr_dtype z, sr_dtype v, const void* dz) {
+    const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR, pre = r.layout == SR_COEFF_PRE_SHUFFLE;
+    const int64_t es = (int64_t)route_esize(z);
+    const int G = pm ? 4 : (r.L <= 8 * LCH ? 1 : r.L <= 16 * LCH ? 2 : 4);
+    if (r.T > 16 || r.total < LANES_FROM) return 0;
+    if (!pm && (G - 1) * 8 * r.lstride * es >= (int64_t)1 << 31) return 0;
+    a.r = r;
+    a.ipx = pre ? (int64_t)r.h * r.w : r.px;
+    a.tiles_per_image = (a.ipx + 64 / G - 1) / (64 / G);
+    a.tiles = r.total / a.ipx * a.tiles_per_image;
+    a.vec = pm && r.L % 8 == 0 && (uintptr_t)r.z % 16 == 0 && (uintptr_t)dz % 16 == 0;
+    a.half_value = v == SR_F16;
+    return G;
+}
+hipError_t launch_lanes(const LaneArgs& a, sr_dtype z, int G, bool stats, int grid, hipStream_t st) {
+    return z == SR_F32 ? route_lanes<float>(a, G, stats, grid, st) : z == SR_F16 ? route_lanes<__half>(a, G, stats, grid, st)
+                                                                                 : route_lanes<bf16raw>(a, G, stats, grid, st);
+}
+int grid_for(int64_t tiles, int waves, int64_t most) {
+    const int64_t need = (tiles + waves - 1) / waves;
+    return (int)(need < most ? need : most);
+}
+
 // The outputs of a call (bytes, null where there is none) against its inputs and one another.
 struct Span { const void* p; size_t n; };
 template <int NO, int NI>
@@ -377,7 +402,10 @@ int sr_list_route(const sr_tensor* coeff, int L, int scale, int entries, int kin
     if (st != SR_OK || empty) return st;
     const Span out[] = {span(index), span(value)}, in[] = {span(coeff), span(mask)};
     if (any_overlap(out, in)) return SR_ERR_ALIAS;
-    const hipError_t e = launch_route<false>(a, coeff->dtype, value->dtype, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
+    LaneArgs m;
+    const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
+    const hipError_t e = G ? launch_lanes(m, coeff->dtype, G, false, grid_for(m.tiles, LWAVES, 1 << 20), (hipStream_t)stream)
+                           : launch_route<false>(a, coeff->dtype, value->dtype, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }
 
@@ -406,8 +434,11 @@ int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries,
     hipError_t e = hipSuccess;
     if (!empty) {
         a.partial = workspace;
-        a.records = blocks_for(a.total, ROUTE_RECORDS);
-        e = launch_route<true>(a, coeff->dtype, value->dtype, a.records, (hipStream_t)stream);
+        LaneArgs m;
+        const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
+        a.records = G ? grid_for(m.tiles, LWAVES, ROUTE_RECORDS / 2) : blocks_for(a.total, ROUTE_RECORDS);
+        e = G ? launch_lanes(m, coeff->dtype, G, true, a.records, (hipStream_t)stream)
+              : launch_route<true>(a, coeff->dtype, value->dtype, a.records, (hipStream_t)stream);
     }
     if (e == hipSuccess) {
         k_route_finish<<<1, FNT, 0, (hipStream_t)stream>>>(workspace, empty ? 0 : a.records, L, entries, counts, share, loss);
@@ -437,6 +468,17 @@ int sr_list_route_grad(const sr_tensor* coeff, const sr_tensor* index, const sr_
     a.counts = counts;
     a.dloss = dloss;
     a.dz = dcoeff->data;
-    const hipError_t e = launch_route_grad(a, coeff->dtype, dvalue ? dvalue->dtype : SR_F32, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
+    const sr_dtype vd = dvalue ? dvalue->dtype : SR_F32;
+    LaneArgs m;
+    const int G = lanes_of(m, a, coeff->dtype, vd, a.dz);
+    hipError_t e;
+    if (!G) {
+        e = launch_route_grad(a, coeff->dtype, vd, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
+    } else {
+        const int grid = grid_for(m.tiles, DWAVES, 4 * compute_units());
+        e = coeff->dtype == SR_F32 ? route_grad_lanes<float>(m, G, grid, (hipStream_t)stream)
+          : coeff->dtype == SR_F16 ? route_grad_lanes<__half>(m, G, grid, (hipStream_t)stream)
+                                   : route_grad_lanes<bf16raw>(m, G, grid, (hipStream_t)stream);
+    }
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }

@@ -1,0 +1,6 @@
+// The router's kernels for many pixels, f16 logits (sr_route_lanes.h).
+#include "sr_route_lanes.h"
+
+namespace srd {
+SR_ROUTE_LANES(__half)
+}  // namespace srd

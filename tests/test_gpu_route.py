@@ -192,12 +192,59 @@ def test_lists_losses_and_gradients(shape, kind, types):
     check_all(n, L, H, W, T, *types, kind, layout, scale, masked, seed=L * 7 + W)
 
 
+# enough pixels for the kernels with one to four lanes a pixel
+MANY = [
+    # (n, L, H, W, entries, layout, scale, masked)
+    (1, 72, 31, 67, 8, PLANAR, 1, False),
+    (2, 72, 40, 33, 5, PLANAR, 1, True),
+    (1, 72, 2100, 1, 16, PLANAR, 1, False),
+    (1, 71, 33, 65, 1, PLANAR, 1, True),
+    (1, 1, 50, 60, 1, PLANAR, 1, False),
+    (1, 9, 50, 50, 9, PLANAR, 1, True),
+    (1, 16, 46, 47, 16, PLANAR, 1, False),
+    (1, 73, 41, 53, 8, PLANAR, 1, False),        # two lanes a pixel
+    (2, 144, 33, 34, 4, PLANAR, 1, True),
+    (1, 128, 47, 46, 16, PLANAR, 1, False),
+    (1, 145, 45, 46, 8, PLANAR, 1, True),        # four
+    (1, 256, 43, 49, 12, PLANAR, 1, False),
+    (1, 72, 48, 50, 8, PRE, 2, True),
+    (2, 40, 39, 33, 3, PRE, 3, False),
+    (1, 100, 52, 44, 8, PRE, 4, True),
+    (1, 72, 1, 2111, 8, PM, 1, False),           # tokens: aligned rows
+    (3, 64, 1, 701, 2, PM, 1, True),
+    (1, 256, 1, 2049, 8, PM, 1, False),
+    (1, 73, 1, 2077, 4, PM, 1, True),            # rows that are not
+    (1, 12, 1, 2050, 12, PM, 1, False),          # ... of fp32, whole 16-byte pieces but no whole eight atoms
+    (2, 8, 30, 41, 3, PM, 1, True),
+    (1, 5, 1, 2060, 5, PM, 1, False),
+    (1, 200, 1, 2055, 16, PM, 1, False),
+    (1, 72, 40, 52, 17, PLANAR, 1, False),       # a list longer than they take
+]
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("f16", "f16"), ("bf16", "f32"), ("f16", "f32")], ids=lambda t: "-".join(t))
+@pytest.mark.parametrize("kind", [SOFT, CHOSEN, VALUES], ids=["softmax", "chosen", "values"])
+@pytest.mark.parametrize("shape", MANY, ids=lambda s: "n%dL%d_%dx%d_T%d_o%ds%d%s" % (s[:7] + ("m" if s[7] else "",)))
+def test_many_pixels(shape, kind, types):
+    n, L, H, W, T, layout, scale, masked = shape
+    check_all(n, L, H, W, T, *types, kind, layout, scale, masked, seed=L * 5 + W)
+
+
+@pytest.mark.parametrize("zd,vd", [("f16", "f16"), ("f32", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("layout,L", [(PLANAR, 72), (PM, 72), (PM, 64), (PRE, 72), (PLANAR, 100)])
+def test_many_pixels_at_odd_addresses(layout, L, zd, vd):
+    for shift in (1, 4):
+        check_all(1, L, 42, 66, 8, zd, vd, SOFT, layout, 2, True, seed=8, shift=shift)
+
+
 @pytest.mark.parametrize("spread", [0.0, 30.0, 300.0])
 @pytest.mark.parametrize("kind", [SOFT, CHOSEN])
 def test_flat_and_steep_logits(kind, spread):
     """All logits alike: the first atoms win, every value is 1/L; far apart: all but one vanish."""
     check_all(1, 72, 12, 33, 8, "f32", "f32", kind, PLANAR, seed=3, spread=spread, special=False)
     check_all(1, 72, 12, 33, 8, "bf16", "f16", kind, PM, seed=4, spread=spread, special=False)
+    check_all(1, 72, 32, 65, 8, "f32", "f32", kind, PLANAR, seed=5, spread=spread, special=False)
+    check_all(1, 128, 32, 65, 8, "bf16", "f16", kind, PM, seed=6, spread=spread, special=False)
 
 
 @pytest.mark.parametrize("zd,vd", [("f16", "f16"), ("f32", "f16"), ("bf16", "f32")])
@@ -216,7 +263,7 @@ def test_random_shapes():
         T = min(L, pick(1, 2, 4, 8, num(1, 16), num(1, 20)))
         layout = pick(PLANAR, PLANAR, PM, PRE)
         s = pick(2, 3, 4) if layout == PRE else 1
-        h, w = num(1, 12), num(1, 40)
+        h, w = (num(1, 12), num(1, 40)) if at % 2 else (num(20, 30), num(110, 130))
         args = (pick(1, 1, 2), L, h * s, w * s, T, pick("f32", "f16", "bf16"), pick("f32", "f16"), pick(SOFT, CHOSEN, VALUES), layout, s, pick(True, False))
         print(at, args, flush=True)
         check_all(*args, seed=1000 + at)
@@ -224,27 +271,26 @@ def test_random_shapes():
 
 def test_padding_is_not_looked_at():
     """NaN and infinities in masked pixels: values 0, atoms 0, 1, ...; nothing of them in losses and gradients."""
-    for layout in (PLANAR, PM):
-        for L in (72, 200):
-            z = logits(2, L, 9, 21, "f32", 5, special=False)
-            mask = make_mask(2, 9, 21, 6)
-            dirty = torch.where(mask == 0, torch.tensor([float("nan"), INF, -INF])[torch.arange(z.numel()) % 3].view(z.shape), z)
-            got = []
-            for t in (z, dirty):
-                c = stored(t, layout, 1).to(DEV)
-                index, value = torch.empty((2, 8, 9, 21), device=DEV, dtype=torch.uint8), torch.empty((2, 8, 9, 21), device=DEV)
-                counts, share, loss = torch.empty(L + 1, device=DEV, dtype=torch.int64), torch.empty(L, device=DEV), torch.empty(2, device=DEV)
-                sr.sr_list_route_balance(c, L, 1, 8, SOFT, layout, mask.to(DEV), index, value, counts, share, loss)
-                dz = torch.empty_like(c)
-                dv = torch.randn(value.shape, generator=torch.Generator().manual_seed(9)).to(DEV)
-                sr.sr_list_route_grad(c, index, dv, L, 1, 8, SOFT, layout, mask.to(DEV), counts, loss, dz)
-                got.append((index, value, counts, share, loss, dz))
-            for a, b in zip(*got):
-                assert torch.equal(a, b)
+    for layout, L, H in ((PLANAR, 72, 9), (PLANAR, 200, 9), (PM, 72, 9), (PM, 200, 9), (PLANAR, 72, 60), (PLANAR, 200, 60), (PM, 72, 60), (PM, 200, 60)):
+        z = logits(2, L, H, 21, "f32", 5, special=False)
+        mask = make_mask(2, H, 21, 6)
+        dirty = torch.where(mask == 0, torch.tensor([float("nan"), INF, -INF])[torch.arange(z.numel()) % 3].view(z.shape), z)
+        got = []
+        for t in (z, dirty):
+            c = stored(t, layout, 1).to(DEV)
+            index, value = torch.empty((2, 8, H, 21), device=DEV, dtype=torch.uint8), torch.empty((2, 8, H, 21), device=DEV)
+            counts, share, loss = torch.empty(L + 1, device=DEV, dtype=torch.int64), torch.empty(L, device=DEV), torch.empty(2, device=DEV)
+            sr.sr_list_route_balance(c, L, 1, 8, SOFT, layout, mask.to(DEV), index, value, counts, share, loss)
+            dz = torch.empty_like(c)
+            dv = torch.randn(value.shape, generator=torch.Generator().manual_seed(9)).to(DEV)
+            sr.sr_list_route_grad(c, index, dv, L, 1, 8, SOFT, layout, mask.to(DEV), counts, loss, dz)
+            got.append((index, value, counts, share, loss, dz))
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
 
 
 def test_nan_and_infinite_logits_still_list_different_atoms():
-    for L, layout, px in ((72, PLANAR, 300), (72, PM, 3), (200, PLANAR, 200), (40, PM, 500)):
+    for L, layout, px in ((72, PLANAR, 300), (72, PM, 3), (200, PLANAR, 200), (40, PM, 500), (72, PLANAR, 2500), (200, PLANAR, 2100), (40, PM, 2100)):
         z = logits(1, L, 1, px, "f32", 11, special=False)
         g = torch.Generator().manual_seed(12)
         for bad in (float("nan"), INF, -INF, -float("nan")):
@@ -274,7 +320,7 @@ def test_no_live_pixel_and_empty_calls():
 
 def test_gradient_with_foreign_lists():
     """Atoms listed twice or not below L: unspecified values at that pixel, the others as they are."""
-    for layout, W in ((PLANAR, 300), (PM, 4)):
+    for layout, W in ((PLANAR, 300), (PM, 4), (PLANAR, 1500), (PM, 1500)):
         z = logits(1, 72, 2, W, "f32", 21, special=False)
         index, _ = ro.route(z.double(), 8, SOFT)
         dv = torch.randn((1, 8, 2, W), generator=torch.Generator().manual_seed(3))
