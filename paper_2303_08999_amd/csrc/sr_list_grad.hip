@@ -7,32 +7,14 @@
 //
 // Here: checks, and the kernel that takes every case: a thread forms a pixel's E and the products of its entries, a
 // wavefront adds the entries of every fourth atom to the tile's dD, a tap per lane, in the order of the pixels.
-#include <stdint.h>
 #include <string.h>
 
-#include "sr_launch.h"
-#include "../../include/sr_route.h"
+#include "sr_list_grad.h"
 
 namespace srd {
-
-struct ListGradArgs {
-    const void* lr;                  // [N][C][h][w]
-    const unsigned char* index;      // [N][T][H][W]
-    const void* value;               // [N][T][H][W]
-    const float* dict;               // [L][k][k]
-    const unsigned char* mask;       // [N][H][W] or null
-    const void* dout;                // [N][C][H][W]
-    void* dvalue;                    // [N][T][H][W] or null
-    double* partial;                 // [workgroups][L][k][k], or null: no gradient of the dictionary
-    int N, C, h, w, H, W, s, L, T;
-    int tiles_x, tiles_y;
-    int64_t tiles;
-};
-
 namespace {
 
 constexpr int GTW = 64, GTH = 4, GNT = GTW * GTH;
-constexpr int GRAD_RECORDS = 256;            // workgroups of a call that writes ddict, at most
 constexpr int FLUSH = 16;                    // tiles (of 256 pixels) whose sums are held in fp32
 
 template <typename TV, typename TIO, int K>
@@ -172,6 +154,12 @@ bool overlap(const void* p, size_t np, const void* q, size_t nq) {
 }
 
 }  // namespace
+
+bool list_grad_mfma_supported(const ListGradArgs& a, int k) {
+    (void)k;
+    return a.T <= 16 && a.L <= 128 && (a.C == 1 || a.C == 3);
+}
+
 }  // namespace srd
 
 using namespace srd;
@@ -232,11 +220,18 @@ int sr_dict_assemble_list_grad(const sr_tensor* lr, const sr_tensor* index, cons
         a.mask = mask ? (const unsigned char*)mask->data : nullptr;
         a.dout = dout->data; a.dvalue = dvalue ? dvalue->data : nullptr; a.partial = ddict ? (double*)workspace : nullptr;
         a.N = lr->n; a.C = channels; a.h = lr->h; a.w = lr->w; a.H = (int)H; a.W = (int)W; a.s = scale; a.L = L; a.T = entries;
-        a.tiles_x = (a.W + GTW - 1) / GTW; a.tiles_y = (a.H + GTH - 1) / GTH;
+        a.io_f16 = lr->dtype == SR_F16;
+        const bool mfma = list_grad_mfma_supported(a, k);
+        const int tw = mfma ? GM_TW : GTW, th = mfma ? GM_TH : GTH;
+        a.tiles_x = (a.W + tw - 1) / tw; a.tiles_y = (a.H + th - 1) / th;
         a.tiles = (int64_t)a.N * a.tiles_x * a.tiles_y;
-        records = (int)(a.tiles < GRAD_RECORDS ? a.tiles : GRAD_RECORDS);
-        const int grid = ddict ? records : (int)(a.tiles < 4 * compute_units() ? a.tiles : 4 * compute_units());
-        if (value->dtype == SR_F16)
+        const int most = mfma ? 2 * compute_units() : (ddict ? GRAD_RECORDS : 4 * compute_units());
+        const int limit = most < GRAD_RECORDS || !ddict ? most : GRAD_RECORDS;
+        const int grid = (int)(a.tiles < limit ? a.tiles : limit);
+        records = grid;
+        if (mfma)
+            e = value->dtype == SR_F16 ? launch_list_grad_mfma<__half>(a, k, grid, st) : launch_list_grad_mfma<float>(a, k, grid, st);
+        else if (value->dtype == SR_F16)
             e = lr->dtype == SR_F16 ? launch_k<__half, __half>(a, k, grid, st) : launch_k<__half, float>(a, k, grid, st);
         else
             e = lr->dtype == SR_F16 ? launch_k<float, __half>(a, k, grid, st) : launch_k<float, float>(a, k, grid, st);
