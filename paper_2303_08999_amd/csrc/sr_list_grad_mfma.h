@@ -28,7 +28,7 @@ typedef u32x4v __attribute__((may_alias)) lds_u4;
 typedef unsigned __attribute__((may_alias)) lds_u;
 typedef unsigned short __attribute__((may_alias)) lds_h;
 
-template <int K, int LP, int CM, typename TV>
+template <int K, int LP, int CM, int TQ, typename TV>
 struct GradCfg {
     static constexpr int KK = K * K, R = (K - 1) / 2, NS = (KK + 31) / 32, NT = (KK + 15) / 16, MT = LP / 16;
     static constexpr int UW = GM_TW + K - 1, UH = GM_TH + K - 1;
@@ -39,7 +39,8 @@ struct GradCfg {
     static constexpr int PP = 40;                  // pitch of Phi in halves: 16 rows' 16-byte pieces fall on all 64 banks
     static constexpr int EP = 36;                  // pitch of [tap][pixel] in words, likewise
     static constexpr int RP = LP + 4;              // pitch of a pixel's responses, likewise
-    static constexpr int PHI_B = LP * PP * 2 * (SPLIT ? 2 : 1);
+    static constexpr int PHI_ROWS = LP + 1;        // the last one takes what is not to be added
+    static constexpr int PHI_B = PHI_ROWS * PP * 2 * (SPLIT ? 2 : 1);
     static constexpr int ER_B = 32 * NS * EP * 4 > 16 * RP * 4 ? 32 * NS * EP * 4 : 16 * RP * 4;
     static constexpr int WAVE_B = PHI_B + ER_B;
     static constexpr int WPE = K == 7 || LP > 80 ? 1 : 2;                              // wavefronts per SIMD (registers)
@@ -63,15 +64,22 @@ __device__ __forceinline__ void split_pair(float x, float y, unsigned& hi, unsig
     __builtin_memcpy(&lo, &l, 4);
 }
 
-template <int K, int LP, int CM, typename TV>
-__global__ __launch_bounds__(256, (GradCfg<K, LP, CM, TV>::WPE))
+// What a unit needs of memory, as it is stored, requested one unit ahead.
+template <int CM, int TQ> struct GradFetch {
+    unsigned dy[2][CM], idx[2][TQ], val[2][TQ], on[2];
+};
+
+template <int K, int LP, int CM, int TQ, typename TV>
+__global__ __launch_bounds__(256, (GradCfg<K, LP, CM, TQ, TV>::WPE))
 void k_list_grad_mfma(const ListGradArgs a) {
-    using F = GradCfg<K, LP, CM, TV>;
+    using F = GradCfg<K, LP, CM, TQ, TV>;
     constexpr int KK = F::KK, R = F::R, NS = F::NS, NT = F::NT, MT = F::MT, UW = F::UW, UH = F::UH, MAXLRX = F::MAXLRX, MAXLRY = F::MAXLRY;
-    __shared__ float U[F::UN + 4];                   // up-sampled tile, then a zero; before that, in its place, the LR footprint
+    constexpr int UNITS = GM_TH * 2 / 4;             // of a wavefront in a tile
+    constexpr unsigned VB = sizeof(TV);
+    __shared__ float U[F::UN];                       // up-sampled tile; before that, in its place, the LR footprint
     __shared__ float V[F::VN];
-    __shared__ float4 xw[UW], yw[UH];
-    __shared__ int xb[UW], yb[UH];
+    __shared__ float4 tw[UW + UH];                   // a tile's columns, then its rows: weights, first LR column or row
+    __shared__ int tb[UW + UH];
     __shared__ __align__(16) unsigned char scratch[4][F::WAVE_B];
     __shared__ float dmax[4];
 
@@ -79,7 +87,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned char* const phi = scratch[wave];
     unsigned char* const er = scratch[wave] + F::PHI_B;
-    const size_t plane = (size_t)a.H * a.W;
+    const int64_t plane = (int64_t)a.H * a.W;
     const unsigned lmax = (unsigned)a.L - 1u;
 
     // ---- the dictionary as operands of R: lane (q, n) has atom 16 mt + n, taps 32 s + 8 q and on, times 2^14 / its largest exponent
@@ -89,7 +97,6 @@ void k_list_grad_mfma(const ListGradArgs a) {
     for (int d = 32; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
     if (lane == 0) dmax[wave] = big;
     for (int e = lane; e < F::PHI_B / 16; e += 64) ((lds_u4*)phi)[e] = (u32x4v){0, 0, 0, 0};
-    if (tid < 4) U[F::UN + tid] = 0.0f;
     __syncthreads();
     const int dx = exponent_field(fmaxf(fmaxf(dmax[0], dmax[1]), fmaxf(dmax[2], dmax[3])));
     const float dscale = pow2_field(268 - dx), dback = pow2_field(dx - 14);
@@ -112,14 +119,15 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 Dh[mt][s][i] = hi, Dl[mt][s][i] = lo;
             }
         }
-    // where a lane's taps are in the tile, from its pixel's corner (the zero behind the tile: a tap that is none)
+    // where a lane's taps are in the tile, from the wavefront's first row on, in bytes (taps that are none: the last one once more; their
+    // responses meet zeros of D, their columns of G are not handed on)
     int tap[NS][8];
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int j = 32 * s + 8 * q + i;
-            tap[s][i] = j < KK ? j / K * UW + j % K : -1;
+            const int j = min(32 * s + 8 * q + i, KK - 1);
+            tap[s][i] = 4 * ((wave * (GM_TH / 4) + j / K) * UW + j % K + n);
         }
     float4v G[MT][NT];
 #pragma unroll
@@ -130,111 +138,133 @@ void k_list_grad_mfma(const ListGradArgs a) {
     bool first = true;
     int held = 0;
 
-    // hands the sums on: the wavefronts one after the other, through their scratch (G is 16 x 16 tiles: lane (q, n) has atoms 4 q ..
-    // 4 q + 3 of tap n)
-    auto hand_on = [&]() {
-#pragma unroll 1
-        for (int w = 0; w < 4; ++w) {
-            if (wave == w) {
+    struct Tile { int im, Y0, X0; };
+    auto tile_at = [&](unsigned t) -> Tile {
+        const unsigned per = (unsigned)a.tiles_x * (unsigned)a.tiles_y, im = t / per, in = t - im * per, ty = in / (unsigned)a.tiles_x;
+        return {(int)im, (int)ty * GM_TH, (int)(in - ty * (unsigned)a.tiles_x) * GM_TW};
+    };
+    // Requests a unit: lane (q, n) has of pixel n of either group the entries 4 r + q.  Every address is one of the tensors'; what is outside of
+    // the image or the list is set aside when it is used.
+    auto fetch = [&](GradFetch<CM, TQ>& f, const Tile& t, int u) {
+        const int Y = min(t.Y0 + wave * (GM_TH / 4) + u / 2, a.H - 1), X = min(t.X0 + u % 2 * 32, a.W - 1);
+        const int64_t at = (int64_t)Y * a.W + X;     // the same for the whole wavefront
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+        for (int g = 0; g < 2; ++g) {
+            const unsigned x = (unsigned)min(16 * g + n, a.W - 1 - X);
+            f.on[g] = a.mask ? (unsigned)(a.mask + (int64_t)t.im * plane + at)[x] : 1u;
+            if (a.io_f16) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                for (int c = 0; c < CM; ++c) f.dy[g][c] = ((const unsigned short*)a.dout + ((int64_t)t.im * CM + c) * plane + at)[x];
+            } else {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int l = 16 * mt + 4 * q + r, j = 16 * t + n;
-                            if (l < a.L && j < KK) {
-                                double* at = rec + l * KK + j;
-                                *at = (first && w == 0 ? 0.0 : *at) + (double)G[mt][t][r];
-                            }
-                            G[mt][t][r] = 0.0f;
-                        }
+                for (int c = 0; c < CM; ++c) f.dy[g][c] = ((const unsigned*)a.dout + ((int64_t)t.im * CM + c) * plane + at)[x];
             }
-            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < TQ; ++r) {
+                const int t0 = min(4 * r, a.T - 1);
+                const unsigned e = (unsigned)min(q, a.T - 1 - t0) * (unsigned)plane + x;
+                const int64_t base = ((int64_t)t.im * a.T + t0) * plane + at;
+                f.idx[g][r] = (a.index + base)[e];
+                f.val[g][r] = VB == 2 ? (unsigned)((const unsigned short*)a.value + base)[e] : ((const unsigned*)a.value + base)[e];
+            }
         }
-        first = false;
     };
 
-    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int im = (int)(tile / ((int64_t)a.tiles_x * a.tiles_y));
-        const int in = (int)(tile - (int64_t)im * a.tiles_x * a.tiles_y);
-        const int Y0 = in / a.tiles_x * GM_TH, X0 = in % a.tiles_x * GM_TW;
-        // ---- stage 1, all channels together
-        const TileOrigin o = tile_origin(Y0, X0, R, UH, UW, a.H, a.W, a.s);
+    const unsigned tiles = (unsigned)a.tiles;
+    unsigned tile = blockIdx.x;
+    GradFetch<CM, TQ> next;
+    Tile tn = tile_at(tile);
+    fetch(next, tn, 0);
+    for (; tile < tiles; tile += gridDim.x) {
+        const Tile tl = tn;
+        const bool last = tile + gridDim.x >= tiles;
+        if (!last) tn = tile_at(tile + gridDim.x);
+        // ---- stage 1, all channels together (build_taps, load_lr_tile, vpass and hpass of sr_device.h, the same values; every loop has the
+        // same number of turns for all lanes)
+        const TileOrigin o = tile_origin(tl.Y0, tl.X0, R, UH, UW, a.H, a.W, a.s);
         __syncthreads();                             // the last tile has been used
-        build_taps<UW, MAXLRX, 256>(X0, R, a.W, a.s, o.lx0, xw, xb, tid);
-        build_taps<UH, MAXLRY, 256>(Y0, R, a.H, a.s, o.ly0, yw, yb, tid);
+        if (tid < UW + UH) {
+            const bool row = tid >= UW;
+            int m;
+            const int f = src_floor(clampi((row ? tl.Y0 + tid - UW : tl.X0 + tid) - R, 0, (row ? a.H : a.W) - 1), a.s, m);
+            float wt[4];
+            keys_weights(m, a.s, wt);
+            tw[tid] = make_float4(wt[0], wt[1], wt[2], wt[3]);
+            tb[tid] = clampi(f - 1 - (row ? o.ly0 : o.lx0), 0, (row ? MAXLRY : MAXLRX) - 4);
+        }
+        {
+            constexpr int LRN = CM * MAXLRY * MAXLRX;
+            const int64_t lp = (int64_t)a.h * a.w;
 #pragma unroll
-        for (int c = 0; c < CM; ++c) {
-            const size_t pl = ((size_t)im * CM + c) * (size_t)a.h * a.w;
-            if (a.io_f16) load_lr_tile<__half, MAXLRY, MAXLRX, 256>((const __half*)a.lr + pl, a.h, a.w, o, U + c * MAXLRY * MAXLRX, tid);
-            else load_lr_tile<float, MAXLRY, MAXLRX, 256>((const float*)a.lr + pl, a.h, a.w, o, U + c * MAXLRY * MAXLRX, tid);
+            for (int i = 0; i < (LRN + 255) / 256; ++i) {
+                const int e = min(tid + 256 * i, LRN - 1);
+                const int c = e / (MAXLRY * MAXLRX), r = e - c * (MAXLRY * MAXLRX), ry = r / MAXLRX, rx = r - ry * MAXLRX;
+                const int64_t at = ((int64_t)tl.im * CM + c) * lp + (int64_t)clampi(o.ly0 + ry, 0, a.h - 1) * a.w + clampi(o.lx0 + rx, 0, a.w - 1);
+                U[e] = a.io_f16 ? __half2float(((const __half*)a.lr)[at]) : ((const float*)a.lr)[at];
+            }
         }
         __syncthreads();
-#pragma unroll
-        for (int c = 0; c < CM; ++c) vpass<MAXLRX, UH, 256>(U + c * MAXLRY * MAXLRX, V + c * UH * MAXLRX, yw, yb, tid);
+        {
+            constexpr int VN = CM * UH * MAXLRX;
+#pragma unroll 2
+            for (int i = 0; i < (VN + 255) / 256; ++i) {
+                const int e = min(tid + 256 * i, VN - 1);
+                const int c = e / (UH * MAXLRX), r = e - c * (UH * MAXLRX), yy = r / MAXLRX, rx = r - yy * MAXLRX;
+                const float4 w4 = tw[UW + yy];
+                const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
+                const float* p = U + c * (MAXLRY * MAXLRX) + tb[UW + yy] * MAXLRX + rx;
+                V[e] = dot4(wt, p[0], p[MAXLRX], p[2 * MAXLRX], p[3 * MAXLRX]);
+            }
+        }
         __syncthreads();
-#pragma unroll
-        for (int c = 0; c < CM; ++c)
-            hpass<MAXLRX, UW, UH, 256>(V + c * UH * MAXLRX, xw, xb, tid, [&](int yy, int xx, float v) { U[(c * UH + yy) * UW + xx] = v; });
+#pragma unroll 2
+        for (int i = 0; i < (F::UN + 255) / 256; ++i) {
+            const int e = min(tid + 256 * i, F::UN - 1);
+            const int row = e / UW, xx = e - row * UW;
+            const float4 w4 = tw[xx];
+            const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
+            const float* p = V + row * MAXLRX + tb[xx];
+            U[e] = dot4(wt, p[0], p[1], p[2], p[3]);
+        }
         __syncthreads();
 
         // ---- a wavefront's units: 32 pixels of a row, two groups of 16
 #pragma unroll 1
-        for (int u = 0; u < GM_TH * 2 / 4; ++u) {
-            const int ty = wave * (GM_TH / 4) + u / 2, Y = Y0 + ty, x0 = u % 2 * 32;
-            if (Y >= a.H || X0 + x0 >= a.W) continue;
-            unsigned idx[2][4];
-            TV val[2][4];
-            float dy[2][CM];
-            bool on[2], inside[2];
-            size_t at[2];
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int X = X0 + x0 + 16 * g + n;
-                inside[g] = X < a.W;
-                at[g] = (size_t)Y * a.W + (inside[g] ? X : 0);
-                on[g] = inside[g] && (!a.mask || a.mask[(size_t)im * plane + at[g]] != 0);
-#pragma unroll
-                for (int c = 0; c < CM; ++c) {
-                    const size_t e = ((size_t)im * CM + c) * plane + at[g];
-                    dy[g][c] = !on[g] ? 0.0f : a.io_f16 ? ld_as_float((const __half*)a.dout, e) : ((const float*)a.dout)[e];
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (4 * r < a.T) {
-                        const int t = 4 * r + q;
-                        const size_t e = ((size_t)im * a.T + (t < a.T ? t : 0)) * plane + at[g];
-                        const unsigned l = inside[g] ? (unsigned)a.index[e] : 0u;
-                        idx[g][r] = l < lmax ? l : lmax;
-                        val[g][r] = on[g] && t < a.T ? ((const TV*)a.value)[e] : (TV)0.0f;
-                    }
-            }
+        for (int u = 0; u < UNITS; ++u) {
+            const int Y = tl.Y0 + wave * (GM_TH / 4) + u / 2, x0 = u % 2 * 32;
+            GradFetch<CM, TQ> f = next;
+            if (u + 1 < UNITS || !last) fetch(next, u + 1 < UNITS ? tl : tn, (u + 1) % UNITS);
+            if (Y >= a.H || tl.X0 + x0 >= a.W) continue;
             unsigned word[2][NS][8];                 // E as (high, low) halves, of the pixel's own scale
             int ex[2];
+            const char* const Ub = (const char*)U + 4 * (u / 2 * UW + x0);
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                float E[NS][8];
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) E[s][i] = 0.0f;
+                const int X = tl.X0 + x0 + 16 * g + n;
+                const bool inside = X < a.W, on = inside && f.on[g] != 0;
+                float dy[CM];
 #pragma unroll
                 for (int c = 0; c < CM; ++c) {
-                    const float* const corner = U + (c * UH + ty) * UW + x0 + 16 * g + n;
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float* p = tap[s][i] < 0 ? U + F::UN : corner + tap[s][i];
-                            E[s][i] = fmaf(dy[g][c], *p, E[s][i]);
-                        }
+                    const float v = a.io_f16 ? __half2float(__ushort_as_half((unsigned short)f.dy[g][c])) : __uint_as_float(f.dy[g][c]);
+                    dy[c] = on ? v : 0.0f;
                 }
-                float m = 0.0f;
+#pragma unroll
+                for (int r = 0; r < TQ; ++r) {
+                    f.idx[g][r] = f.idx[g][r] < lmax ? f.idx[g][r] : lmax;
+                    f.val[g][r] = on ? f.val[g][r] : 0u;
+                }
+                float E[NS][8], m = 0.0f;
 #pragma unroll
                 for (int s = 0; s < NS; ++s)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(E[s][i]));
+                    for (int i = 0; i < 8; ++i) {
+                        const char* p = Ub + tap[s][i];
+                        float e = dy[0] * *(const float*)(p + 64 * g);
+#pragma unroll
+                        for (int c = 1; c < CM; ++c) e = fmaf(dy[c], *(const float*)(p + 64 * g + 4 * c * UH * UW), e);
+                        E[s][i] = e;
+                        m = fmaxf(m, fabsf(e));
+                    }
                 m = fmaxf(m, __shfl_xor(m, 16));
                 m = fmaxf(m, __shfl_xor(m, 32));
                 ex[g] = exponent_field(m);
@@ -247,8 +277,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
                         unsigned hi, lo;
                         split_pair(E[s][2 * i] * sc, E[s][2 * i + 1] * sc, hi, lo);
                         Eh[s][i] = hi, El[s][i] = lo;
-                        word[g][s][2 * i] = (hi & 0xffffu) | (lo << 16);
-                        word[g][s][2 * i + 1] = (hi >> 16) | (lo & 0xffff0000u);
+                        word[g][s][2 * i] = __builtin_amdgcn_perm(lo, hi, 0x05040100u);
+                        word[g][s][2 * i + 1] = __builtin_amdgcn_perm(lo, hi, 0x07060302u);
                     }
                 if (a.dvalue) {
                     wave_lds_fence();
@@ -267,39 +297,47 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     }
                     wave_lds_fence();
                     const float back = pow2_field(ex[g] - 14);
+                    float v[TQ];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (4 * r < a.T) {
-                            const int t = 4 * r + q;
-                            const float v = *(lds_f*)(er + 4 * (n * F::RP + idx[g][r])) * back * dback;
-                            if (inside[g] && t < a.T) st_from_float((TV*)a.dvalue, ((size_t)im * a.T + t) * plane + at[g], on[g] ? v : 0.0f);
-                        }
+                    for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
+                    if (inside) {
+                        TV* const to = (TV*)a.dvalue + ((int64_t)tl.im * a.T * plane + (int64_t)Y * a.W + tl.X0 + x0);
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r)
+                            if (4 * r + q < a.T) st_from_float(to + 4 * r * plane, (unsigned)q * (unsigned)plane + 16 * g + n, on ? v[r] : 0.0f);
+                    }
                 }
             }
             if (rec) {
-                // the unit's scale, its values' scale; E to [tap][pixel], the lists to [atom][pixel]
+                // the unit's scale, its values' scale; E to [tap][pixel]
                 int es = max(ex[0], ex[1]);
 #pragma unroll
                 for (int d = 8; d > 0; d >>= 1) es = max(es, __shfl_xor(es, d));
-                float vback = 1.0f, vsc = 1.0f;
+                float vback = 1.0f;
+                unsigned val[2][TQ], vlo[2][F::SPLIT ? TQ : 1];
+                int cur[2][TQ];
                 if (F::SPLIT) {
                     float m = 0.0f;
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (4 * r < a.T) m = fmaxf(m, fabsf((float)val[g][r]));
+                        for (int r = 0; r < TQ; ++r)
+                            if (4 * r + q < a.T) m = fmaxf(m, fabsf(__uint_as_float(f.val[g][r])));
 #pragma unroll
                     for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
                     const int vx = exponent_field(m);
-                    vsc = pow2_field(268 - vx);
+                    const float vsc = pow2_field(268 - vx);
                     vback = pow2_field(vx - 14);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r) split_pair(__uint_as_float(f.val[g][r]) * vsc, 0.0f, val[g][r], vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0]);
                 }
                 wave_lds_fence();
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    const _Float16 f = (_Float16)pow2_field(127 + ex[g] - es);
-                    const half2v ff = {f, f};
+                    const _Float16 fs = (_Float16)pow2_field(127 + ex[g] - es);
+                    const half2v ff = {fs, fs};
 #pragma unroll
                     for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -307,6 +345,11 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             const half2v v = __builtin_bit_cast(half2v, word[g][s][i]) * ff;
                             *(lds_u*)(er + 4 * ((32 * s + 8 * q + i) * F::EP + 16 * g + n)) = __builtin_bit_cast(unsigned, v);
                         }
+#pragma unroll
+                    for (int r = 0; r < TQ; ++r) {
+                        if (!F::SPLIT) val[g][r] = f.val[g][r];
+                        cur[g][r] = 2 * ((4 * r + q < a.T ? (int)f.idx[g][r] : LP) * F::PP + 16 * g + n);
+                    }
                 }
                 wave_lds_fence();
                 half8 eh[NT], el[NT];
@@ -326,50 +369,41 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 }
                 const float back = pow2_field(es - 14) * vback;
                 // Entries into the dense columns.  An atom that a pixel lists twice has one place there: every entry writes its number, those that
-                // find another's wait for the next pass (lists as the router makes them: one pass).
-                unsigned left = 0;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (4 * r + q < a.T) left |= 0x11u << r;
+                // find another's wait for the next pass (lists as the router makes them: one pass).  The array is all zero between uses.
+                bool more;
 #pragma unroll 1
                 do {
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (left >> (4 * g + r) & 1) *(lds_h*)(phi + 2 * (idx[g][r] * F::PP + 16 * g + n)) = (unsigned short)(4 * r + q + 1);
+                        for (int r = 0; r < TQ; ++r) *(lds_h*)(phi + cur[g][r]) = (unsigned short)(4 * r + q + 1);
                     wave_lds_fence();
-                    unsigned mine = 0;
+                    unsigned seen[2][TQ];
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if ((left >> (4 * g + r) & 1) && *(lds_h*)(phi + 2 * (idx[g][r] * F::PP + 16 * g + n)) == 4 * r + q + 1) mine |= 1u << (4 * g + r);
+                        for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
                     wave_lds_fence();
+                    int put[2][TQ];
+                    more = false;
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (mine >> (4 * g + r) & 1) {
-                                unsigned char* p = phi + 2 * (idx[g][r] * F::PP + 16 * g + n);
-                                if (F::SPLIT) {
-                                    unsigned hi, lo;
-                                    split_pair((float)val[g][r] * vsc, 0.0f, hi, lo);
-                                    *(lds_h*)p = (unsigned short)hi;
-                                    *(lds_h*)(p + LP * F::PP * 2) = (unsigned short)lo;
-                                } else {
-                                    unsigned short h;
-                                    __builtin_memcpy(&h, &val[g][r], 2);
-                                    *(lds_h*)p = h;
-                                }
-                            }
-                    left &= ~mine;
+                        for (int r = 0; r < TQ; ++r) {
+                            const int aside = 2 * (LP * F::PP + 16 * g + n);
+                            const bool mine = seen[g][r] == (unsigned)(4 * r + q + 1);
+                            put[g][r] = mine ? cur[g][r] : aside;
+                            cur[g][r] = mine ? aside : cur[g][r];
+                            more = more || cur[g][r] != aside;
+                            *(lds_h*)(phi + put[g][r]) = (unsigned short)val[g][r];
+                            if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = (unsigned short)vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0];
+                        }
                     wave_lds_fence();
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         const half8 p0 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((16 * mt + n) * F::PP + 8 * q)));
                         half8 p1;
-                        if (F::SPLIT) p1 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((LP + 16 * mt + n) * F::PP + 8 * q)));
+                        if (F::SPLIT) p1 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((F::PHI_ROWS + 16 * mt + n) * F::PP + 8 * q)));
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
                             float4v r = {0, 0, 0, 0};
@@ -384,27 +418,50 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (mine >> (4 * g + r) & 1) {
-                                unsigned char* p = phi + 2 * (idx[g][r] * F::PP + 16 * g + n);
-                                *(lds_h*)p = 0;
-                                if (F::SPLIT) *(lds_h*)(p + LP * F::PP * 2) = 0;
-                            }
+                        for (int r = 0; r < TQ; ++r) {
+                            *(lds_h*)(phi + put[g][r]) = 0;
+                            if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = 0;
+                        }
                     wave_lds_fence();
-                } while (__any(left));
+                } while (__any(more));
             }
         }
-        if (rec && ++held == 4096 / (GM_TW * GM_TH / 4)) {
+        // ---- the sums handed on, the wavefronts one after the other (G is 16 x 16 tiles: lane (q, n) has atoms 4 q .. 4 q + 3 of tap n)
+        if (rec && (++held == 4096 / (GM_TW * GM_TH / 4) || last)) {
             held = 0;
-            hand_on();
+#pragma unroll 1
+            for (int w = 0; w < 4; ++w) {
+                if (wave == w) {
+                    int l0 = 4 * q, j0 = n;          // (hidden: no address of a record is worth a register for the whole tile)
+                    asm volatile("" : "+v"(l0), "+v"(j0));
+                    const bool fresh = first && w == 0;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const int j = j0 + 16 * t, l = l0 + 16 * mt;
+                            double* const at = rec + l * KK + j;
+                            double was[4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) was[r] = !fresh && l + r < a.L && j < KK ? at[r * KK] : 0.0;
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                if (l + r < a.L && j < KK) at[r * KK] = was[r] + (double)G[mt][t][r];
+                                G[mt][t][r] = 0.0f;
+                            }
+                        }
+                }
+                __syncthreads();
+            }
+            first = false;
         }
     }
-    if (rec) hand_on();
 }
 
 template <int K, int LP, int CM, typename TV>
 static hipError_t grad_mfma_one(const ListGradArgs& a, int grid, hipStream_t st) {
-    k_list_grad_mfma<K, LP, CM, TV><<<grid, 256, 0, st>>>(a);
+    if (a.T <= 8) k_list_grad_mfma<K, LP, CM, 2, TV><<<grid, 256, 0, st>>>(a);
+    else k_list_grad_mfma<K, LP, CM, 4, TV><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 template <int K, typename TV>
