@@ -30,21 +30,34 @@ typedef unsigned short __attribute__((may_alias)) lds_h;
 
 template <int K, int LP, int CM, int TQ, typename TV>
 struct GradCfg {
-    static constexpr int KK = K * K, R = (K - 1) / 2, NS = (KK + 31) / 32, NT = (KK + 15) / 16, MT = LP / 16;
-    static constexpr int UW = GM_TW + K - 1, UH = GM_TH + K - 1;
+    static constexpr int KK = K * K, R = (K - 1) / 2, MT = LP / 16;
+    // Taps in the operands' places (s, q, i), of which 8 q + i is the place in a sum over 32: lanes q have row 4 s + q of the patch, so
+    // that the four groups of 16 lanes read four rows of the tile, 16 banks apart; 5x5 atoms have their fifth row in two places more.
+    static constexpr int NS = (K + 2) / 4, NI = K == 5 ? 7 : K, NT = 2 * NS;
+    static constexpr int UW = GM_TW + K - 1, UH = GM_TH + K - 1, UP = 80;             // the tile, its pitch (16 modulo 64)
     static constexpr int MAXLRX = (UW - 1) / 2 + 5, MAXLRY = (UH - 1) / 2 + 5;       // scale >= 2
-    static constexpr int UN = CM * UH * UW;                                            // and one zero behind
-    static constexpr int VN = CM * UH * MAXLRX;
+    static constexpr int UN = CM * UH * UP, VN = CM * UH * MAXLRX;
     static constexpr bool SPLIT = sizeof(TV) == 4;                                     // values in two parts
     static constexpr int PP = 40;                  // pitch of Phi in halves: 16 rows' 16-byte pieces fall on all 64 banks
     static constexpr int EP = 36;                  // pitch of [tap][pixel] in words, likewise
     static constexpr int RP = LP + 4;              // pitch of a pixel's responses, likewise
     static constexpr int PHI_ROWS = LP + 1;        // the last one takes what is not to be added
     static constexpr int PHI_B = PHI_ROWS * PP * 2 * (SPLIT ? 2 : 1);
-    static constexpr int ER_B = 32 * NS * EP * 4 > 16 * RP * 4 ? 32 * NS * EP * 4 : 16 * RP * 4;
+    static constexpr int R_B = 16 * RP * 4;        // responses of a group
+    // Groups whose responses are formed together: two hide each other's latency, one takes fewer registers and less scratch.
+    static constexpr int RG = (K == 7 && LP > 80) || (TQ == 4 && LP <= 80 && !SPLIT) ? 1 : 2;
+    static constexpr int ER_0 = 32 * NS * EP * 4 > RG * R_B ? 32 * NS * EP * 4 : RG * R_B;
+    static constexpr int ER_B = ER_0 > VN * 4 ? ER_0 : (VN * 4 + 15) / 16 * 16;
     static constexpr int WAVE_B = PHI_B + ER_B;
-    static constexpr int WPE = K == 7 || LP > 80 ? 1 : 2;                              // wavefronts per SIMD (registers)
-    static_assert(CM * MAXLRY * MAXLRX <= UN, "the LR rows fit where the tile goes");
+    static constexpr int WPE = K == 7 || LP > 80 || SPLIT ? 1 : 2;                     // wavefronts per SIMD (registers, LDS)
+    static_assert(CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
+    // the tap at a place, or -1
+    static __device__ __forceinline__ int tap(int s, int q, int i) {
+        const int row = 4 * s + q;
+        if (i < K) return row < K ? row * K + i : -1;
+        if (K == 5 && i == 5) return 20 + q;
+        return K == 5 && i == 6 && q == 0 ? 24 : -1;
+    }
 };
 
 __device__ __forceinline__ void wave_lds_fence() {
@@ -73,13 +86,13 @@ template <int K, int LP, int CM, int TQ, typename TV>
 __global__ __launch_bounds__(256, (GradCfg<K, LP, CM, TQ, TV>::WPE))
 void k_list_grad_mfma(const ListGradArgs a) {
     using F = GradCfg<K, LP, CM, TQ, TV>;
-    constexpr int KK = F::KK, R = F::R, NS = F::NS, NT = F::NT, MT = F::MT, UW = F::UW, UH = F::UH, MAXLRX = F::MAXLRX, MAXLRY = F::MAXLRY;
+    constexpr int KK = F::KK, R = F::R, NS = F::NS, NI = F::NI, NT = F::NT, MT = F::MT, UW = F::UW, UH = F::UH, UP = F::UP;
+    constexpr int MAXLRX = F::MAXLRX, MAXLRY = F::MAXLRY;
     constexpr int UNITS = GM_TH * 2 / 4;             // of a wavefront in a tile
     constexpr unsigned VB = sizeof(TV);
     __shared__ float U[F::UN];                       // up-sampled tile; before that, in its place, the LR footprint
-    __shared__ float V[F::VN];
-    __shared__ float4 tw[UW + UH];                   // a tile's columns, then its rows: weights, first LR column or row
-    __shared__ int tb[UW + UH];
+    __shared__ float4 yw[UH];                        // a tile's rows: weights, first LR row
+    __shared__ int yb[UH];
     __shared__ __align__(16) unsigned char scratch[4][F::WAVE_B];
     __shared__ float dmax[4];
 
@@ -87,6 +100,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned char* const phi = scratch[wave];
     unsigned char* const er = scratch[wave] + F::PHI_B;
+    float* const V = (float*)(scratch[0] + F::PHI_B);      // after the vertical pass
     const int64_t plane = (int64_t)a.H * a.W;
     const unsigned lmax = (unsigned)a.L - 1u;
 
@@ -109,8 +123,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int j = 32 * s + 8 * q + i;
-                v[i] = l < a.L && j < KK ? a.dict[l * KK + j] * dscale : 0.0f;
+                const int j = F::tap(s, q, i);
+                v[i] = l < a.L && j >= 0 ? a.dict[l * KK + j] * dscale : 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -119,15 +133,15 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 Dh[mt][s][i] = hi, Dl[mt][s][i] = lo;
             }
         }
-    // where a lane's taps are in the tile, from the wavefront's first row on, in bytes (taps that are none: the last one once more; their
+    // where a lane's taps are in the tile, from the wavefront's first row on, in bytes (places without one: the patch's last tap; their
     // responses meet zeros of D, their columns of G are not handed on)
-    int tap[NS][8];
+    int tap[NS][NI];
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = min(32 * s + 8 * q + i, KK - 1);
-            tap[s][i] = 4 * ((wave * (GM_TH / 4) + j / K) * UW + j % K + n);
+        for (int i = 0; i < NI; ++i) {
+            const int j = F::tap(s, q, i) < 0 ? KK - 1 : F::tap(s, q, i);
+            tap[s][i] = 4 * ((wave * (GM_TH / 4) + j / K) * UP + j % K + n);
         }
     float4v G[MT][NT];
 #pragma unroll
@@ -179,52 +193,54 @@ void k_list_grad_mfma(const ListGradArgs a) {
         const Tile tl = tn;
         const bool last = tile + gridDim.x >= tiles;
         if (!last) tn = tile_at(tile + gridDim.x);
-        // ---- stage 1, all channels together (build_taps, load_lr_tile, vpass and hpass of sr_device.h, the same values; every loop has the
-        // same number of turns for all lanes)
+        // ---- stage 1 of all channels, the values of sr_device.h; every loop has the same number of turns for all lanes.  LR rows and rows
+        // after the vertical pass are a wavefront's each, columns of the tile a thread's, whose weights stay in registers.
         const TileOrigin o = tile_origin(tl.Y0, tl.X0, R, UH, UW, a.H, a.W, a.s);
         __syncthreads();                             // the last tile has been used
-        if (tid < UW + UH) {
-            const bool row = tid >= UW;
+        if (tid < UH) {
             int m;
-            const int f = src_floor(clampi((row ? tl.Y0 + tid - UW : tl.X0 + tid) - R, 0, (row ? a.H : a.W) - 1), a.s, m);
+            const int f = src_floor(clampi(tl.Y0 + tid - R, 0, a.H - 1), a.s, m);
             float wt[4];
             keys_weights(m, a.s, wt);
-            tw[tid] = make_float4(wt[0], wt[1], wt[2], wt[3]);
-            tb[tid] = clampi(f - 1 - (row ? o.ly0 : o.lx0), 0, (row ? MAXLRY : MAXLRX) - 4);
+            yw[tid] = make_float4(wt[0], wt[1], wt[2], wt[3]);
+            yb[tid] = clampi(f - 1 - o.ly0, 0, MAXLRY - 4);
         }
         {
-            constexpr int LRN = CM * MAXLRY * MAXLRX;
-            const int64_t lp = (int64_t)a.h * a.w;
+            const int rx = min(lane, MAXLRX - 1), x = clampi(o.lx0 + rx, 0, a.w - 1);
+            float v[(CM * MAXLRY + 3) / 4];
 #pragma unroll
-            for (int i = 0; i < (LRN + 255) / 256; ++i) {
-                const int e = min(tid + 256 * i, LRN - 1);
-                const int c = e / (MAXLRY * MAXLRX), r = e - c * (MAXLRY * MAXLRX), ry = r / MAXLRX, rx = r - ry * MAXLRX;
-                const int64_t at = ((int64_t)tl.im * CM + c) * lp + (int64_t)clampi(o.ly0 + ry, 0, a.h - 1) * a.w + clampi(o.lx0 + rx, 0, a.w - 1);
-                U[e] = a.io_f16 ? __half2float(((const __half*)a.lr)[at]) : ((const float*)a.lr)[at];
+            for (int i = 0; i < (CM * MAXLRY + 3) / 4; ++i) {
+                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
+                const int64_t at = (((int64_t)tl.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w;
+                v[i] = a.io_f16 ? __half2float(((const __half*)a.lr + at)[x]) : ((const float*)a.lr + at)[x];
+            }
+#pragma unroll
+            for (int i = 0; i < (CM * MAXLRY + 3) / 4; ++i) U[min(wave + 4 * i, CM * MAXLRY - 1) * MAXLRX + rx] = v[i];
+        }
+        __syncthreads();
+        {
+            const int rx = min(lane, MAXLRX - 1);
+#pragma unroll 3
+            for (int i = 0; i < (CM * UH + 3) / 4; ++i) {
+                const int p = min(wave + 4 * i, CM * UH - 1), c = p / UH, yy = p - c * UH;
+                const float4 w4 = yw[yy];
+                const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
+                const float* r = U + (c * MAXLRY + yb[yy]) * MAXLRX + rx;
+                V[p * MAXLRX + rx] = dot4(wt, r[0], r[MAXLRX], r[2 * MAXLRX], r[3 * MAXLRX]);
             }
         }
         __syncthreads();
         {
-            constexpr int VN = CM * UH * MAXLRX;
-#pragma unroll 2
-            for (int i = 0; i < (VN + 255) / 256; ++i) {
-                const int e = min(tid + 256 * i, VN - 1);
-                const int c = e / (UH * MAXLRX), r = e - c * (UH * MAXLRX), yy = r / MAXLRX, rx = r - yy * MAXLRX;
-                const float4 w4 = tw[UW + yy];
-                const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
-                const float* p = U + c * (MAXLRY * MAXLRX) + tb[UW + yy] * MAXLRX + rx;
-                V[e] = dot4(wt, p[0], p[MAXLRX], p[2 * MAXLRX], p[3 * MAXLRX]);
-            }
-        }
-        __syncthreads();
-#pragma unroll 2
-        for (int i = 0; i < (F::UN + 255) / 256; ++i) {
-            const int e = min(tid + 256 * i, F::UN - 1);
-            const int row = e / UW, xx = e - row * UW;
-            const float4 w4 = tw[xx];
-            const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
-            const float* p = V + row * MAXLRX + tb[xx];
-            U[e] = dot4(wt, p[0], p[1], p[2], p[3]);
+            const int col = min(tid, 3 * UW - 1), third = col / UW, xx = col - third * UW;
+            int m;
+            const int f = src_floor(clampi(tl.X0 + xx - R, 0, a.W - 1), a.s, m);
+            float wt[4];
+            keys_weights(m, a.s, wt);
+            const float* r = V + third * MAXLRX + clampi(f - 1 - o.lx0, 0, MAXLRX - 4);
+            float* to = U + third * UP + xx;
+#pragma unroll 4
+            for (int i = 0; i < CM * UH / 3; ++i, r += 3 * MAXLRX, to += 3 * UP) *to = dot4(wt, r[0], r[1], r[2], r[3]);
+            if (CM * UH % 3 && third < CM * UH % 3) *to = dot4(wt, r[0], r[1], r[2], r[3]);
         }
         __syncthreads();
 
@@ -235,87 +251,111 @@ void k_list_grad_mfma(const ListGradArgs a) {
             GradFetch<CM, TQ> f = next;
             if (u + 1 < UNITS || !last) fetch(next, u + 1 < UNITS ? tl : tn, (u + 1) % UNITS);
             if (Y >= a.H || tl.X0 + x0 >= a.W) continue;
-            unsigned word[2][NS][8];                 // E as (high, low) halves, of the pixel's own scale
-            int ex[2];
-            const char* const Ub = (const char*)U + 4 * (u / 2 * UW + x0);
+            const char* const Ub = (const char*)U + 4 * (u / 2 * UP + x0);
+            // Entries go into the dense columns.  An atom that a pixel lists twice has one place there: every entry writes its number, those
+            // that find another's wait for a later pass (lists as the router makes them: one pass).  The array is all zero between uses.
+            bool inside[2], on[2];
+            int cur[2][TQ];
+            unsigned seen[2][TQ];
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const int X = tl.X0 + x0 + 16 * g + n;
-                const bool inside = X < a.W, on = inside && f.on[g] != 0;
-                float dy[CM];
-#pragma unroll
-                for (int c = 0; c < CM; ++c) {
-                    const float v = a.io_f16 ? __half2float(__ushort_as_half((unsigned short)f.dy[g][c])) : __uint_as_float(f.dy[g][c]);
-                    dy[c] = on ? v : 0.0f;
-                }
+                inside[g] = tl.X0 + x0 + 16 * g + n < a.W;
+                on[g] = inside[g] && f.on[g] != 0;
 #pragma unroll
                 for (int r = 0; r < TQ; ++r) {
                     f.idx[g][r] = f.idx[g][r] < lmax ? f.idx[g][r] : lmax;
-                    f.val[g][r] = on ? f.val[g][r] : 0u;
-                }
-                float E[NS][8], m = 0.0f;
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const char* p = Ub + tap[s][i];
-                        float e = dy[0] * *(const float*)(p + 64 * g);
-#pragma unroll
-                        for (int c = 1; c < CM; ++c) e = fmaf(dy[c], *(const float*)(p + 64 * g + 4 * c * UH * UW), e);
-                        E[s][i] = e;
-                        m = fmaxf(m, fabsf(e));
-                    }
-                m = fmaxf(m, __shfl_xor(m, 16));
-                m = fmaxf(m, __shfl_xor(m, 32));
-                ex[g] = exponent_field(m);
-                const float sc = pow2_field(268 - ex[g]);
-                u32x4v Eh[NS], El[NS];
-#pragma unroll
-                for (int s = 0; s < NS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        unsigned hi, lo;
-                        split_pair(E[s][2 * i] * sc, E[s][2 * i + 1] * sc, hi, lo);
-                        Eh[s][i] = hi, El[s][i] = lo;
-                        word[g][s][2 * i] = __builtin_amdgcn_perm(lo, hi, 0x05040100u);
-                        word[g][s][2 * i + 1] = __builtin_amdgcn_perm(lo, hi, 0x07060302u);
-                    }
-                if (a.dvalue) {
-                    wave_lds_fence();
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        float4v r = {0, 0, 0, 0};
-#pragma unroll
-                        for (int s = 0; s < NS; ++s) {
-                            const half8 dh = __builtin_bit_cast(half8, Dh[mt][s]), dl = __builtin_bit_cast(half8, Dl[mt][s]);
-                            const half8 eh = __builtin_bit_cast(half8, Eh[s]), el = __builtin_bit_cast(half8, El[s]);
-                            r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dl, eh, r, 0, 0, 0);
-                            r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, el, r, 0, 0, 0);
-                            r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, eh, r, 0, 0, 0);
-                        }
-                        *(lds_f4*)(er + 4 * (n * F::RP + 16 * mt + 4 * q)) = r;
-                    }
-                    wave_lds_fence();
-                    const float back = pow2_field(ex[g] - 14);
-                    float v[TQ];
-#pragma unroll
-                    for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
-                    if (inside) {
-                        TV* const to = (TV*)a.dvalue + ((int64_t)tl.im * a.T * plane + (int64_t)Y * a.W + tl.X0 + x0);
-#pragma unroll
-                        for (int r = 0; r < TQ; ++r)
-                            if (4 * r + q < a.T) st_from_float(to + 4 * r * plane, (unsigned)q * (unsigned)plane + 16 * g + n, on ? v[r] : 0.0f);
-                    }
+                    f.val[g][r] = on[g] ? f.val[g][r] : 0u;
+                    cur[g][r] = 2 * ((4 * r + q < a.T ? (int)f.idx[g][r] : LP) * F::PP + 16 * g + n);
+                    if (rec) *(lds_h*)(phi + cur[g][r]) = (unsigned short)(4 * r + q + 1);
                 }
             }
             if (rec) {
-                // the unit's scale, its values' scale; E to [tap][pixel]
+                wave_lds_fence();
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
+            }
+            u32x4v Eh[2][NS], El[2][NS];             // E of the pixel's own scale, high and low parts
+            int ex[2];
+#pragma unroll
+            for (int g0 = 0; g0 < 2; g0 += F::RG) {
+#pragma unroll
+                for (int g = g0; g < g0 + F::RG; ++g) {
+                    float dy[CM];
+#pragma unroll
+                    for (int c = 0; c < CM; ++c) {
+                        const float v = a.io_f16 ? __half2float(__ushort_as_half((unsigned short)f.dy[g][c])) : __uint_as_float(f.dy[g][c]);
+                        dy[c] = on[g] ? v : 0.0f;
+                    }
+                    float E[NS][8], m = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            const char* p = Ub + tap[s][i];
+                            float e = dy[0] * *(const float*)(p + 64 * g);
+#pragma unroll
+                            for (int c = 1; c < CM; ++c) e = fmaf(dy[c], *(const float*)(p + 64 * g + 4 * c * UH * UP), e);
+                            E[s][i] = e;
+                            m = fmaxf(m, fabsf(e));
+                        }
+#pragma unroll
+                        for (int i = NI; i < 8; ++i) E[s][i] = 0.0f;
+                    }
+                    m = fmaxf(m, __shfl_xor(m, 16));
+                    m = fmaxf(m, __shfl_xor(m, 32));
+                    ex[g] = exponent_field(m);
+                    const float sc = pow2_field(268 - ex[g]);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            unsigned hi = 0, lo = 0;
+                            if (2 * i < NI) split_pair(E[s][2 * i] * sc, E[s][2 * i + 1] * sc, hi, lo);
+                            Eh[g][s][i] = hi, El[g][s][i] = lo;
+                        }
+                }
+                if (a.dvalue) {
+#pragma unroll
+                    for (int g = g0; g < g0 + F::RG; ++g)
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            float4v r = {0, 0, 0, 0};
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) {
+                                const half8 dh = __builtin_bit_cast(half8, Dh[mt][s]), dl = __builtin_bit_cast(half8, Dl[mt][s]);
+                                const half8 eh = __builtin_bit_cast(half8, Eh[g][s]), el = __builtin_bit_cast(half8, El[g][s]);
+                                r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dl, eh, r, 0, 0, 0);
+                                r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, el, r, 0, 0, 0);
+                                r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, eh, r, 0, 0, 0);
+                            }
+                            *(lds_f4*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + 16 * mt + 4 * q)) = r;
+                        }
+                    wave_lds_fence();
+#pragma unroll
+                    for (int g = g0; g < g0 + F::RG; ++g) {
+                        const float back = pow2_field(ex[g] - 14);
+                        float v[TQ];
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
+                        if (inside[g]) {
+                            TV* const to = (TV*)a.dvalue + ((int64_t)tl.im * a.T * plane + (int64_t)Y * a.W + tl.X0 + x0);
+#pragma unroll
+                            for (int r = 0; r < TQ; ++r)
+                                if (4 * r + q < a.T) st_from_float(to + 4 * r * plane, (unsigned)q * (unsigned)plane + 16 * g + n, on[g] ? v[r] : 0.0f);
+                        }
+                    }
+                    wave_lds_fence();
+                }
+            }
+            if (rec) {
+                // the unit's scale, its values' scale; E to [tap][pixel] as words of (high, low)
                 int es = max(ex[0], ex[1]);
 #pragma unroll
                 for (int d = 8; d > 0; d >>= 1) es = max(es, __shfl_xor(es, d));
                 float vback = 1.0f;
                 unsigned val[2][TQ], vlo[2][F::SPLIT ? TQ : 1];
-                int cur[2][TQ];
                 if (F::SPLIT) {
                     float m = 0.0f;
 #pragma unroll
@@ -333,7 +373,6 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) split_pair(__uint_as_float(f.val[g][r]) * vsc, 0.0f, val[g][r], vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0]);
                 }
-                wave_lds_fence();
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const _Float16 fs = (_Float16)pow2_field(127 + ex[g] - es);
@@ -341,15 +380,13 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                     for (int s = 0; s < NS; ++s)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const half2v v = __builtin_bit_cast(half2v, word[g][s][i]) * ff;
-                            *(lds_u*)(er + 4 * ((32 * s + 8 * q + i) * F::EP + 16 * g + n)) = __builtin_bit_cast(unsigned, v);
+                        for (int i = 0; i < NI; ++i) {
+                            const unsigned w = __builtin_amdgcn_perm(El[g][s][i / 2], Eh[g][s][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+                            *(lds_u*)(er + 4 * ((32 * s + 8 * q + i) * F::EP + 16 * g + n)) = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, w) * ff);
                         }
 #pragma unroll
-                    for (int r = 0; r < TQ; ++r) {
+                    for (int r = 0; r < TQ; ++r)
                         if (!F::SPLIT) val[g][r] = f.val[g][r];
-                        cur[g][r] = 2 * ((4 * r + q < a.T ? (int)f.idx[g][r] : LP) * F::PP + 16 * g + n);
-                    }
                 }
                 wave_lds_fence();
                 half8 eh[NT], el[NT];
@@ -368,24 +405,9 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     eh[t] = __builtin_bit_cast(half8, h), el[t] = __builtin_bit_cast(half8, l);
                 }
                 const float back = pow2_field(es - 14) * vback;
-                // Entries into the dense columns.  An atom that a pixel lists twice has one place there: every entry writes its number, those that
-                // find another's wait for the next pass (lists as the router makes them: one pass).  The array is all zero between uses.
-                bool more;
-#pragma unroll 1
-                do {
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int r = 0; r < TQ; ++r) *(lds_h*)(phi + cur[g][r]) = (unsigned short)(4 * r + q + 1);
-                    wave_lds_fence();
-                    unsigned seen[2][TQ];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
-                    wave_lds_fence();
+                while (true) {
                     int put[2][TQ];
-                    more = false;
+                    bool more = false;
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -423,7 +445,18 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = 0;
                         }
                     wave_lds_fence();
-                } while (__any(more));
+                    if (!__any(more)) break;
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r) *(lds_h*)(phi + cur[g][r]) = (unsigned short)(4 * r + q + 1);
+                    wave_lds_fence();
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
+                    wave_lds_fence();
+                }
             }
         }
         // ---- the sums handed on, the wavefronts one after the other (G is 16 x 16 tiles: lane (q, n) has atoms 4 q .. 4 q + 3 of tap n)
@@ -439,14 +472,15 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            const int j = j0 + 16 * t, l = l0 + 16 * mt;
+                            const int place = j0 + 16 * t, l = l0 + 16 * mt;
+                            const int j = F::tap(place / 32, place / 8 % 4, place % 8);
                             double* const at = rec + l * KK + j;
                             double was[4];
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) was[r] = !fresh && l + r < a.L && j < KK ? at[r * KK] : 0.0;
+                            for (int r = 0; r < 4; ++r) was[r] = !fresh && l + r < a.L && j >= 0 ? at[r * KK] : 0.0;
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                if (l + r < a.L && j < KK) at[r * KK] = was[r] + (double)G[mt][t][r];
+                                if (l + r < a.L && j >= 0) at[r * KK] = was[r] + (double)G[mt][t][r];
                                 G[mt][t][r] = 0.0f;
                             }
                         }
