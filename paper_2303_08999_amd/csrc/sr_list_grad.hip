@@ -157,8 +157,8 @@ bool overlap(const void* p, size_t np, const void* q, size_t nq) {
 
 bool list_grad_mfma_supported(const ListGradArgs& a, int k) {
     (void)k;
-    // three planes of values lie within 32-bit offsets
-    return a.T <= 16 && a.L <= 128 && (a.C == 1 || a.C == 3) && (int64_t)a.H * a.W < (int64_t)1 << 28 &&
+    // an image's lists and its dout lie within 32-bit offsets, as bytes of fp32
+    return a.T <= 16 && a.L <= 128 && (a.C == 1 || a.C == 3) && (int64_t)a.H * a.W * (a.T > 3 ? a.T : 3) < (int64_t)1 << 30 &&
            (int64_t)a.N * ((a.W + GM_TW - 1) / GM_TW) * ((a.H + GM_TH - 1) / GM_TH) < (int64_t)1 << 30;
 }
 

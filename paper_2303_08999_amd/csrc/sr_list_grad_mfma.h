@@ -10,8 +10,9 @@
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
 // numbers, 22 bits; D likewise with one power of two; R takes the three products that matter.  For G the pixels of a unit share
-// the largest one's power of two (parts below 2^-38 of it are lost), fp16 values enter as they are, fp32 ones split as well; a
-// unit's sums are added in fp32, unscaled, and handed on in double after at most 4096 pixels of a wavefront.
+// the largest one's power of two (or up to eight times that: parts below 2^-35 of it are lost).  fp16 values enter as they are and
+// the sums stay in the matrix instructions; fp32 ones are split as well, and a unit's sums are added unscaled.  Both are fp32, and
+// handed on in double after at most 4096 pixels of a wavefront.
 #pragma once
 #include "sr_list_grad.h"
 
@@ -49,6 +50,8 @@ struct GradCfg {
     static constexpr int ER_0 = 32 * NS * EP * 4 > RG * R_B ? 32 * NS * EP * 4 : RG * R_B;
     static constexpr int ER_B = ER_0 > VN * 4 ? ER_0 : (VN * 4 + 15) / 16 * 16;
     static constexpr int WAVE_B = PHI_B + ER_B;
+    static constexpr bool DL = K == 7 && LP > 80 && !SPLIT;                            // D's operands in LDS, not in 128 registers
+    static constexpr bool ACC = !SPLIT;            // G is summed by the matrix instructions, under one power of two
     static constexpr int WPE = K == 7 || LP > 80 || SPLIT ? 1 : 2;                     // wavefronts per SIMD (registers, LDS)
     static_assert(CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
     // the tap at a place, or -1
@@ -69,10 +72,10 @@ __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float(
 // exponent field of a magnitude, from 15 on: its reciprocal scale below stays a number
 __device__ __forceinline__ int exponent_field(float m) { return clampi((int)(__float_as_uint(m) >> 23), 15, 254); }
 
-// x and y scaled into fp16's range -> words (high part, low part)
-__device__ __forceinline__ void split_pair(float x, float y, unsigned& hi, unsigned& lo) {
-    const auto h = __builtin_amdgcn_cvt_pkrtz(x, y);
-    const auto l = __builtin_amdgcn_cvt_pkrtz(x - (float)h[0], y - (float)h[1]);
+// x and y, times sc into fp16's range -> words (high part, low part); sc is a power of two
+__device__ __forceinline__ void split_pair(float x, float y, float sc, unsigned& hi, unsigned& lo) {
+    const auto h = __builtin_amdgcn_cvt_pkrtz(x * sc, y * sc);
+    const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf(x, sc, -(float)h[0]), fmaf(y, sc, -(float)h[1]));
     __builtin_memcpy(&hi, &h, 4);
     __builtin_memcpy(&lo, &l, 4);
 }
@@ -95,6 +98,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     __shared__ int yb[UH];
     __shared__ __align__(16) unsigned char scratch[4][F::WAVE_B];
     __shared__ float dmax[4];
+    __shared__ u32x4v Dsh[F::DL ? 2 * MT * NS * 64 : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, n = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -114,24 +118,28 @@ void k_list_grad_mfma(const ListGradArgs a) {
     __syncthreads();
     const int dx = exponent_field(fmaxf(fmaxf(dmax[0], dmax[1]), fmaxf(dmax[2], dmax[3])));
     const float dscale = pow2_field(268 - dx), dback = pow2_field(dx - 14);
-    u32x4v Dh[MT][NS], Dl[MT][NS];
+    u32x4v Dh[F::DL ? 1 : MT][NS], Dl[F::DL ? 1 : MT][NS];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
+            if (F::DL && (mt & 3) != wave) continue;
             const int l = 16 * mt + n;
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int j = F::tap(s, q, i);
-                v[i] = l < a.L && j >= 0 ? a.dict[l * KK + j] * dscale : 0.0f;
+                v[i] = l < a.L && j >= 0 ? a.dict[l * KK + j] : 0.0f;
             }
+            u32x4v dh, dl;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 unsigned hi, lo;
-                split_pair(v[2 * i], v[2 * i + 1], hi, lo);
-                Dh[mt][s][i] = hi, Dl[mt][s][i] = lo;
+                split_pair(v[2 * i], v[2 * i + 1], dscale, hi, lo);
+                dh[i] = hi, dl[i] = lo;
             }
+            if (F::DL) Dsh[F::DL ? 2 * (mt * NS + s) * 64 + lane : 0] = dh, Dsh[F::DL ? (2 * (mt * NS + s) + 1) * 64 + lane : 0] = dl;
+            else Dh[F::DL ? 0 : mt][s] = dh, Dl[F::DL ? 0 : mt][s] = dl;
         }
     // where a lane's taps are in the tile, from the wavefront's first row on, in bytes (places without one: the patch's last tap; their
     // responses meet zeros of D, their columns of G are not handed on)
@@ -150,7 +158,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
         for (int t = 0; t < NT; ++t) G[mt][t] = (float4v){0, 0, 0, 0};
     double* const rec = a.partial ? a.partial + (size_t)blockIdx.x * a.L * KK : nullptr;
     bool first = true;
-    int held = 0;
+    int held = 0, scale = 15;                        // G times 2^(scale - 14) is the sum (ACC)
 
     struct Tile { int im, Y0, X0; };
     auto tile_at = [&](unsigned t) -> Tile {
@@ -158,28 +166,33 @@ void k_list_grad_mfma(const ListGradArgs a) {
         return {(int)im, (int)ty * GM_TH, (int)(in - ty * (unsigned)a.tiles_x) * GM_TW};
     };
     // Requests a unit: lane (q, n) has of pixel n of either group the entries 4 r + q.  Every address is one of the tensors'; what is outside of
-    // the image or the list is set aside when it is used.
+    // the image or the list is set aside when it is used.  An image's lists and its dout lie within 32-bit offsets.
+    const unsigned pl = (unsigned)plane;
+    unsigned entry[TQ];
+#pragma unroll
+    for (int r = 0; r < TQ; ++r) entry[r] = (unsigned)min(4 * r + q, a.T - 1) * pl;
     auto fetch = [&](GradFetch<CM, TQ>& f, const Tile& t, int u) {
         const int Y = min(t.Y0 + wave * (GM_TH / 4) + u / 2, a.H - 1), X = min(t.X0 + u % 2 * 32, a.W - 1);
-        const int64_t at = (int64_t)Y * a.W + X;     // the same for the whole wavefront
+        const unsigned at = (unsigned)Y * (unsigned)a.W + (unsigned)X;     // the same for the whole wavefront
+        const unsigned char* const index = a.index + (int64_t)t.im * a.T * plane;
+        const char* const value = (const char*)a.value + (int64_t)t.im * a.T * plane * VB;
+        const char* const dout = (const char*)a.dout + (int64_t)t.im * CM * plane * (a.io_f16 ? 2 : 4);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-            const unsigned x = (unsigned)min(16 * g + n, a.W - 1 - X);
-            f.on[g] = a.mask ? (unsigned)(a.mask + (int64_t)t.im * plane + at)[x] : 1u;
+            const unsigned x = at + (unsigned)min(16 * g + n, a.W - 1 - X);
+            f.on[g] = a.mask ? (unsigned)(a.mask + (int64_t)t.im * plane)[x] : 1u;
             if (a.io_f16) {
 #pragma unroll
-                for (int c = 0; c < CM; ++c) f.dy[g][c] = ((const unsigned short*)a.dout + ((int64_t)t.im * CM + c) * plane + at)[x];
+                for (int c = 0; c < CM; ++c) f.dy[g][c] = *(const unsigned short*)(dout + (unsigned)c * (pl * 2) + x * 2);
             } else {
 #pragma unroll
-                for (int c = 0; c < CM; ++c) f.dy[g][c] = ((const unsigned*)a.dout + ((int64_t)t.im * CM + c) * plane + at)[x];
+                for (int c = 0; c < CM; ++c) f.dy[g][c] = *(const unsigned*)(dout + (unsigned)c * (pl * 4) + x * 4);
             }
 #pragma unroll
             for (int r = 0; r < TQ; ++r) {
-                const int t0 = min(4 * r, a.T - 1);
-                const unsigned e = (unsigned)min(q, a.T - 1 - t0) * (unsigned)plane + x;
-                const int64_t base = ((int64_t)t.im * a.T + t0) * plane + at;
-                f.idx[g][r] = (a.index + base)[e];
-                f.val[g][r] = VB == 2 ? (unsigned)((const unsigned short*)a.value + base)[e] : ((const unsigned*)a.value + base)[e];
+                const unsigned e = entry[r] + x;
+                f.idx[g][r] = index[e];
+                f.val[g][r] = VB == 2 ? (unsigned)*(const unsigned short*)(value + e * 2) : *(const unsigned*)(value + e * 4);
             }
         }
     };
@@ -312,7 +325,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             unsigned hi = 0, lo = 0;
-                            if (2 * i < NI) split_pair(E[s][2 * i] * sc, E[s][2 * i + 1] * sc, hi, lo);
+                            if (2 * i < NI) split_pair(E[s][2 * i], E[s][2 * i + 1], sc, hi, lo);
                             Eh[g][s][i] = hi, El[g][s][i] = lo;
                         }
                 }
@@ -324,7 +337,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             float4v r = {0, 0, 0, 0};
 #pragma unroll
                             for (int s = 0; s < NS; ++s) {
-                                const half8 dh = __builtin_bit_cast(half8, Dh[mt][s]), dl = __builtin_bit_cast(half8, Dl[mt][s]);
+                                const half8 dh = __builtin_bit_cast(half8, F::DL ? Dsh[F::DL ? 2 * (mt * NS + s) * 64 + lane : 0] : Dh[F::DL ? 0 : mt][s]);
+                            const half8 dl = __builtin_bit_cast(half8, F::DL ? Dsh[F::DL ? (2 * (mt * NS + s) + 1) * 64 + lane : 0] : Dl[F::DL ? 0 : mt][s]);
                                 const half8 eh = __builtin_bit_cast(half8, Eh[g][s]), el = __builtin_bit_cast(half8, El[g][s]);
                                 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dl, eh, r, 0, 0, 0);
                                 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, el, r, 0, 0, 0);
@@ -340,10 +354,11 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
                         if (inside[g]) {
-                            TV* const to = (TV*)a.dvalue + ((int64_t)tl.im * a.T * plane + (int64_t)Y * a.W + tl.X0 + x0);
+                            char* const to = (char*)a.dvalue + (int64_t)tl.im * a.T * plane * VB;
+                        const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);
 #pragma unroll
                             for (int r = 0; r < TQ; ++r)
-                                if (4 * r + q < a.T) st_from_float(to + 4 * r * plane, (unsigned)q * (unsigned)plane + 16 * g + n, on[g] ? v[r] : 0.0f);
+                                if (4 * r + q < a.T) st_from_float((TV*)(to + (entry[r] + x) * VB), 0, on[g] ? v[r] : 0.0f);
                         }
                     }
                     wave_lds_fence();
@@ -354,6 +369,22 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 int es = max(ex[0], ex[1]);
 #pragma unroll
                 for (int d = 8; d > 0; d >>= 1) es = max(es, __shfl_xor(es, d));
+                if (F::ACC) {
+                    // G's own power of two: at most four times the unit's, or G changes to the double of it
+                    es = __builtin_amdgcn_readfirstlane(es);
+                    if (es > scale || es < scale - 2) {
+                        const int to = min(es + 1, 254), by = scale - to;
+                        const float f1 = pow2_field(127 + by / 2), f2 = pow2_field(127 + by - by / 2);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) G[mt][t][i] = G[mt][t][i] * f1 * f2;
+                        scale = to;
+                    }
+                    es = scale;
+                }
                 float vback = 1.0f;
                 unsigned val[2][TQ], vlo[2][F::SPLIT ? TQ : 1];
                 if (F::SPLIT) {
@@ -371,7 +402,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) split_pair(__uint_as_float(f.val[g][r]) * vsc, 0.0f, val[g][r], vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0]);
+                        for (int r = 0; r < TQ; ++r) split_pair(__uint_as_float(f.val[g][r]), 0.0f, vsc, val[g][r], vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0]);
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
@@ -428,12 +459,14 @@ void k_list_grad_mfma(const ListGradArgs a) {
                         if (F::SPLIT) p1 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((F::PHI_ROWS + 16 * mt + n) * F::PP + 8 * q)));
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            float4v r = {0, 0, 0, 0};
+                            float4v r = F::ACC ? G[mt][t] : (float4v){0, 0, 0, 0};
                             if (F::SPLIT) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, eh[t], r, 0, 0, 0);
                             r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, el[t], r, 0, 0, 0);
                             r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, eh[t], r, 0, 0, 0);
+                            if (F::ACC) G[mt][t] = r;
+                            else
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) G[mt][t][i] = fmaf(r[i], back, G[mt][t][i]);
+                                for (int i = 0; i < 4; ++i) G[mt][t][i] = fmaf(r[i], back, G[mt][t][i]);
                         }
                     }
                     wave_lds_fence();
@@ -468,6 +501,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     int l0 = 4 * q, j0 = n;          // (hidden: no address of a record is worth a register for the whole tile)
                     asm volatile("" : "+v"(l0), "+v"(j0));
                     const bool fresh = first && w == 0;
+                    const float back = F::ACC ? pow2_field(scale - 14) : 1.0f;
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -480,7 +514,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             for (int r = 0; r < 4; ++r) was[r] = !fresh && l + r < a.L && j >= 0 ? at[r * KK] : 0.0;
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                if (l + r < a.L && j >= 0) at[r * KK] = was[r] + (double)G[mt][t][r];
+                                if (l + r < a.L && j >= 0) at[r * KK] = was[r] + (double)(G[mt][t][r] * back);
                                 G[mt][t][r] = 0.0f;
                             }
                         }
