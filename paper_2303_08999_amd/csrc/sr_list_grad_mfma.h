@@ -67,6 +67,21 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
+// The largest of a row of 16 lanes, in all of them; over the four rows of a wavefront.
+template <int CTRL> __device__ __forceinline__ int row_turned(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+__device__ __forceinline__ int row_max(int v) {
+    v = max(v, row_turned<0x128>(v));                // row_ror 8, 4, 2, 1
+    v = max(v, row_turned<0x124>(v));
+    v = max(v, row_turned<0x122>(v));
+    return max(v, row_turned<0x121>(v));
+}
+__device__ __forceinline__ float rows_max(float v) {
+    const unsigned u = __float_as_uint(v);           // magnitudes: their order is that of their bits
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned b = max(a[0], a[1]);
+    const auto c = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return __uint_as_float(max(c[0], c[1]));
+}
 // 2^n for an exponent field (n + 127), kept where fp32 has it
 __device__ __forceinline__ float pow2_field(int field) { return __uint_as_float((unsigned)clampi(field, 1, 254) << 23); }
 // exponent field of a magnitude, from 15 on: its reciprocal scale below stays a number
@@ -167,7 +182,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     };
     // Requests a unit: lane (q, n) has of pixel n of either group the entries 4 r + q.  Every address is one of the tensors'; what is outside of
     // the image or the list is set aside when it is used.  An image's lists and its dout lie within 32-bit offsets.
-    const unsigned pl = (unsigned)plane;
+    const unsigned pl = (unsigned)plane, half_io = a.io_f16 ? ~0u : 0u;
     unsigned entry[TQ];
 #pragma unroll
     for (int r = 0; r < TQ; ++r) entry[r] = (unsigned)min(4 * r + q, a.T - 1) * pl;
@@ -197,10 +212,32 @@ void k_list_grad_mfma(const ListGradArgs a) {
         }
     };
 
+    // Requests a tile's LR rows, one a wavefront at a time, a tile ahead.
+    constexpr int LRI = (CM * MAXLRY + 3) / 4;
+    unsigned lrv[LRI];
+    auto fetch_lr = [&](const Tile& t) {
+        const TileOrigin o = tile_origin(t.Y0, t.X0, R, UH, UW, a.H, a.W, a.s);
+        const unsigned x = (unsigned)clampi(o.lx0 + min(lane, MAXLRX - 1), 0, a.w - 1);
+        if (a.io_f16) {
+#pragma unroll
+            for (int i = 0; i < LRI; ++i) {
+                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
+                lrv[i] = ((const unsigned short*)a.lr + (((int64_t)t.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w)[x];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LRI; ++i) {
+                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
+                lrv[i] = ((const unsigned*)a.lr + (((int64_t)t.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w)[x];
+            }
+        }
+    };
+
     const unsigned tiles = (unsigned)a.tiles;
     unsigned tile = blockIdx.x;
     GradFetch<CM, TQ> next;
     Tile tn = tile_at(tile);
+    fetch_lr(tn);
     fetch(next, tn, 0);
     for (; tile < tiles; tile += gridDim.x) {
         const Tile tl = tn;
@@ -218,17 +255,10 @@ void k_list_grad_mfma(const ListGradArgs a) {
             yw[tid] = make_float4(wt[0], wt[1], wt[2], wt[3]);
             yb[tid] = clampi(f - 1 - o.ly0, 0, MAXLRY - 4);
         }
-        {
-            const int rx = min(lane, MAXLRX - 1), x = clampi(o.lx0 + rx, 0, a.w - 1);
-            float v[(CM * MAXLRY + 3) / 4];
 #pragma unroll
-            for (int i = 0; i < (CM * MAXLRY + 3) / 4; ++i) {
-                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
-                const int64_t at = (((int64_t)tl.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w;
-                v[i] = a.io_f16 ? __half2float(((const __half*)a.lr + at)[x]) : ((const float*)a.lr + at)[x];
-            }
-#pragma unroll
-            for (int i = 0; i < (CM * MAXLRY + 3) / 4; ++i) U[min(wave + 4 * i, CM * MAXLRY - 1) * MAXLRX + rx] = v[i];
+        for (int i = 0; i < LRI; ++i) {
+            const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)lrv[i])));
+            U[min(wave + 4 * i, CM * MAXLRY - 1) * MAXLRX + min(lane, MAXLRX - 1)] = __uint_as_float((h & half_io) | (lrv[i] & ~half_io));
         }
         __syncthreads();
         {
@@ -256,6 +286,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
             if (CM * UH % 3 && third < CM * UH % 3) *to = dot4(wt, r[0], r[1], r[2], r[3]);
         }
         __syncthreads();
+
+        if (!last) fetch_lr(tn);
 
         // ---- a wavefront's units: 32 pixels of a row, two groups of 16
 #pragma unroll 1
@@ -298,7 +330,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     float dy[CM];
 #pragma unroll
                     for (int c = 0; c < CM; ++c) {
-                        const float v = a.io_f16 ? __half2float(__ushort_as_half((unsigned short)f.dy[g][c])) : __uint_as_float(f.dy[g][c]);
+                        const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)f.dy[g][c])));
+                    const float v = __uint_as_float((h & half_io) | (f.dy[g][c] & ~half_io));      // (a select: no branch cuts the unit here)
                         dy[c] = on[g] ? v : 0.0f;
                     }
                     float E[NS][8], m = 0.0f;
@@ -316,8 +349,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int i = NI; i < 8; ++i) E[s][i] = 0.0f;
                     }
-                    m = fmaxf(m, __shfl_xor(m, 16));
-                    m = fmaxf(m, __shfl_xor(m, 32));
+                    m = rows_max(m);
                     ex[g] = exponent_field(m);
                     const float sc = pow2_field(268 - ex[g]);
 #pragma unroll
@@ -366,9 +398,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
             }
             if (rec) {
                 // the unit's scale, its values' scale; E to [tap][pixel] as words of (high, low)
-                int es = max(ex[0], ex[1]);
-#pragma unroll
-                for (int d = 8; d > 0; d >>= 1) es = max(es, __shfl_xor(es, d));
+                int es = row_max(max(ex[0], ex[1]));
                 if (F::ACC) {
                     // G's own power of two: at most four times the unit's, or G changes to the double of it
                     es = __builtin_amdgcn_readfirstlane(es);
@@ -394,8 +424,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int r = 0; r < TQ; ++r)
                             if (4 * r + q < a.T) m = fmaxf(m, fabsf(__uint_as_float(f.val[g][r])));
-#pragma unroll
-                    for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+                    m = rows_max(__int_as_float(row_max(__float_as_int(m))));
                     const int vx = exponent_field(m);
                     const float vsc = pow2_field(268 - vx);
                     vback = pow2_field(vx - 14);
