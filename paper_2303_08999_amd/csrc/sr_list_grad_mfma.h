@@ -53,7 +53,7 @@ struct GradCfg {
     static constexpr bool DL = K == 7 && LP > 80 && !SPLIT;                            // D's operands in LDS, not in 128 registers
     static constexpr bool ACC = !SPLIT;            // G is summed by the matrix instructions, under one power of two
     static constexpr int WPE = K == 7 || LP > 80 || SPLIT ? 1 : 2;                     // wavefronts per SIMD (registers, LDS)
-    static_assert(CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
+    static_assert(LP * 16 * 4 <= ER_B && CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
     // the tap at a place, or -1
     static __device__ __forceinline__ int tap(int s, int q, int i) {
         const int row = 4 * s + q;
@@ -175,10 +175,10 @@ void k_list_grad_mfma(const ListGradArgs a) {
     bool first = true;
     int held = 0, scale = 15;                        // G times 2^(scale - 14) is the sum (ACC)
 
-    struct Tile { int im, Y0, X0; };
+    struct Tile { int im, Y0, X0; int64_t list, image; };   // (elements before its lists, before its dout)
     auto tile_at = [&](unsigned t) -> Tile {
         const unsigned per = (unsigned)a.tiles_x * (unsigned)a.tiles_y, im = t / per, in = t - im * per, ty = in / (unsigned)a.tiles_x;
-        return {(int)im, (int)ty * GM_TH, (int)(in - ty * (unsigned)a.tiles_x) * GM_TW};
+        return {(int)im, (int)ty * GM_TH, (int)(in - ty * (unsigned)a.tiles_x) * GM_TW, (int64_t)im * a.T * plane, (int64_t)im * CM * plane};
     };
     // Requests a unit: lane (q, n) has of pixel n of either group the entries 4 r + q.  Every address is one of the tensors'; what is outside of
     // the image or the list is set aside when it is used.  An image's lists and its dout lie within 32-bit offsets.
@@ -189,9 +189,9 @@ void k_list_grad_mfma(const ListGradArgs a) {
     auto fetch = [&](GradFetch<CM, TQ>& f, const Tile& t, int u) {
         const int Y = min(t.Y0 + wave * (GM_TH / 4) + u / 2, a.H - 1), X = min(t.X0 + u % 2 * 32, a.W - 1);
         const unsigned at = (unsigned)Y * (unsigned)a.W + (unsigned)X;     // the same for the whole wavefront
-        const unsigned char* const index = a.index + (int64_t)t.im * a.T * plane;
-        const char* const value = (const char*)a.value + (int64_t)t.im * a.T * plane * VB;
-        const char* const dout = (const char*)a.dout + (int64_t)t.im * CM * plane * (a.io_f16 ? 2 : 4);
+        const unsigned char* const index = a.index + t.list;
+        const char* const value = (const char*)a.value + t.list * VB;
+        const char* const dout = (const char*)a.dout + t.image * (a.io_f16 ? 2 : 4);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const unsigned x = at + (unsigned)min(16 * g + n, a.W - 1 - X);
@@ -212,24 +212,27 @@ void k_list_grad_mfma(const ListGradArgs a) {
         }
     };
 
-    // Requests a tile's LR rows, one a wavefront at a time, a tile ahead.
-    constexpr int LRI = (CM * MAXLRY + 3) / 4;
-    unsigned lrv[LRI];
+    // Requests a tile's LR rows, every fourth one a wavefront's, a tile ahead.  (An image's channels lie within 32-bit offsets.)
+    constexpr int LRI = (MAXLRY + 3) / 4, VI = (UH + 3) / 4;
+    const int lane_x = min(lane, MAXLRX - 1);
+    unsigned lrv[CM][LRI];
     auto fetch_lr = [&](const Tile& t) {
         const TileOrigin o = tile_origin(t.Y0, t.X0, R, UH, UW, a.H, a.W, a.s);
-        const unsigned x = (unsigned)clampi(o.lx0 + min(lane, MAXLRX - 1), 0, a.w - 1);
+        const unsigned x = (unsigned)clampi(o.lx0 + lane_x, 0, a.w - 1), lp = (unsigned)a.h * (unsigned)a.w;
+        unsigned row[LRI];
+#pragma unroll
+        for (int i = 0; i < LRI; ++i) row[i] = (unsigned)clampi(o.ly0 + min(wave + 4 * i, MAXLRY - 1), 0, a.h - 1) * (unsigned)a.w;
+        const char* const lr = (const char*)a.lr + (int64_t)t.im * CM * lp * (a.io_f16 ? 2 : 4);
         if (a.io_f16) {
 #pragma unroll
-            for (int i = 0; i < LRI; ++i) {
-                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
-                lrv[i] = ((const unsigned short*)a.lr + (((int64_t)t.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w)[x];
-            }
+            for (int c = 0; c < CM; ++c)
+#pragma unroll
+                for (int i = 0; i < LRI; ++i) lrv[c][i] = *(const unsigned short*)(lr + ((unsigned)c * lp + row[i]) * 2 + x * 2);
         } else {
 #pragma unroll
-            for (int i = 0; i < LRI; ++i) {
-                const int p = min(wave + 4 * i, CM * MAXLRY - 1), c = p / MAXLRY, ry = p - c * MAXLRY;
-                lrv[i] = ((const unsigned*)a.lr + (((int64_t)t.im * CM + c) * a.h + clampi(o.ly0 + ry, 0, a.h - 1)) * a.w)[x];
-            }
+            for (int c = 0; c < CM; ++c)
+#pragma unroll
+                for (int i = 0; i < LRI; ++i) lrv[c][i] = *(const unsigned*)(lr + ((unsigned)c * lp + row[i]) * 4 + x * 4);
         }
     };
 
@@ -256,21 +259,22 @@ void k_list_grad_mfma(const ListGradArgs a) {
             yb[tid] = clampi(f - 1 - o.ly0, 0, MAXLRY - 4);
         }
 #pragma unroll
-        for (int i = 0; i < LRI; ++i) {
-            const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)lrv[i])));
-            U[min(wave + 4 * i, CM * MAXLRY - 1) * MAXLRX + min(lane, MAXLRX - 1)] = __uint_as_float((h & half_io) | (lrv[i] & ~half_io));
-        }
-        __syncthreads();
-        {
-            const int rx = min(lane, MAXLRX - 1);
-#pragma unroll 3
-            for (int i = 0; i < (CM * UH + 3) / 4; ++i) {
-                const int p = min(wave + 4 * i, CM * UH - 1), c = p / UH, yy = p - c * UH;
-                const float4 w4 = yw[yy];
-                const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
-                const float* r = U + (c * MAXLRY + yb[yy]) * MAXLRX + rx;
-                V[p * MAXLRX + rx] = dot4(wt, r[0], r[MAXLRX], r[2 * MAXLRX], r[3 * MAXLRX]);
+        for (int c = 0; c < CM; ++c)
+#pragma unroll
+            for (int i = 0; i < LRI; ++i) {
+                const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)lrv[c][i])));
+                U[(c * MAXLRY + min(wave + 4 * i, MAXLRY - 1)) * MAXLRX + lane_x] = __uint_as_float((h & half_io) | (lrv[c][i] & ~half_io));
             }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VI; ++i) {
+            const int yy = min(wave + 4 * i, UH - 1);
+            const float4 w4 = yw[yy];
+            const float wt[4] = {w4.x, w4.y, w4.z, w4.w};
+            const float* r = U + yb[yy] * MAXLRX + lane_x;
+#pragma unroll
+            for (int c = 0; c < CM; ++c, r += MAXLRY * MAXLRX)
+                V[(c * UH + yy) * MAXLRX + lane_x] = dot4(wt, r[0], r[MAXLRX], r[2 * MAXLRX], r[3 * MAXLRX]);
         }
         __syncthreads();
         {
@@ -386,7 +390,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
                         if (inside[g]) {
-                            char* const to = (char*)a.dvalue + (int64_t)tl.im * a.T * plane * VB;
+                            char* const to = (char*)a.dvalue + tl.list * VB;
                         const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);
 #pragma unroll
                             for (int r = 0; r < TQ; ++r)
@@ -521,34 +525,38 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 }
             }
         }
-        // ---- the sums handed on, the wavefronts one after the other (G is 16 x 16 tiles: lane (q, n) has atoms 4 q .. 4 q + 3 of tap n)
+        // ---- the wavefronts' sums to the record, 16 places of all atoms at a time, through the scratch (G is 16 x 16 tiles: lane (q, n) has
+        // atoms 4 q .. 4 q + 3 of place n)
         if (rec && (++held == 4096 / (GM_TW * GM_TH / 4) || last)) {
             held = 0;
-#pragma unroll 1
-            for (int w = 0; w < 4; ++w) {
-                if (wave == w) {
-                    int l0 = 4 * q, j0 = n;          // (hidden: no address of a record is worth a register for the whole tile)
-                    asm volatile("" : "+v"(l0), "+v"(j0));
-                    const bool fresh = first && w == 0;
-                    const float back = F::ACC ? pow2_field(scale - 14) : 1.0f;
+            const float back = F::ACC ? pow2_field(scale - 14) : 1.0f;
+            int id = tid;                            // (hidden: no address of a record is worth a register for the whole tile)
+            asm volatile("" : "+v"(id));
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            const int place = j0 + 16 * t, l = l0 + 16 * mt;
-                            const int j = F::tap(place / 32, place / 8 % 4, place % 8);
-                            double* const at = rec + l * KK + j;
-                            double was[4];
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) was[r] = !fresh && l + r < a.L && j >= 0 ? at[r * KK] : 0.0;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                if (l + r < a.L && j >= 0) at[r * KK] = was[r] + (double)(G[mt][t][r] * back);
-                                G[mt][t][r] = 0.0f;
-                            }
-                        }
-                }
+            for (int t = 0; t < NT; ++t) {
                 __syncthreads();
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        *(lds_f*)(er + 4 * ((16 * mt + 4 * q + r) * 16 + n)) = G[mt][t][r] * back;
+                        G[mt][t][r] = 0.0f;
+                    }
+                __syncthreads();
+                double was[MT];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const int l = 16 * i + id / 16, place = 16 * t + id % 16, j = F::tap(place / 32, place / 8 % 4, place % 8);
+                    was[i] = !first && l < a.L && j >= 0 ? rec[l * KK + j] : 0.0;
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const int l = 16 * i + id / 16, place = 16 * t + id % 16, j = F::tap(place / 32, place / 8 % 4, place % 8);
+                    double v = was[i];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v += (double)*(lds_f*)(scratch[w] + F::PHI_B + 4 * (256 * i + id));
+                    if (l < a.L && j >= 0) rec[l * KK + j] = v;
+                }
             }
             first = false;
         }
