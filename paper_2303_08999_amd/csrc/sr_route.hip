@@ -353,9 +353,9 @@ constexpr int64_t LANES_FROM = 2048;     // pixels
 int lanes_of(LaneArgs& a, const RouteArgs& r, sr_dtype z, sr_dtype v, const void* dz) {
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR, pre = r.layout == SR_COEFF_PRE_SHUFFLE;
     const int64_t es = (int64_t)route_esize(z);
-    const int G = pm ? 4 : (r.L <= 8 * LCH ? 1 : r.L <= 16 * LCH ? 2 : 4);
+    const int G = pm || r.L > 8 * LCH ? 4 : 1;
     if (r.T > 16 || r.total < LANES_FROM) return 0;
-    if (!pm && (G - 1) * 8 * r.lstride * es >= (int64_t)1 << 31) return 0;
+    if (G > 1 && 32 * r.lstride * es >= (int64_t)1 << 32) return 0;
     a.r = r;
     a.ipx = pre ? (int64_t)r.h * r.w : r.px;
     a.tiles_per_image = (a.ipx + 64 / G - 1) / (64 / G);

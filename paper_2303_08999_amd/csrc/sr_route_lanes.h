@@ -5,11 +5,30 @@
 // keep the atom beside the key (med3, a compare and two selects for each place).  The lists of a pixel's G lanes are merged as
 // bitonic sequences.  The softmax runs over the same registers once the largest logit is known: one pass over memory.
 #pragma once
+#include <type_traits>
+
 #include "sr_route.h"
 
 namespace srd {
 
-constexpr int LCH = 9;                   // chunks of 8 atoms that a lane holds: 72 atoms, times G
+// A pointer that is the same for the whole wavefront, kept in scalar registers from here on: what is added to it per lane stays apart, as the
+// 32-bit offset of a load or store.
+#define SR_GLOBAL __attribute__((address_space(1)))
+typedef char SR_GLOBAL* gptr;
+__device__ __forceinline__ gptr scalar(gptr p) {
+    asm("" : "+s"(p));
+    return p;
+}
+template <typename T> __device__ __forceinline__ T gload(gptr at, unsigned off) { return *(const T SR_GLOBAL*)(at + off); }
+template <typename T> __device__ __forceinline__ void gstore(gptr at, unsigned off, T v) { *(T SR_GLOBAL*)(at + off) = v; }
+
+// ... and that offset, made 64 bits wide only where it is used (widened once for a whole tile it takes an addition per access)
+__device__ __forceinline__ unsigned lane_offset(unsigned off) {
+    asm("" : "+v"(off));
+    return off;
+}
+
+constexpr int LCH = 9;                   // most chunks of 8 atoms that a lane holds: 72 atoms, times G
 
 // What the lanes of a pixel walk: images of ipx pixels, each with its logits lstride apart (the order before the pixel-shuffle is
 // s * s such images for every frame: one for each place under an LR pixel).
@@ -31,29 +50,40 @@ __device__ __forceinline__ unsigned med3u(unsigned a, unsigned b, unsigned c) {
     return d;
 }
 
-typedef short short2v __attribute__((ext_vector_type(2)));
+// A result as it is stored
+template <typename TZ> struct Stored { typedef unsigned short type; };
+template <> struct Stored<float> { typedef float type; };
+template <typename TZ> __device__ __forceinline__ typename Stored<TZ>::type as_stored(float v) {
+    TZ t;
+    typename Stored<TZ>::type u;
+    st_from_float(&t, 0, v);
+    __builtin_memcpy(&u, &t, sizeof(t));
+    return u;
+}
 
-// Eight logits as they are stored: 16-bit ones two in a word.
-template <typename TZ> struct Chunk {                        // __half, bf16raw
-    static constexpr int WORDS = 4;
-    unsigned w[4];
-    // atom 0 at `at + off` (`at` the same for the whole wavefront), the next `stride` bytes on; the first n of them
-    template <bool ALL> __device__ __forceinline__ void load(const char* at, unsigned off, int64_t stride, int n) {
-        unsigned v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j, at += stride) v[j] = ALL || j < n ? (unsigned)*(const unsigned short*)(at + off) : 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[2 * j] | (v[2 * j + 1] << 16);
+typedef short short2v __attribute__((ext_vector_type(2)));
+typedef unsigned vec4u __attribute__((ext_vector_type(4)));
+typedef float vec4f __attribute__((ext_vector_type(4)));
+
+// Eight logits as they are stored: those of a contiguous row (VEC) 16 bytes at a time, 16-bit ones two in a word; else one in a
+// register, where its load puts it: nothing is done to a load's result before all of a tile's loads are under way.
+template <typename TZ, bool VEC> struct Chunk {              // __half, bf16raw
+    unsigned w[VEC ? 4 : 8];
+    __device__ __forceinline__ void load(int j, gptr at, unsigned off) { w[VEC ? 0 : j] = gload<unsigned short>(at, off); }
+    __device__ __forceinline__ void load_row(gptr at, unsigned off) {
+        const vec4u v = gload<vec4u>(at, off);
+        w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
     }
-    __device__ __forceinline__ void load_vec(const char* at, unsigned off) {
-        const uint4 v = *(const uint4*)(at + off);
-        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    }
-    __device__ __forceinline__ float get(int j) const;
-    // signed order of the two logits of a word: negative ones mirrored, so that -0 is +0
+    __device__ __forceinline__ unsigned pair(int i) const { return VEC ? w[i] : w[VEC ? 0 : 2 * i] | (w[VEC ? 0 : 2 * i + 1] << 16); }
+    __device__ __forceinline__ unsigned bits(int j) const { return VEC ? (j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu) : w[VEC ? 0 : j]; }
+    static __device__ __forceinline__ float widen(unsigned b, const __half*) { return __half2float(__ushort_as_half((unsigned short)b)); }
+    static __device__ __forceinline__ float widen(unsigned b, const bf16raw*) { return __uint_as_float(b << 16); }
+    __device__ __forceinline__ float get(int j) const { return widen(bits(j), (const TZ*)nullptr); }
+    // signed order of the two logits of a pair: negative ones mirrored, so that -0 is +0
     __device__ __forceinline__ unsigned order2(int i) const {
+        const unsigned p = pair(i);
         short2v b, t, s;
-        __builtin_memcpy(&b, &w[i], 4);
+        __builtin_memcpy(&b, &p, 4);
         s = b >> 15;
         t = (short)-32768 - b;
         const short2v o = (t & s) | (b & ~s);
@@ -62,24 +92,12 @@ template <typename TZ> struct Chunk {                        // __half, bf16raw
         return u;
     }
 };
-template <> __device__ __forceinline__ float Chunk<__half>::get(int j) const {
-    __half h[2];
-    __builtin_memcpy(h, &w[j / 2], 4);
-    return __half2float(h[j & 1]);
-}
-template <> __device__ __forceinline__ float Chunk<bf16raw>::get(int j) const {
-    return __uint_as_float(j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
-}
-template <> struct Chunk<float> {
-    static constexpr int WORDS = 8;
+template <bool VEC> struct Chunk<float, VEC> {
     float w[8];
-    template <bool ALL> __device__ __forceinline__ void load(const char* at, unsigned off, int64_t stride, int n) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j, at += stride) w[j] = ALL || j < n ? *(const float*)(at + off) : 0.0f;
-    }
-    __device__ __forceinline__ void load_vec(const char* at, unsigned off) {
-        const float4 a = *(const float4*)(at + off), b = *(const float4*)(at + off + 16);
-        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    __device__ __forceinline__ void load(int j, gptr at, unsigned off) { w[j] = gload<float>(at, off); }
+    __device__ __forceinline__ void load_row(gptr at, unsigned off) {
+        const vec4f a = gload<vec4f>(at, off), b = gload<vec4f>(at, off + 16);
+        w[0] = a[0], w[1] = a[1], w[2] = a[2], w[3] = a[3], w[4] = b[0], w[5] = b[1], w[6] = b[2], w[7] = b[3];
     }
     __device__ __forceinline__ float get(int j) const { return w[j]; }
 };
@@ -97,7 +115,7 @@ template <typename TZ, int TC> struct TopList {              // 16-bit logits
         for (int i = TC - 1; i > 0; --i) k[i] = med3i(k[i - 1], x, k[i]);
         k[0] = x > k[0] ? x : k[0];
     }
-    template <bool ALL> __device__ __forceinline__ void insert(const Chunk<TZ>& c, int at, int n) {
+    template <bool ALL, bool VEC> __device__ __forceinline__ void insert(const Chunk<TZ, VEC>& c, int at, int n) {   // the first n are atoms
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const unsigned o = c.order2(i);
@@ -112,9 +130,7 @@ template <typename TZ, int TC> struct TopList {              // 16-bit logits
     }
     __device__ __forceinline__ float logit(int t) const {
         const int o = k[t] >> 16, b = o < 0 ? -32768 - o : o;
-        Chunk<TZ> c;
-        c.w[0] = (unsigned)b & 0xffffu;
-        return c.get(0);
+        return Chunk<TZ, false>::widen((unsigned)b & 0xffffu, (const TZ*)nullptr);
     }
     __device__ __forceinline__ void merge(int d) {
         int o[TC];
@@ -151,11 +167,14 @@ template <int TC> struct TopList<float, TC> {
         }
         id[0] = c[0] ? l : id[0];
         k[0] = c[0] ? x : k[0];
+#pragma unroll
+        for (int i = 0; i < TC; ++i) asm("" : "+v"(id[i]));  // (one key's selects are not to be mixed with the next one's)
     }
-    template <bool ALL> __device__ __forceinline__ void insert(const Chunk<float>& c, int at, int n) {
+    template <bool ALL, bool VEC> __device__ __forceinline__ void insert(const Chunk<float, VEC>& c, int at, int n) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const unsigned o = logit_order(c.w[j]);
+            __builtin_amdgcn_sched_barrier(0);               // one key at a time: each takes as many masks as there are places
             put(ALL || j < n ? (o > 1u ? o : 1u) : 0u, at + j);
         }
     }
@@ -226,24 +245,40 @@ __device__ __forceinline__ LanePixel lane_pixel(const LaneArgs& a, int64_t tile,
     return p;
 }
 
-// Loads the lane's atoms, (c G + g) 8 and on in chunk c.  L and the stride are hidden from the compiler, which would otherwise
-// keep the offsets of all planes and the comparisons of all chunks in registers from tile to tile (hundreds of spills).
-template <typename TZ, int G>
-__device__ __forceinline__ void load_chunks(Chunk<TZ> (&z)[LCH], const LaneArgs& a, const LanePixel& p, int L) {
+// Loads the lane's NC chunks: atoms (c G + g) 8 and on in chunk c.  FULL: all of them are there (L = 8 G NC); else places beyond the last atom
+// get some atom's logit, never an address beyond it, and are set aside when they are used.  There is no branch: all loads of a tile are under way
+// before the first is waited for.  The stride is hidden from the compiler, which would keep the offsets of all planes from tile to tile.
+template <typename TZ, int G, bool VEC, int NC, bool FULL>
+__device__ __forceinline__ void load_chunks(Chunk<TZ, VEC> (&z)[NC], const LaneArgs& a, const LanePixel& p, int L) {
     int64_t stride = a.r.lstride * (int64_t)sizeof(TZ);
     asm volatile("" : "+s"(stride));
-    const char* at = p.at;
+    gptr at = scalar((gptr)p.at);
+    if (VEC) {
 #pragma unroll
-    for (int c = 0; c < LCH; ++c, at += stride * (8 * G)) {
-        const int n = L - (c * G + p.g) * 8;
-        if (c * G * 8 < L) {
-            if (a.vec) {
-                if (n > 0) z[c].load_vec(at, p.off);
-            } else if ((c + 1) * G * 8 <= L) {
-                z[c].template load<true>(at, p.off, stride, 8);
-            } else {
-                z[c].template load<false>(at, p.off, stride, n);
+        for (int c = 0; c < NC; ++c) {
+            const int l = (c * G + p.g) * 8;
+            z[c].load_row(at, p.off + (unsigned)sizeof(TZ) * (unsigned)((FULL || l < L ? l : 0) - p.g * 8));
+        }
+    } else if (G == 1) {
+        const unsigned off = lane_offset(p.off);
+#pragma unroll
+        for (int l = 0; l < 8 * NC; ++l) {
+            z[l / 8].load(l % 8, at, off);
+            at = scalar(at + (FULL || l + 1 < L ? stride : 0));
+        }
+    } else {
+        const int last = (L - 1) / (8 * G);          // the last chunk that any lane has atoms in
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            // the lane's plane of the chunk, or the last atom's; from there on as long as there are atoms
+            const int l = (min(c, last) * G + p.g) * 8;
+            unsigned off = p.off - (unsigned)max(l - (L - 1), 0) * (unsigned)stride;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                z[c].load(j, at, lane_offset(off));
+                off += FULL || l + j + 1 < L ? (unsigned)stride : 0u;
             }
+            at = scalar(at + (FULL || c < last ? stride * (8 * G) : 0));
         }
     }
 }
@@ -272,19 +307,19 @@ template <int G> __device__ __forceinline__ float lanes_max(float v, int step) {
 
 constexpr int LNT = 256, LWAVES = LNT / 64;
 
-template <typename TZ, int TC, int G, bool STATS>
+template <typename TZ, int TC, int G, bool VEC, int NC, bool FULL, bool STATS>
 __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneArgs a) {
     const RouteArgs& r = a.r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR;
     const int step = pm ? 1 : 64 / G;    // from one of a pixel's lanes to the next
     __shared__ unsigned bins[STATS ? LWAVES * SR_MAX_ATOMS : 1];
-    float share[STATS ? LCH * 8 : 1];
+    float share[STATS ? NC * 8 : 1];
     unsigned live = 0;
     double sq = 0.0;
     if (STATS) {
 #pragma unroll
-        for (int j = 0; j < LCH * 8; ++j) share[j] = 0.0f;
+        for (int j = 0; j < NC * 8; ++j) share[j] = 0.0f;
         for (int l = threadIdx.x; l < LWAVES * SR_MAX_ATOMS; l += LNT) bins[l] = 0;
         __syncthreads();
     }
@@ -302,15 +337,16 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
         int L = r.L;
         int64_t px = r.px;
         asm volatile("" : "+s"(L), "+s"(px));
-        Chunk<TZ> z[LCH];
-        load_chunks<TZ, G>(z, a, p, L);
+        Chunk<TZ, VEC> z[NC];
+        load_chunks<TZ, G, VEC, NC, FULL>(z, a, p, L);
         TopList<TZ, TC> top;
         top.clear();
 #pragma unroll
-        for (int c = 0; c < LCH; ++c) {
-            if ((c + 1) * G * 8 <= L) top.template insert<true>(z[c], 8 * c, 8);
-            else if (c * G * 8 < L) top.template insert<false>(z[c], 8 * c, L - (c * G + p.g) * 8);
+        for (int c = 0; c < NC; ++c) {
+            __builtin_amdgcn_sched_barrier(0);
+            top.template insert<FULL, VEC>(z[c], 8 * c, L - (c * G + p.g) * 8);
         }
+        asm volatile("" : "+s"(L));          // (its comparisons are made again below: 72 masks are too many to keep)
         if (G > 1) {
 #pragma unroll
             for (int t = 0; t < TC; ++t) {
@@ -324,20 +360,18 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
         const float m = top.logit(0);
         const float o = exp_origin<TZ>(m);
         float whole = 0.0f, s = 0.0f;
-        float e[STATS ? LCH * 8 : 1];
+        float e[STATS ? NC * 8 : 1];
         if (STATS || r.kind == SR_ROUTE_SOFTMAX) {
 #pragma unroll
-            for (int c = 0; c < LCH; ++c) {
-                const bool all = (c + 1) * G * 8 <= L;
-                const int n = L - (c * G + p.g) * 8;
-                if (c * G * 8 < L)
+            for (int c = 0; c < NC; ++c) {
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float x = exp_from<TZ>(z[c].get(j), o);
-                        if (!all && j >= n) x = 0.0f;
-                        s += x;
-                        if (STATS) e[STATS ? c * 8 + j : 0] = x;
-                    }
+                for (int j = 0; j < 8; ++j) {
+                    float x = exp_from<TZ>(z[c].get(j), o);
+                    if (!FULL) x = j < L - (c * G + p.g) * 8 ? x : 0.0f;
+                    s += x;
+                    if (STATS) e[STATS ? c * 8 + j : 0] = x;
+                }
             }
             s = lanes_sum<G>(s, step);
             whole = s;
@@ -363,8 +397,7 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
         if (STATS && m != -INFINITY) {
             const float is = 1.0f / s, lse = m + logit_log(s);
 #pragma unroll
-            for (int c = 0; c < LCH; ++c)
-                if (c * G * 8 < L)
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) share[STATS ? c * 8 + j : 0] = fmaf(e[STATS ? c * 8 + j : 0], is, share[STATS ? c * 8 + j : 0]);
             if (p.g == 0) {
@@ -382,15 +415,14 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
     sq = pixels_sum<1>(sq, pm);
     live = pixels_sum<1>(live, pm);
 #pragma unroll
-    for (int c = 0; c < LCH; ++c)
-        if (c * G * 8 < r.L)
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int j = 0; j < 8; ++j) share[STATS ? c * 8 + j : 0] = pixels_sum<G>(share[STATS ? c * 8 + j : 0], pm);
     for (int w = 0; w < LWAVES; ++w) {
         if (wave == w) {
             if (first)
 #pragma unroll
-                for (int c = 0; c < LCH; ++c)
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int l = (c * G + g) * 8 + j;
@@ -413,81 +445,118 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
     if (threadIdx.x == 0) *rec.squares = sh_sq, *rec.live = sh_live;
 }
 
-// The gradient.  A pixel's entries are scattered into a row of LDS per lane ([atom], 16-byte pieces without bank conflicts:
-// the pitch of 76 words puts 16 lanes' pieces on 64 banks) and read back beside its logits.
-constexpr int DNT = 128, DWAVES = DNT / 64, DPITCH = LCH * 8 + 4;
-constexpr unsigned NOT_LISTED = 0x7fc5a5a5u;                 // a NaN that no computation gives
+// The gradient.  Which entry names an atom is a byte per atom in LDS, a row for every lane (all zero between tiles; the pitch of 19
+// words is free of bank conflicts); the entries' gradients are a table beside it, entry 0 the zero of atoms that are not listed.
+// 7 KB a wavefront and 110 registers: four wavefronts per SIMD hide the latency of a tile's loads (with the gradients themselves
+// scattered, 20 KB, it was two, and 1247 us instead of MEASURED for a 4K frame of 72 fp16 logits).
+constexpr int DNT = 256, DWAVES = DNT / 64;
 
-template <typename TZ, int G, int KIND, bool LOSS>
-__global__ __launch_bounds__(DNT, 2) void k_route_grad_lanes(const LaneArgs a) {
+template <typename TZ, int G, bool VEC, int NC, bool FULL, int TT, int KIND, bool LOSS>
+__global__ __launch_bounds__(DNT, 4) void k_route_grad_lanes(const LaneArgs a) {
     const RouteArgs& r = a.r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int step = r.layout == SR_COEFF_PIXEL_MAJOR ? 1 : 64 / G;
-    __shared__ float4 gl[DWAVES][64][DPITCH / 4];
-    __shared__ float4 fl[LOSS ? (LCH * 8 * G) / 4 : 1];
-    const float none = KIND == SR_ROUTE_CHOSEN ? __uint_as_float(NOT_LISTED) : 0.0f;
-    float* own = (float*)gl[wave][lane];
+    __shared__ unsigned map[DWAVES][64 * (NC * 8 + 4) / 4];
+    __shared__ float table[DWAVES][(TT + 1) * 64];
+    __shared__ float4 fl[LOSS ? (NC * 8 * G) / 4 : 1];
+    unsigned* const row = map[wave] + lane * ((NC * 8 + 4) / 4);
+    float* const tab = table[wave];
 #pragma unroll
-    for (int q = 0; q < LCH * 2; ++q) gl[wave][lane][q] = make_float4(none, none, none, none);
+    for (int q = 0; q < NC * 2; ++q) row[q] = 0;
+    tab[lane] = 0.0f;
     float w0 = 0.0f, w1 = 0.0f;
     if (LOSS) {
         const double M = (double)r.counts[r.L], inv = M > 0.0 ? 1.0 / M : 0.0;
         w0 = (float)(r.dloss[0] * (double)r.L * inv);
         w1 = (float)(r.dloss[1] * 2.0 * inv);
-        for (int l = threadIdx.x; l < LCH * 8 * G; l += DNT) ((float*)fl)[l] = l < r.L ? (float)((double)r.counts[l] * inv / r.T) : 0.0f;
+        for (int l = threadIdx.x; l < NC * 8 * G; l += DNT) ((float*)fl)[l] = l < r.L ? (float)((double)r.counts[l] * inv / r.T) : 0.0f;
         __syncthreads();
     }
+    // the table's address of the entry that names place j (0 .. 3) of a word of the row
+    const unsigned lane4 = 4u * (unsigned)lane;
+    auto entry = [&](unsigned word, int j) -> unsigned { return __builtin_amdgcn_perm(word, lane4, 0x0c0c0000u | (unsigned)(4 + j) << 8); };
     for (int64_t tile = (int64_t)blockIdx.x * DWAVES + wave; tile < a.tiles; tile += (int64_t)gridDim.x * DWAVES) {
         const LanePixel p = lane_pixel<TZ, G>(a, tile, lane);
         if (!p.inside) continue;
-        const bool on = !r.mask || r.mask[p.mask] != 0;
         int L = r.L;
         int64_t px = r.px, stride = r.lstride * (int64_t)sizeof(TZ);
         asm volatile("" : "+s"(L), "+s"(px), "+s"(stride));
-        float e[LCH * 8], m = -INFINITY, s = 0.0f, scale = 0.0f, tilt = 0.0f, pull = 0.0f;
-        if (on && KIND != SR_ROUTE_VALUES) {
-            Chunk<TZ> z[LCH];
-            load_chunks<TZ, G>(z, a, p, L);
+        gptr to = scalar((gptr)r.dz + (p.at - (const char*)r.z));
+        // writes a chunk of the lane: n atoms of it are there
+        auto write = [&](gptr q, int n, const float (&d)[8]) {
+            const unsigned off = lane_offset(p.off);
+            if (VEC) {
+                if (FULL || n > 0) {
+                    TZ st[8];
 #pragma unroll
-            for (int c = 0; c < LCH; ++c)
-                if (c * G * 8 < L)
+                    for (int j = 0; j < 8; ++j) st_from_float(st, j, d[j]);
+#pragma unroll
+                    for (int k = 0; k < (int)sizeof(TZ) / 2; ++k) {
+                        vec4u u;
+                        __builtin_memcpy(&u, (const char*)st + 16 * k, 16);
+                        gstore(q, off + 16 * k, u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j, q = scalar(q + stride))
+                    if (FULL || j < n) gstore(q, off, as_stored<TZ>(d[j]));
+            }
+        };
+        if (r.mask && r.mask[p.mask] == 0) {
+            const float zero[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+            for (int c = 0; c * G * 8 < L; ++c, to = scalar(to + stride * (8 * G))) write(to, L - (c * G + p.g) * 8, zero);
+            continue;
+        }
+        int at[TT];                          // the place in the lane's row of an entry, or -1
+        if (r.value) {
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+                if (t < r.T) {
+                    const int l = r.index[p.out + t * px];
+                    tab[64 * (t + 1) + lane] = a.half_value ? ld_as_float((const __half*)r.value, p.out + t * px) : ld_as_float((const float*)r.value, p.out + t * px);
+                    const int c = (l >> 3) / G;
+                    at[t] = l < L && (G == 1 || (l >> 3) % G == p.g) ? c * 8 + (l & 7) : -1;
+                    if (at[t] >= 0) ((unsigned char*)row)[at[t]] = (unsigned char)(t + 1);
+                }
+        }
+        float e[NC * 8], scale = 0.0f, tilt = 0.0f, pull = 0.0f, mine = 0.0f;
+        if (KIND != SR_ROUTE_VALUES) {
+            float m = -INFINITY;
+            {
+                Chunk<TZ, VEC> z[NC];
+                load_chunks<TZ, G, VEC, NC, FULL>(z, a, p, L);
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         float x = z[c].get(j);
-                        if ((c + 1) * G * 8 > L && j >= L - (c * G + p.g) * 8) x = -INFINITY;
+                        if (!FULL) x = j < L - (c * G + p.g) * 8 ? x : -INFINITY;
                         e[c * 8 + j] = x;
                         m = fmaxf(m, x);
                     }
-        }
-        // every lane of the pixel takes the entries of its own atoms
-        if (on && r.value)
-            for (int t = 0; t < r.T; ++t) {
-                const int l = r.index[p.out + t * px];
-                const float v = a.half_value ? ld_as_float((const __half*)r.value, p.out + t * px) : ld_as_float((const float*)r.value, p.out + t * px);
-                const int c = (l >> 3) / G;
-                if (l < L && (G == 1 || (l >> 3) % G == p.g)) own[c * 8 + (l & 7)] = v;
             }
-        float mine = 0.0f, sum_q = 0.0f, qg = 0.0f, fp = 0.0f;
-        if (on && KIND != SR_ROUTE_VALUES) {
             m = lanes_max<G>(m, step);
             const float o = exp_origin<TZ>(m);
+            float s = 0.0f, sum_q = 0.0f, qg = 0.0f, fp = 0.0f;
 #pragma unroll
-            for (int c = 0; c < LCH; ++c)
-                if (c * G * 8 < L)
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float4 G4 = gl[wave][lane][c * 2 + h];
+                        __builtin_amdgcn_sched_barrier(0);
+                        const unsigned word = row[c * 2 + h];
                         float4 f4 = make_float4(0, 0, 0, 0);
                         if (LOSS) f4 = fl[(c * G + p.g) * 2 + h];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const float x = exp_from<TZ>(e[c * 8 + 4 * h + j], o), gv = ((const float*)&G4)[j];
+                            const unsigned en = entry(word, j);
+                            const float x = exp_from<TZ>(e[c * 8 + 4 * h + j], o), gv = *(const float*)((const char*)tab + en);
                             e[c * 8 + 4 * h + j] = x;
                             s += x;
                             if (KIND == SR_ROUTE_CHOSEN) {
-                                const bool is = __float_as_uint(gv) != NOT_LISTED;
-                                sum_q += is ? x : 0.0f;
-                                qg = is ? fmaf(x, gv, qg) : qg;
+                                sum_q += en >= 256u ? x : 0.0f;
+                                qg = en >= 256u ? fmaf(x, gv, qg) : qg;
                             } else {
                                 qg = fmaf(x, gv, qg);
                             }
@@ -508,59 +577,39 @@ __global__ __launch_bounds__(DNT, 2) void k_route_grad_lanes(const LaneArgs a) {
                 tilt = fmaf(w1, lse, -w0 * (fp * is));
             }
         }
-        char* to = (char*)r.dz + (p.at - (const char*)r.z);
+        int again = 0;                       // (hidden: the rows are read again; kept, what they said would take another 144 registers)
+        asm volatile("" : "+v"(again));
 #pragma unroll
-        for (int c = 0; c < LCH; ++c, to += stride * (8 * G))
-            if (c * G * 8 < L) {
-                const int n = L - (c * G + p.g) * 8;
+        for (int c = 0; c < NC; ++c, to = scalar(to + stride * (8 * G)))
+            if (FULL || c * G * 8 < L) {
+                __builtin_amdgcn_sched_barrier(0);
                 float d[8];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float4 G4 = gl[wave][lane][c * 2 + h];
+                    const unsigned word = row[c * 2 + h + again];
                     float4 f4 = make_float4(0, 0, 0, 0);
-                    if (LOSS) f4 = fl[(c * G + p.g) * 2 + h];
+                    if (LOSS) f4 = fl[(c * G + p.g) * 2 + h + again];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float x = e[c * 8 + 4 * h + j], gv = ((const float*)&G4)[j];
-                        float y;
-                        if (KIND == SR_ROUTE_VALUES) {
-                            y = gv;
-                        } else {
+                        const unsigned en = entry(word, j);
+                        const float gv = *(const float*)((const char*)(tab + again) + en);
+                        float y = gv;
+                        if (KIND != SR_ROUTE_VALUES) {
+                            const float x = e[c * 8 + 4 * h + j];
                             y = x * scale * (gv - pull);
-                            if (KIND == SR_ROUTE_CHOSEN) y = __float_as_uint(gv) != NOT_LISTED ? y : 0.0f;
+                            if (KIND == SR_ROUTE_CHOSEN) y = en >= 256u ? y : 0.0f;
                             if (LOSS) y = fmaf(x * mine, fmaf(w0, ((const float*)&f4)[j], tilt), y);
                         }
-                        d[4 * h + j] = on ? y : 0.0f;
+                        d[4 * h + j] = y;
                     }
                 }
-                if (a.vec) {
-                    if (n > 0) {
-                        TZ st[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) st_from_float(st, j, d[j]);
-#pragma unroll
-                        for (int q = 0; q < (int)sizeof(TZ) / 2; ++q) {
-                            uint4 u;
-                            __builtin_memcpy(&u, (const char*)st + 16 * q, 16);
-                            *(uint4*)(to + p.off + 16 * q) = u;
-                        }
-                    }
-                } else if ((c + 1) * G * 8 <= L) {
-                    char* q = to;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j, q += stride) st_from_float((TZ*)(q + p.off), 0, d[j]);
-                } else {
-                    char* q = to;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j, q += stride)
-                        if (j < n) st_from_float((TZ*)(q + p.off), 0, d[j]);
-                }
+                write(to, L - (c * G + p.g) * 8, d);
             }
-        if (on && r.value)
-            for (int t = 0; t < r.T; ++t) {
-                const int l = r.index[p.out + t * px], c = (l >> 3) / G;
-                if (l < L && (G == 1 || (l >> 3) % G == p.g)) own[c * 8 + (l & 7)] = none;
-            }
+        if (r.value) {
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+                if (t < r.T && at[t] >= 0) ((unsigned char*)row)[at[t]] = 0;
+        }
     }
 }
 
@@ -568,29 +617,51 @@ __global__ __launch_bounds__(DNT, 2) void k_route_grad_lanes(const LaneArgs a) {
 template <typename TZ> hipError_t route_lanes(const LaneArgs& a, int G, bool stats, int grid, hipStream_t st);
 template <typename TZ> hipError_t route_grad_lanes(const LaneArgs& a, int G, int grid, hipStream_t st);
 
+// Which instantiation: lanes of a pixel, rows of logits or planes, chunks of a lane.
+#define SR_ROUTE_FORMS(F)                                                                                                          \
+    if (a.vec) return a.r.L <= 64 ? F(4, true, 2, false) : a.r.L <= 128 ? F(4, true, 4, false) : F(4, true, LCH, false);            \
+    if (G > 1) return F(4, false, LCH, false);                                                                                     \
+    return a.r.L == 8 * LCH ? F(1, false, LCH, true) : a.r.L <= 24 ? F(1, false, 3, false) : F(1, false, LCH, false);
+
 #define SR_ROUTE_LANES(TZ)                                                                                                         \
-    template <int TC, int G> static hipError_t route_tc(const LaneArgs& a, bool stats, int grid, hipStream_t st) {                 \
-        if (stats) k_route_lanes<TZ, TC, G, true><<<grid, LNT, 0, st>>>(a);                                                        \
-        else k_route_lanes<TZ, TC, G, false><<<grid, LNT, 0, st>>>(a);                                                             \
+    template <int G, bool VEC, int NC, bool FULL> static hipError_t route_one(const LaneArgs& a, bool stats, int grid, hipStream_t st) { \
+        if (a.r.T <= 4) {                                                                                                          \
+            if (stats) k_route_lanes<TZ, 4, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                      \
+            else k_route_lanes<TZ, 4, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                           \
+        } else if (a.r.T <= 8) {                                                                                                   \
+            if (stats) k_route_lanes<TZ, 8, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                      \
+            else k_route_lanes<TZ, 8, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                           \
+        } else {                                                                                                                   \
+            if (stats) k_route_lanes<TZ, 16, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                     \
+            else k_route_lanes<TZ, 16, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                          \
+        }                                                                                                                          \
         return hipGetLastError();                                                                                                  \
     }                                                                                                                              \
-    template <int G> static hipError_t route_g(const LaneArgs& a, bool stats, int grid, hipStream_t st) {                          \
-        return a.r.T <= 4 ? route_tc<4, G>(a, stats, grid, st) : a.r.T <= 8 ? route_tc<8, G>(a, stats, grid, st) : route_tc<16, G>(a, stats, grid, st); \
+    template <int G, bool VEC, int NC, bool FULL, int KIND> static hipError_t grad_kind(const LaneArgs& a, int grid, hipStream_t st) { \
+        constexpr bool loss = KIND != SR_ROUTE_VALUES;                                                                             \
+        if (a.r.T <= 8) {                                                                                                          \
+            if (a.r.counts) k_route_grad_lanes<TZ, G, VEC, NC, FULL, 8, KIND, loss><<<grid, DNT, 0, st>>>(a);                      \
+            else k_route_grad_lanes<TZ, G, VEC, NC, FULL, 8, KIND, false><<<grid, DNT, 0, st>>>(a);                                \
+        } else {                                                                                                                   \
+            if (a.r.counts) k_route_grad_lanes<TZ, G, VEC, NC, FULL, 16, KIND, loss><<<grid, DNT, 0, st>>>(a);                     \
+            else k_route_grad_lanes<TZ, G, VEC, NC, FULL, 16, KIND, false><<<grid, DNT, 0, st>>>(a);                               \
+        }                                                                                                                          \
+        return hipGetLastError();                                                                                                  \
+    }                                                                                                                              \
+    template <int G, bool VEC, int NC, bool FULL> static hipError_t grad_one(const LaneArgs& a, int grid, hipStream_t st) {        \
+        return a.r.kind == SR_ROUTE_SOFTMAX ? grad_kind<G, VEC, NC, FULL, SR_ROUTE_SOFTMAX>(a, grid, st)                           \
+             : a.r.kind == SR_ROUTE_CHOSEN ? grad_kind<G, VEC, NC, FULL, SR_ROUTE_CHOSEN>(a, grid, st)                             \
+                                           : grad_kind<G, VEC, NC, FULL, SR_ROUTE_VALUES>(a, grid, st);                            \
     }                                                                                                                              \
     template <> hipError_t route_lanes<TZ>(const LaneArgs& a, int G, bool stats, int grid, hipStream_t st) {                       \
-        return G == 1 ? route_g<1>(a, stats, grid, st) : G == 2 ? route_g<2>(a, stats, grid, st) : route_g<4>(a, stats, grid, st); \
-    }                                                                                                                              \
-    template <int G, int KIND> static hipError_t grad_k(const LaneArgs& a, int grid, hipStream_t st) {                             \
-        if (a.r.counts) k_route_grad_lanes<TZ, G, KIND, KIND != SR_ROUTE_VALUES><<<grid, DNT, 0, st>>>(a);                         \
-        else k_route_grad_lanes<TZ, G, KIND, false><<<grid, DNT, 0, st>>>(a);                                                      \
-        return hipGetLastError();                                                                                                  \
-    }                                                                                                                              \
-    template <int G> static hipError_t grad_g(const LaneArgs& a, int grid, hipStream_t st) {                                       \
-        return a.r.kind == SR_ROUTE_SOFTMAX ? grad_k<G, SR_ROUTE_SOFTMAX>(a, grid, st)                                             \
-             : a.r.kind == SR_ROUTE_CHOSEN ? grad_k<G, SR_ROUTE_CHOSEN>(a, grid, st) : grad_k<G, SR_ROUTE_VALUES>(a, grid, st);    \
+        auto f = [&](auto g, auto v, auto n, auto w) { return route_one<g.value, v.value, n.value, w.value>(a, stats, grid, st); }; \
+        SR_ROUTE_FORMS(SR_ROUTE_FORM)                                                                                              \
     }                                                                                                                              \
     template <> hipError_t route_grad_lanes<TZ>(const LaneArgs& a, int G, int grid, hipStream_t st) {                              \
-        return G == 1 ? grad_g<1>(a, grid, st) : G == 2 ? grad_g<2>(a, grid, st) : grad_g<4>(a, grid, st);                         \
+        auto f = [&](auto g, auto v, auto n, auto w) { return grad_one<g.value, v.value, n.value, w.value>(a, grid, st); };        \
+        SR_ROUTE_FORMS(SR_ROUTE_FORM)                                                                                              \
     }
+#define SR_ROUTE_FORM(g, v, n, w) \
+    f(std::integral_constant<int, g>{}, std::bool_constant<v>{}, std::integral_constant<int, n>{}, std::bool_constant<w>{})
 
 }  // namespace srd
