@@ -145,11 +145,22 @@ __global__ __launch_bounds__(FNT) void k_route_finish(const void* partial, int r
     const int tid = threadIdx.x, groups = FNT / L, g = tid / L, l = tid - g * L;
     double s = 0.0;
     unsigned long long c = 0;
+    // eight records' loads under way at a time: one after the other their latencies are what the kernel takes (15 us of 512 records)
+    constexpr int AHEAD = 8;
     if (g < groups)
-        for (int r = g; r < records; r += groups) {
-            const RouteRecord rec((void*)partial, L, r);
-            s += rec.share[l];
-            c += rec.counts[l];
+        for (int r0 = g; r0 < records; r0 += AHEAD * groups) {
+            double v[AHEAD];
+            unsigned long long n[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int r = r0 + i * groups;
+                const RouteRecord rec((void*)partial, L, r < records ? r : r0);
+                v[i] = rec.share[l];
+                n[i] = rec.counts[l];
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (r0 + i * groups < records) s += v[i], c += n[i];
         }
     sh_s[tid] = s;
     sh_c[tid] = c;
@@ -404,7 +415,7 @@ int sr_list_route(const sr_tensor* coeff, int L, int scale, int entries, int kin
     if (any_overlap(out, in)) return SR_ERR_ALIAS;
     LaneArgs m;
     const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
-    const hipError_t e = G ? launch_lanes(m, coeff->dtype, G, false, grid_for(m.tiles, LWAVES, 1 << 20), (hipStream_t)stream)
+    const hipError_t e = G ? launch_lanes(m, coeff->dtype, G, false, grid_for(m.tiles, lanes_threads(false) / 64, 1 << 20), (hipStream_t)stream)
                            : launch_route<false>(a, coeff->dtype, value->dtype, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }
@@ -436,7 +447,7 @@ int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries,
         a.partial = workspace;
         LaneArgs m;
         const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
-        a.records = G ? grid_for(m.tiles, LWAVES, ROUTE_RECORDS / 2) : blocks_for(a.total, ROUTE_RECORDS);
+        a.records = G ? grid_for(m.tiles, lanes_threads(true) / 64, compute_units() < ROUTE_RECORDS ? compute_units() : ROUTE_RECORDS) : blocks_for(a.total, ROUTE_RECORDS);
         e = G ? launch_lanes(m, coeff->dtype, G, true, a.records, (hipStream_t)stream)
               : launch_route<true>(a, coeff->dtype, value->dtype, a.records, (hipStream_t)stream);
     }

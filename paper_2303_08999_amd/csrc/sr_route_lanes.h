@@ -283,14 +283,19 @@ __device__ __forceinline__ void load_chunks(Chunk<TZ, VEC> (&z)[NC], const LaneA
     }
 }
 
-// Sum over the lanes of a wavefront that hold the same chunk (g), in every lane.
-template <int G, typename T> __device__ __forceinline__ T pixels_sum(T v, bool pm) {
-    if (G == 1 || !pm) {
-#pragma unroll
-        for (int d = 64 / G / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    } else {
-#pragma unroll
-        for (int d = 32; d >= G; d >>= 1) v += __shfl_xor(v, d);
+// Sum over the lanes of a wavefront that hold the same atoms, without LDS: turns within rows of 16 lanes, then rows exchanged.
+template <int CTRL> __device__ __forceinline__ float row_turned(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+template <int G> __device__ __forceinline__ float pixels_sum(float v, bool pm) {
+    if (G == 1 || !pm) v += row_turned<0x121>(v), v += row_turned<0x122>(v);     // row_ror 1, 2
+    v += row_turned<0x124>(v);
+    v += row_turned<0x128>(v);
+    if (G == 1 || pm) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+        const auto c = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(c[0]) + __uint_as_float(c[1]);
     }
     return v;
 }
@@ -305,10 +310,12 @@ template <int G> __device__ __forceinline__ float lanes_max(float v, int step) {
     return v;
 }
 
-constexpr int LNT = 256, LWAVES = LNT / 64;
+// Workgroups: with the losses one a CU, so that few records are left to be added up (512 of them took 13 us).
+constexpr int lanes_threads(bool stats) { return stats ? 512 : 256; }
 
 template <typename TZ, int TC, int G, bool VEC, int NC, bool FULL, bool STATS>
-__global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneArgs a) {
+__global__ __launch_bounds__(lanes_threads(STATS), STATS ? 2 : 4) void k_route_lanes(const LaneArgs a) {
+    constexpr int LNT = lanes_threads(STATS), LWAVES = LNT / 64;
     const RouteArgs& r = a.r;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR;
@@ -407,42 +414,38 @@ __global__ __launch_bounds__(LNT, STATS ? 2 : 4) void k_route_lanes(const LaneAr
         }
     }
     if (!STATS) return;
-    // over the wavefront's lanes in fp32, over the wavefronts in double, one after the other
-    __shared__ double sum[STATS ? SR_MAX_ATOMS + 32 : 1], sh_sq;
-    __shared__ unsigned sh_live;
+    // over the wavefront's lanes in fp32, over the wavefronts in double
+    __shared__ float part[STATS ? LWAVES : 1][STATS ? G * NC * 8 : 1];
+    __shared__ double part_sq[LWAVES];
+    __shared__ unsigned part_live[LWAVES];
     const int g = G == 1 ? 0 : (pm ? lane % G : lane / (64 / G));
     const bool first = pm ? lane < G : lane % (64 / G) == 0;
-    sq = pixels_sum<1>(sq, pm);
-    live = pixels_sum<1>(live, pm);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sq += __shfl_xor(sq, d), live += __shfl_xor(live, d);
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) share[STATS ? c * 8 + j : 0] = pixels_sum<G>(share[STATS ? c * 8 + j : 0], pm);
-    for (int w = 0; w < LWAVES; ++w) {
-        if (wave == w) {
-            if (first)
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int l = (c * G + g) * 8 + j;
-                        if (l < r.L) sum[l] = (w ? sum[l] : 0.0) + share[STATS ? c * 8 + j : 0];
-                    }
-            if (lane == 0) {
-                sh_sq = (w ? sh_sq : 0.0) + sq;
-                sh_live = (w ? sh_live : 0u) + live;
-            }
+        for (int j = 0; j < 8; ++j) {
+            const float v = pixels_sum<G>(share[STATS ? c * 8 + j : 0], pm);
+            if (first) part[STATS ? wave : 0][STATS ? (c * G + g) * 8 + j : 0] = v;
         }
-        __syncthreads();
-    }
+    if (lane == 0) part_sq[wave] = sq, part_live[wave] = live;
+    __syncthreads();
     const RouteRecord rec(r.partial, r.L, blockIdx.x);
     for (int l = threadIdx.x; l < r.L; l += LNT) {
-        rec.share[l] = sum[l];
+        double v = 0.0;
         unsigned n = 0;
-        for (int w = 0; w < LWAVES; ++w) n += bins[w * SR_MAX_ATOMS + l];
+        for (int w = 0; w < LWAVES; ++w) v += (double)part[STATS ? w : 0][STATS ? l : 0], n += bins[w * SR_MAX_ATOMS + l];
+        rec.share[l] = v;
         rec.counts[l] = n;
     }
-    if (threadIdx.x == 0) *rec.squares = sh_sq, *rec.live = sh_live;
+    if (threadIdx.x == 0) {
+        double v = 0.0;
+        unsigned long long n = 0;
+        for (int w = 0; w < LWAVES; ++w) v += part_sq[w], n += part_live[w];
+        *rec.squares = v;
+        *rec.live = n;
+    }
 }
 
 // The gradient.  Which entry names an atom is a byte per atom in LDS, a row for every lane (all zero between tiles; the pitch of 19
@@ -626,14 +629,14 @@ template <typename TZ> hipError_t route_grad_lanes(const LaneArgs& a, int G, int
 #define SR_ROUTE_LANES(TZ)                                                                                                         \
     template <int G, bool VEC, int NC, bool FULL> static hipError_t route_one(const LaneArgs& a, bool stats, int grid, hipStream_t st) { \
         if (a.r.T <= 4) {                                                                                                          \
-            if (stats) k_route_lanes<TZ, 4, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                      \
-            else k_route_lanes<TZ, 4, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                           \
+            if (stats) k_route_lanes<TZ, 4, G, VEC, NC, FULL, true><<<grid, lanes_threads(true), 0, st>>>(a);                   \
+            else k_route_lanes<TZ, 4, G, VEC, NC, FULL, false><<<grid, lanes_threads(false), 0, st>>>(a);                       \
         } else if (a.r.T <= 8) {                                                                                                   \
-            if (stats) k_route_lanes<TZ, 8, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                      \
-            else k_route_lanes<TZ, 8, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                           \
+            if (stats) k_route_lanes<TZ, 8, G, VEC, NC, FULL, true><<<grid, lanes_threads(true), 0, st>>>(a);                   \
+            else k_route_lanes<TZ, 8, G, VEC, NC, FULL, false><<<grid, lanes_threads(false), 0, st>>>(a);                       \
         } else {                                                                                                                   \
-            if (stats) k_route_lanes<TZ, 16, G, VEC, NC, FULL, true><<<grid, LNT, 0, st>>>(a);                                     \
-            else k_route_lanes<TZ, 16, G, VEC, NC, FULL, false><<<grid, LNT, 0, st>>>(a);                                          \
+            if (stats) k_route_lanes<TZ, 16, G, VEC, NC, FULL, true><<<grid, lanes_threads(true), 0, st>>>(a);                  \
+            else k_route_lanes<TZ, 16, G, VEC, NC, FULL, false><<<grid, lanes_threads(false), 0, st>>>(a);                      \
         }                                                                                                                          \
         return hipGetLastError();                                                                                                  \
     }                                                                                                                              \
