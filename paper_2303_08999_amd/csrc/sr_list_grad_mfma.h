@@ -95,19 +95,27 @@ __device__ __forceinline__ void split_pair(float x, float y, float sc, unsigned&
     __builtin_memcpy(&lo, &l, 4);
 }
 
+// A stored value's bits, and the value
+template <typename T> struct Bits { typedef unsigned short type; };
+template <> struct Bits<float> { typedef unsigned type; };
+__device__ __forceinline__ float from_bits(unsigned b, const __half*) { return __half2float(__ushort_as_half((unsigned short)b)); }
+__device__ __forceinline__ float from_bits(unsigned b, const float*) { return __uint_as_float(b); }
+
 // What a unit needs of memory, as it is stored, requested one unit ahead.
 template <int CM, int TQ> struct GradFetch {
     unsigned dy[2][CM], idx[2][TQ], val[2][TQ], on[2];
 };
 
-template <int K, int LP, int CM, int TQ, typename TV>
+template <int K, int LP, int CM, int TQ, typename TV, typename TIO>
 __global__ __launch_bounds__(256, (GradCfg<K, LP, CM, TQ, TV>::WPE))
 void k_list_grad_mfma(const ListGradArgs a) {
     using F = GradCfg<K, LP, CM, TQ, TV>;
     constexpr int KK = F::KK, R = F::R, NS = F::NS, NI = F::NI, NT = F::NT, MT = F::MT, UW = F::UW, UH = F::UH, UP = F::UP;
     constexpr int MAXLRX = F::MAXLRX, MAXLRY = F::MAXLRY;
     constexpr int UNITS = GM_TH * 2 / 4;             // of a wavefront in a tile
-    constexpr unsigned VB = sizeof(TV);
+    constexpr unsigned VB = sizeof(TV), IB = sizeof(TIO);
+    typedef typename Bits<TIO>::type io_bits;
+    typedef typename Bits<TV>::type value_bits;
     __shared__ float U[F::UN];                       // up-sampled tile; before that, in its place, the LR footprint
     __shared__ float4 yw[UH];                        // a tile's rows: weights, first LR row
     __shared__ int yb[UH];
@@ -182,7 +190,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
     };
     // Requests a unit: lane (q, n) has of pixel n of either group the entries 4 r + q.  Every address is one of the tensors'; what is outside of
     // the image or the list is set aside when it is used.  An image's lists and its dout lie within 32-bit offsets.
-    const unsigned pl = (unsigned)plane, half_io = a.io_f16 ? ~0u : 0u;
+    // (No branch in here, and every load widened where it is made: a value that is first touched in another block is waited for there.)
+    const unsigned pl = (unsigned)plane, unmasked = a.mask ? 0u : 1u;
     unsigned entry[TQ];
 #pragma unroll
     for (int r = 0; r < TQ; ++r) entry[r] = (unsigned)min(4 * r + q, a.T - 1) * pl;
@@ -191,23 +200,19 @@ void k_list_grad_mfma(const ListGradArgs a) {
         const unsigned at = (unsigned)Y * (unsigned)a.W + (unsigned)X;     // the same for the whole wavefront
         const unsigned char* const index = a.index + t.list;
         const char* const value = (const char*)a.value + t.list * VB;
-        const char* const dout = (const char*)a.dout + t.image * (a.io_f16 ? 2 : 4);
+        const char* const dout = (const char*)a.dout + t.image * IB;
+        const unsigned char* const mask = a.mask ? a.mask + t.im * plane : index;      // without one: some byte, made 1 below
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const unsigned x = at + (unsigned)min(16 * g + n, a.W - 1 - X);
-            f.on[g] = a.mask ? (unsigned)(a.mask + (int64_t)t.im * plane)[x] : 1u;
-            if (a.io_f16) {
+            f.on[g] = mask[x];
 #pragma unroll
-                for (int c = 0; c < CM; ++c) f.dy[g][c] = *(const unsigned short*)(dout + (unsigned)c * (pl * 2) + x * 2);
-            } else {
-#pragma unroll
-                for (int c = 0; c < CM; ++c) f.dy[g][c] = *(const unsigned*)(dout + (unsigned)c * (pl * 4) + x * 4);
-            }
+            for (int c = 0; c < CM; ++c) f.dy[g][c] = *(const io_bits*)(dout + (unsigned)c * (pl * IB) + x * IB);
 #pragma unroll
             for (int r = 0; r < TQ; ++r) {
                 const unsigned e = entry[r] + x;
                 f.idx[g][r] = index[e];
-                f.val[g][r] = VB == 2 ? (unsigned)*(const unsigned short*)(value + e * 2) : *(const unsigned*)(value + e * 4);
+                f.val[g][r] = *(const value_bits*)(value + e * VB);
             }
         }
     };
@@ -222,18 +227,11 @@ void k_list_grad_mfma(const ListGradArgs a) {
         unsigned row[LRI];
 #pragma unroll
         for (int i = 0; i < LRI; ++i) row[i] = (unsigned)clampi(o.ly0 + min(wave + 4 * i, MAXLRY - 1), 0, a.h - 1) * (unsigned)a.w;
-        const char* const lr = (const char*)a.lr + (int64_t)t.im * CM * lp * (a.io_f16 ? 2 : 4);
-        if (a.io_f16) {
+        const char* const lr = (const char*)a.lr + (int64_t)t.im * CM * lp * IB;
 #pragma unroll
-            for (int c = 0; c < CM; ++c)
+        for (int c = 0; c < CM; ++c)
 #pragma unroll
-                for (int i = 0; i < LRI; ++i) lrv[c][i] = *(const unsigned short*)(lr + ((unsigned)c * lp + row[i]) * 2 + x * 2);
-        } else {
-#pragma unroll
-            for (int c = 0; c < CM; ++c)
-#pragma unroll
-                for (int i = 0; i < LRI; ++i) lrv[c][i] = *(const unsigned*)(lr + ((unsigned)c * lp + row[i]) * 4 + x * 4);
-        }
+            for (int i = 0; i < LRI; ++i) lrv[c][i] = *(const io_bits*)(lr + ((unsigned)c * lp + row[i]) * IB + x * IB);
     };
 
     const unsigned tiles = (unsigned)a.tiles;
@@ -262,8 +260,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
         for (int c = 0; c < CM; ++c)
 #pragma unroll
             for (int i = 0; i < LRI; ++i) {
-                const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)lrv[c][i])));
-                U[(c * MAXLRY + min(wave + 4 * i, MAXLRY - 1)) * MAXLRX + lane_x] = __uint_as_float((h & half_io) | (lrv[c][i] & ~half_io));
+                U[(c * MAXLRY + min(wave + 4 * i, MAXLRY - 1)) * MAXLRX + lane_x] = from_bits(lrv[c][i], (const TIO*)nullptr);
             }
         __syncthreads();
 #pragma unroll
@@ -291,7 +288,6 @@ void k_list_grad_mfma(const ListGradArgs a) {
         }
         __syncthreads();
 
-        if (!last) fetch_lr(tn);
 
         // ---- a wavefront's units: 32 pixels of a row, two groups of 16
 #pragma unroll 1
@@ -299,6 +295,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
             const int Y = tl.Y0 + wave * (GM_TH / 4) + u / 2, x0 = u % 2 * 32;
             GradFetch<CM, TQ> f = next;
             if (u + 1 < UNITS || !last) fetch(next, u + 1 < UNITS ? tl : tn, (u + 1) % UNITS);
+            if (u == 1 && !last) fetch_lr(tn);       // (not before the first unit, which would wait for these rows as well)
             if (Y >= a.H || tl.X0 + x0 >= a.W) continue;
             const char* const Ub = (const char*)U + 4 * (u / 2 * UP + x0);
             // Entries go into the dense columns.  An atom that a pixel lists twice has one place there: every entry writes its number, those
@@ -309,7 +306,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 inside[g] = tl.X0 + x0 + 16 * g + n < a.W;
-                on[g] = inside[g] && f.on[g] != 0;
+                on[g] = inside[g] && (f.on[g] | unmasked) != 0;
 #pragma unroll
                 for (int r = 0; r < TQ; ++r) {
                     f.idx[g][r] = f.idx[g][r] < lmax ? f.idx[g][r] : lmax;
@@ -334,9 +331,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     float dy[CM];
 #pragma unroll
                     for (int c = 0; c < CM; ++c) {
-                        const unsigned h = __float_as_uint(__half2float(__ushort_as_half((unsigned short)f.dy[g][c])));
-                    const float v = __uint_as_float((h & half_io) | (f.dy[g][c] & ~half_io));      // (a select: no branch cuts the unit here)
-                        dy[c] = on[g] ? v : 0.0f;
+                        dy[c] = on[g] ? from_bits(f.dy[g][c], (const TIO*)nullptr) : 0.0f;
                     }
                     float E[NS][8], m = 0.0f;
 #pragma unroll
@@ -563,16 +558,20 @@ void k_list_grad_mfma(const ListGradArgs a) {
     }
 }
 
-template <int K, int LP, int CM, typename TV>
+template <int K, int LP, int CM, typename TV, typename TIO>
 static hipError_t grad_mfma_one(const ListGradArgs& a, int grid, hipStream_t st) {
-    if (a.T <= 8) k_list_grad_mfma<K, LP, CM, 2, TV><<<grid, 256, 0, st>>>(a);
-    else k_list_grad_mfma<K, LP, CM, 4, TV><<<grid, 256, 0, st>>>(a);
+    if (a.T <= 8) k_list_grad_mfma<K, LP, CM, 2, TV, TIO><<<grid, 256, 0, st>>>(a);
+    else k_list_grad_mfma<K, LP, CM, 4, TV, TIO><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
+}
+template <int K, typename TV, typename TIO>
+static hipError_t grad_mfma_io(const ListGradArgs& a, int grid, hipStream_t st) {
+    if (a.L <= 80) return a.C == 1 ? grad_mfma_one<K, 80, 1, TV, TIO>(a, grid, st) : grad_mfma_one<K, 80, 3, TV, TIO>(a, grid, st);
+    return a.C == 1 ? grad_mfma_one<K, 128, 1, TV, TIO>(a, grid, st) : grad_mfma_one<K, 128, 3, TV, TIO>(a, grid, st);
 }
 template <int K, typename TV>
 static hipError_t grad_mfma_k(const ListGradArgs& a, int grid, hipStream_t st) {
-    if (a.L <= 80) return a.C == 1 ? grad_mfma_one<K, 80, 1, TV>(a, grid, st) : grad_mfma_one<K, 80, 3, TV>(a, grid, st);
-    return a.C == 1 ? grad_mfma_one<K, 128, 1, TV>(a, grid, st) : grad_mfma_one<K, 128, 3, TV>(a, grid, st);
+    return a.io_f16 ? grad_mfma_io<K, TV, __half>(a, grid, st) : grad_mfma_io<K, TV, float>(a, grid, st);
 }
 
 }  // namespace srd
