@@ -5,7 +5,7 @@
 //     ddict      G[l][j] = sum_i Phi[l][i] E[j][i]     Phi the lists as dense columns
 // v_mfma_f32_16x16x32_f16 serves both: for R the sum runs over the taps, so lane (q, n) forms taps 8 q .. 8 q + 7 of pixel n of a
 // group of 16, which is the operand as it lies in its registers; for G it runs over the 32 pixels of a unit, so E goes through LDS
-// as [tap][pixel], the lists are scattered into a dense [atom][pixel] array that is all zero between uses, and R goes through LDS
+// and comes back turned, the lists are scattered into a dense [atom][pixel] array that is all zero between uses, and R goes through LDS
 // for its gather.  All of that is a wavefront's own scratch: no barrier but around the up-sampled tile.
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
@@ -28,6 +28,8 @@ typedef float __attribute__((may_alias)) lds_f;
 typedef u32x4v __attribute__((may_alias)) lds_u4;
 typedef unsigned __attribute__((may_alias)) lds_u;
 typedef unsigned short __attribute__((may_alias)) lds_h;
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short4v __attribute__((address_space(3), may_alias))* lds_turned;
 
 template <int K, int LP, int CM, int TQ, typename TV>
 struct GradCfg {
@@ -40,14 +42,14 @@ struct GradCfg {
     static constexpr int UN = CM * UH * UP, VN = CM * UH * MAXLRX;
     static constexpr bool SPLIT = sizeof(TV) == 4;                                     // values in two parts
     static constexpr int PP = 40;                  // pitch of Phi in halves: 16 rows' 16-byte pieces fall on all 64 banks
-    static constexpr int EP = 36;                  // pitch of [tap][pixel] in words, likewise
+    static constexpr int EP = 64 * NS + 16;        // pitch of a pixel's taps in bytes, likewise
     static constexpr int RP = LP + 4;              // pitch of a pixel's responses, likewise
     static constexpr int PHI_ROWS = LP + 1;        // the last one takes what is not to be added
     static constexpr int PHI_B = PHI_ROWS * PP * 2 * (SPLIT ? 2 : 1);
     static constexpr int R_B = 16 * RP * 4;        // responses of a group
     // Groups whose responses are formed together: two hide each other's latency, one takes fewer registers and less scratch.
     static constexpr int RG = (K == 7 && LP > 80) || (TQ == 4 && LP <= 80 && !SPLIT) ? 1 : 2;
-    static constexpr int ER_0 = 32 * NS * EP * 4 > RG * R_B ? 32 * NS * EP * 4 : RG * R_B;
+    static constexpr int ER_0 = 2 * 32 * EP > RG * R_B ? 2 * 32 * EP : RG * R_B;
     static constexpr int ER_B = ER_0 > VN * 4 ? ER_0 : (VN * 4 + 15) / 16 * 16;
     static constexpr int WAVE_B = PHI_B + ER_B;
     static constexpr bool DL = K == 7 && LP > 80 && !SPLIT;                            // D's operands in LDS, not in 128 registers
@@ -396,7 +398,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 }
             }
             if (rec) {
-                // the unit's scale, its values' scale; E to [tap][pixel] as words of (high, low)
+                // the unit's scale, its values' scale; E to [pixel][place], high parts, then low ones
                 int es = row_max(max(ex[0], ex[1]));
                 if (F::ACC) {
                     // G's own power of two: at most four times the unit's, or G changes to the double of it
@@ -437,31 +439,34 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     const _Float16 fs = (_Float16)pow2_field(127 + ex[g] - es);
                     const half2v ff = {fs, fs};
 #pragma unroll
-                    for (int s = 0; s < NS; ++s)
+                    for (int s = 0; s < NS; ++s) {
+                        u32x4v h, l;
 #pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            const unsigned w = __builtin_amdgcn_perm(El[g][s][i / 2], Eh[g][s][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
-                            *(lds_u*)(er + 4 * ((32 * s + 8 * q + i) * F::EP + 16 * g + n)) = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, w) * ff);
+                        for (int i = 0; i < 4; ++i) {
+                            h[i] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, (unsigned)Eh[g][s][i]) * ff);
+                            l[i] = __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, (unsigned)El[g][s][i]) * ff);
                         }
+                        unsigned char* const p = er + (16 * g + n) * F::EP + 64 * s + 16 * q;
+                        *(lds_u4*)p = h;
+                        *(lds_u4*)(p + 32 * F::EP) = l;
+                    }
 #pragma unroll
                     for (int r = 0; r < TQ; ++r)
                         if (!F::SPLIT) val[g][r] = f.val[g][r];
                 }
                 wave_lds_fence();
+                // ... and back turned: of the 16 places t, four pixels' rows at a time, lane n gets its place's column; lane (q, n) has pixels
+                // 8 q .. 8 q + 7 of place 16 t + n then
                 half8 eh[NT], el[NT];
+                unsigned char* const column = er + (8 * q + n / 4) * F::EP + 8 * (n % 4);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const lds_u4* p = (const lds_u4*)(er + 4 * ((16 * t + n) * F::EP + 8 * q));
-                    const u32x4v w0 = p[0], w1 = p[1];
-                    u32x4v h, l;
+                    short4v v[4];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        h[i] = __builtin_amdgcn_perm(w0[2 * i + 1], w0[2 * i], 0x05040100u);
-                        l[i] = __builtin_amdgcn_perm(w0[2 * i + 1], w0[2 * i], 0x07060302u);
-                        h[2 + i] = __builtin_amdgcn_perm(w1[2 * i + 1], w1[2 * i], 0x05040100u);
-                        l[2 + i] = __builtin_amdgcn_perm(w1[2 * i + 1], w1[2 * i], 0x07060302u);
-                    }
-                    eh[t] = __builtin_bit_cast(half8, h), el[t] = __builtin_bit_cast(half8, l);
+                    for (int i = 0; i < 4; ++i)
+                        v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_turned)(column + 32 * t + 4 * F::EP * (i % 2) + 32 * F::EP * (i / 2)));
+                    eh[t] = __builtin_bit_cast(half8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    el[t] = __builtin_bit_cast(half8, __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3, 4, 5, 6, 7));
                 }
                 const float back = pow2_field(es - 14) * vback;
                 while (true) {
