@@ -360,12 +360,20 @@ hipError_t launch_route_grad(const RouteArgs& a, sr_dtype z, sr_dtype v, int gri
 }
 
 // The kernels for many pixels (sr_route_lanes.h): lists of at most 16 entries, a pixel's logits within 32-bit offsets of one another.
-constexpr int64_t LANES_FROM = 2048;     // pixels
-int lanes_of(LaneArgs& a, const RouteArgs& r, sr_dtype z, sr_dtype v, const void* dz) {
+// A lane goes through its atoms one after the other, whatever the number of pixels, a wavefront for a pixel takes as long as there are
+// pixels; they meet (72 to 256 atoms, fp32 and bfloat16, us a wavefront / lanes): lists 4096 pixels 9.1 / 9.5 and 9.2 / 12.1; with the
+// losses 1024 pixels 17.2 / 21.0, 2048 pixels 21.9 / 21.1 and 43 / 26; gradient 4096 pixels 8.7 / 8.5, 256 atoms 8192 pixels 12.9 / 12.7
+// and 13.1 / 19.6.  Lists come from the same kernel with and without the losses, so that both calls give the same bits: 2048 pixels costs
+// the lists 2.5 us there and spares the losses 17.  Rows of up to 72 atoms, eight of them a load: one token 5.3 / 4.6, losses 10.9 / 11.6.
+int64_t lanes_from(const RouteArgs& r, bool gradient) {
+    if (gradient) return r.L > 128 ? 8192 : 4096;
+    return r.layout == SR_COEFF_PIXEL_MAJOR && r.L <= 8 * LCH && r.L % 8 == 0 ? 1 : 2048;
+}
+int lanes_of(LaneArgs& a, const RouteArgs& r, sr_dtype z, sr_dtype v, const void* dz, bool gradient) {
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR, pre = r.layout == SR_COEFF_PRE_SHUFFLE;
     const int64_t es = (int64_t)route_esize(z);
     const int G = pm || r.L > 8 * LCH ? 4 : 1;
-    if (r.T > 16 || r.total < LANES_FROM) return 0;
+    if (r.T > 16 || r.total < lanes_from(r, gradient)) return 0;
     if (G > 1 && 32 * r.lstride * es >= (int64_t)1 << 32) return 0;
     a.r = r;
     a.ipx = pre ? (int64_t)r.h * r.w : r.px;
@@ -414,7 +422,7 @@ int sr_list_route(const sr_tensor* coeff, int L, int scale, int entries, int kin
     const Span out[] = {span(index), span(value)}, in[] = {span(coeff), span(mask)};
     if (any_overlap(out, in)) return SR_ERR_ALIAS;
     LaneArgs m;
-    const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
+    const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr, false);
     const hipError_t e = G ? launch_lanes(m, coeff->dtype, G, false, grid_for(m.tiles, lanes_threads(false) / 64, 1 << 20), (hipStream_t)stream)
                            : launch_route<false>(a, coeff->dtype, value->dtype, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
@@ -446,7 +454,7 @@ int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries,
     if (!empty) {
         a.partial = workspace;
         LaneArgs m;
-        const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr);
+        const int G = lanes_of(m, a, coeff->dtype, value->dtype, nullptr, false);
         a.records = G ? grid_for(m.tiles, lanes_threads(true) / 64, compute_units() < ROUTE_RECORDS ? compute_units() : ROUTE_RECORDS) : blocks_for(a.total, ROUTE_RECORDS);
         e = G ? launch_lanes(m, coeff->dtype, G, true, a.records, (hipStream_t)stream)
               : launch_route<true>(a, coeff->dtype, value->dtype, a.records, (hipStream_t)stream);
@@ -481,7 +489,7 @@ int sr_list_route_grad(const sr_tensor* coeff, const sr_tensor* index, const sr_
     a.dz = dcoeff->data;
     const sr_dtype vd = dvalue ? dvalue->dtype : SR_F32;
     LaneArgs m;
-    const int G = lanes_of(m, a, coeff->dtype, vd, a.dz);
+    const int G = lanes_of(m, a, coeff->dtype, vd, a.dz, true);
     hipError_t e;
     if (!G) {
         e = launch_route_grad(a, coeff->dtype, vd, blocks_for(a.total, 8 * compute_units()), (hipStream_t)stream);
