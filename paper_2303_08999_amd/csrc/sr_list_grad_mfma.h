@@ -10,7 +10,8 @@
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
 // numbers, 22 bits; D likewise with one power of two; R takes the three products that matter.  For G the pixels of a unit share
-// the largest one's power of two (or up to eight times that: parts below 2^-35 of it are lost).  fp16 values enter as they are and
+// the largest one's power of two (or up to eight times that: parts below 2^-35 of it are lost; in a unit below 2^-64 of the
+// largest of its run, which a sum in fp32 can hardly hold beside it, below 2^-99 of that one).  fp16 values enter as they are and
 // the sums stay in the matrix instructions; fp32 ones are split as well, and a unit's sums are added unscaled.  Both are fp32, and
 // handed on in double after at most 4096 pixels of a wavefront.
 #pragma once
@@ -183,7 +184,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
         for (int t = 0; t < NT; ++t) G[mt][t] = (float4v){0, 0, 0, 0};
     double* const rec = a.partial ? a.partial + (size_t)blockIdx.x * a.L * KK : nullptr;
     bool first = true;
-    int held = 0, scale = 15;                        // G times 2^(scale - 14) is the sum (ACC)
+    int held = 0, scale = 15, top = 15;              // G times 2^(scale - 14) is the sum (ACC); the largest scale that this G has had
 
     struct Tile { int im, Y0, X0; int64_t list, image; };   // (elements before its lists, before its dout)
     auto tile_at = [&](unsigned t) -> Tile {
@@ -371,7 +372,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                             for (int s = 0; s < NS; ++s) {
                                 const half8 dh = __builtin_bit_cast(half8, F::DL ? Dsh[F::DL ? 2 * (mt * NS + s) * 64 + lane : 0] : Dh[F::DL ? 0 : mt][s]);
-                            const half8 dl = __builtin_bit_cast(half8, F::DL ? Dsh[F::DL ? (2 * (mt * NS + s) + 1) * 64 + lane : 0] : Dl[F::DL ? 0 : mt][s]);
+                                const half8 dl = __builtin_bit_cast(half8, F::DL ? Dsh[F::DL ? (2 * (mt * NS + s) + 1) * 64 + lane : 0] : Dl[F::DL ? 0 : mt][s]);
                                 const half8 eh = __builtin_bit_cast(half8, Eh[g][s]), el = __builtin_bit_cast(half8, El[g][s]);
                                 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dl, eh, r, 0, 0, 0);
                                 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(dh, el, r, 0, 0, 0);
@@ -388,7 +389,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                         for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
                         if (inside[g]) {
                             char* const to = (char*)a.dvalue + tl.list * VB;
-                        const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);
+                            const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);
 #pragma unroll
                             for (int r = 0; r < TQ; ++r)
                                 if (4 * r + q < a.T) st_from_float((TV*)(to + (entry[r] + x) * VB), 0, on[g] ? v[r] : 0.0f);
@@ -401,10 +402,13 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 // the unit's scale, its values' scale; E to [pixel][place], high parts, then low ones
                 int es = row_max(max(ex[0], ex[1]));
                 if (F::ACC) {
-                    // G's own power of two: at most four times the unit's, or G changes to the double of it
+                    // G's own power of two: at most four times the unit's, or G changes to the double of it; never below 2^-64 of
+                    // the largest that it has had: under that one it holds less than 2^(15 + 16) times the 2^16 entries of a run,
+                    // 2^111 under the smallest
                     es = __builtin_amdgcn_readfirstlane(es);
-                    if (es > scale || es < scale - 2) {
-                        const int to = min(es + 1, 254), by = scale - to;
+                    if (es > scale || (es < scale - 2 && scale > top - 64)) {
+                        const int to = max(min(es + 1, 254), top - 64), by = scale - to;
+                        top = max(top, to);
                         const float f1 = pow2_field(127 + by / 2), f2 = pow2_field(127 + by - by / 2);
 #pragma unroll
                         for (int mt = 0; mt < MT; ++mt)
@@ -529,6 +533,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
         // atoms 4 q .. 4 q + 3 of place n)
         if (rec && (++held == 4096 / (GM_TW * GM_TH / 4) || last)) {
             held = 0;
+            top = scale;
             const float back = F::ACC ? pow2_field(scale - 14) : 1.0f;
             int id = tid;                            // (hidden: no address of a record is worth a register for the whole tile)
             asm volatile("" : "+v"(id));

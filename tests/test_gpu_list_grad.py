@@ -117,6 +117,20 @@ def test_gradients_of_very_different_sizes_in_one_image(oracle):
     check(oracle, 1, 3, 16, 40, 4, 72, 5, 8, "f32", "f32", seed=9, spoil=spoil)
 
 
+@pytest.mark.parametrize("k,L,vd", [(5, 72, "f16"), (3, 40, "f16"), (7, 100, "f16"), (5, 72, "f32")])
+@pytest.mark.parametrize("small", [0.0, 2.0 ** -60])
+def test_runs_of_pixels_that_send_back_nothing_or_little(oracle, k, L, vd, small):
+    """Every other run of 32 pixels has a gradient of (nearly) 0 beside large ones, and atoms of its own: the power of two that a
+    wavefront's sums are held under goes down and up again, and the sums with it."""
+    def spoil(d):
+        x = torch.arange(d["dout"].shape[3]) // 32 % 2 == 1
+        d["dout"][..., x] *= small
+        d["dout"][:, :, 5:8] *= small
+        half = L // 2
+        d["index"] = torch.where(x, d["index"] % half, d["index"] % (L - half) + half).to(torch.uint8)
+    check(oracle, 1, 3, 20, 48, 4, L, k, 8, vd, "f32", seed=21, gain=256.0, spoil=spoil)
+
+
 @pytest.mark.parametrize("vd", ["f16", "f32"])
 def test_an_atom_listed_twice_gets_both_terms_and_large_indices_stay_inside(oracle, vd):
     def twice(d):
