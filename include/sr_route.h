@@ -39,7 +39,8 @@ typedef enum {
     SR_ROUTE_SOFTMAX = 0,      /* p of the listed atoms (softmax over all L)       */
     SR_ROUTE_CHOSEN  = 1,      /* softmax over the listed atoms alone              */
     SR_ROUTE_VALUES  = 2       /* the stored values themselves: `coeff` holds
-                                  coefficients, the largest are listed as they are */
+                                  coefficients, the largest are listed as they are
+                                  (-infinity too: no atom is masked)               */
 } sr_route_kind;
 
 /*
@@ -74,7 +75,7 @@ size_t sr_list_route_workspace_bytes(int L);
  *           the load is spread evenly; and (1/M) sum over live pixels of lse^2
  *   workspace, workspace_bytes   DEVICE scratch, 16-byte aligned; its contents before and after are meaningless
  *
- * p and lse are formed in fp32; the sums over pixels run in fp32 over at most 512 pixels and in double from there on.
+ * p and lse are formed in fp32; the sums over pixels run in fp32 over at most 4096 pixels and in double from there on.
  * Without a live pixel all of it is 0; an empty call writes that too.
  */
 int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries, int kind, int coeff_layout,
@@ -96,7 +97,8 @@ int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries,
  *
  * with G_l the gradient of atom l's value (0 where it is not listed), q = p for SR_ROUTE_SOFTMAX and the softmax over the
  * listed atoms for SR_ROUTE_CHOSEN, f_l = counts_l / (M entries).  For SR_ROUTE_VALUES it is G_l, and counts must be NULL.
- * Computed in fp32 from the logits, rounded once.  Masked pixels and masked atoms get 0.
+ * Computed in fp32 from the logits, rounded once.  Masked pixels (whose dvalue and index are not looked at) and masked atoms
+ * get 0.  dvalue is finite at the other pixels (else: unspecified values at that pixel).
  */
 int sr_list_route_grad(const sr_tensor* coeff, const sr_tensor* index, const sr_tensor* dvalue,
                        int L, int scale, int entries, int kind, int coeff_layout, const sr_tensor* mask,
@@ -120,7 +122,8 @@ size_t sr_dict_assemble_list_grad_workspace_bytes(int L, int k);
  *
  * index: atoms below L (others count as atom L - 1); an atom that is listed twice gets both terms.  Finite values only: infinities and NaN in
  * dict, lr, dout or value give unspecified results.  Arithmetic is fp32 or equivalent (fp16 matrix-core products of operands split
- * in two); ddict is summed in fp32 over runs of at most 4096 pixels and in double from there on.
+ * in two); ddict is summed in fp32 over runs of at most 4096 pixels and in double from there on, and what a pixel whose E is
+ * below 2^-64 of the largest in its run adds to it has fewer bits, none below 2^-99.
  * An empty call writes zeros to ddict.
  */
 int sr_dict_assemble_list_grad(const sr_tensor* lr, const sr_tensor* index, const sr_tensor* value, const sr_tensor* dict,

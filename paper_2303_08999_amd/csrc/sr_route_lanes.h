@@ -321,16 +321,41 @@ __global__ __launch_bounds__(lanes_threads(STATS), STATS ? 2 : 4) void k_route_l
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR;
     const int step = pm ? 1 : 64 / G;    // from one of a pixel's lanes to the next
     __shared__ unsigned bins[STATS ? LWAVES * SR_MAX_ATOMS : 1];
+    __shared__ double part[STATS ? LWAVES : 1][STATS ? G * NC * 8 : 1];
+    __shared__ float part_run[STATS ? LWAVES : 1][STATS ? G * NC * 8 : 1];
+    const int g = G == 1 ? 0 : (pm ? lane % G : lane / (64 / G));
     float share[STATS ? NC * 8 : 1];
     unsigned live = 0;
+    int run = 0;
     double sq = 0.0;
     if (STATS) {
 #pragma unroll
         for (int j = 0; j < NC * 8; ++j) share[j] = 0.0f;
         for (int l = threadIdx.x; l < LWAVES * SR_MAX_ATOMS; l += LNT) bins[l] = 0;
+        for (int l = lane; l < G * NC * 8; l += 64) part[wave][l] = 0.0;
         __syncthreads();
     }
+    // the lanes' shares are added up in fp32, each the sum of RUN tiles at most, and to what the wavefront has in double
+    constexpr int RUN = 64;
+    auto keep_shares = [&] {
+        const bool first = pm ? lane < G : lane % (64 / G) == 0;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = pixels_sum<G>(share[STATS ? c * 8 + j : 0], pm);
+                if (first) part_run[STATS ? wave : 0][STATS ? (c * G + g) * 8 + j : 0] = v;
+                share[STATS ? c * 8 + j : 0] = 0.0f;
+            }
+        asm volatile("" ::: "memory");                       // (a wavefront's LDS accesses keep their order)
+        for (int l = lane; l < G * NC * 8; l += 64) part[STATS ? wave : 0][STATS ? l : 0] += (double)part_run[STATS ? wave : 0][STATS ? l : 0];
+        asm volatile("" ::: "memory");
+    };
     for (int64_t tile = (int64_t)blockIdx.x * LWAVES + wave; tile < a.tiles; tile += (int64_t)gridDim.x * LWAVES) {
+        if (STATS && ++run > RUN) {
+            keep_shares();
+            run = 1;
+        }
         const LanePixel p = lane_pixel<TZ, G>(a, tile, lane);
         if (!p.inside) continue;
         if (r.mask && r.mask[p.mask] == 0) {
@@ -414,28 +439,18 @@ __global__ __launch_bounds__(lanes_threads(STATS), STATS ? 2 : 4) void k_route_l
         }
     }
     if (!STATS) return;
-    // over the wavefront's lanes in fp32, over the wavefronts in double
-    __shared__ float part[STATS ? LWAVES : 1][STATS ? G * NC * 8 : 1];
+    keep_shares();
     __shared__ double part_sq[LWAVES];
     __shared__ unsigned part_live[LWAVES];
-    const int g = G == 1 ? 0 : (pm ? lane % G : lane / (64 / G));
-    const bool first = pm ? lane < G : lane % (64 / G) == 0;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) sq += __shfl_xor(sq, d), live += __shfl_xor(live, d);
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float v = pixels_sum<G>(share[STATS ? c * 8 + j : 0], pm);
-            if (first) part[STATS ? wave : 0][STATS ? (c * G + g) * 8 + j : 0] = v;
-        }
     if (lane == 0) part_sq[wave] = sq, part_live[wave] = live;
     __syncthreads();
     const RouteRecord rec(r.partial, r.L, blockIdx.x);
     for (int l = threadIdx.x; l < r.L; l += LNT) {
         double v = 0.0;
         unsigned n = 0;
-        for (int w = 0; w < LWAVES; ++w) v += (double)part[STATS ? w : 0][STATS ? l : 0], n += bins[w * SR_MAX_ATOMS + l];
+        for (int w = 0; w < LWAVES; ++w) v += part[STATS ? w : 0][STATS ? l : 0], n += bins[w * SR_MAX_ATOMS + l];
         rec.share[l] = v;
         rec.counts[l] = n;
     }
@@ -451,7 +466,7 @@ __global__ __launch_bounds__(lanes_threads(STATS), STATS ? 2 : 4) void k_route_l
 // The gradient.  Which entry names an atom is a byte per atom in LDS, a row for every lane (all zero between tiles; the pitch of 19
 // words is free of bank conflicts); the entries' gradients are a table beside it, entry 0 the zero of atoms that are not listed.
 // 7 KB a wavefront and 110 registers: four wavefronts per SIMD hide the latency of a tile's loads (with the gradients themselves
-// scattered, 20 KB, it was two, and 1247 us instead of MEASURED for a 4K frame of 72 fp16 logits).
+// scattered, 20 KB, it was two, and 1247 us instead of 557 for a 4K frame of 72 fp16 logits).
 constexpr int DNT = 256, DWAVES = DNT / 64;
 
 template <typename TZ, int G, bool VEC, int NC, bool FULL, int TT, int KIND, bool LOSS>

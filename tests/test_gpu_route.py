@@ -447,3 +447,28 @@ def test_long_sums():
     assert ((value.double() - v).abs() <= v * (L + 1.75 * 16 + 8) * U).all()
     lse = torch.logsumexp(z.double(), 1)
     assert abs(float(loss[1]) - float((lse * lse).mean())) <= float((lse * lse).mean()) * (514 + 150) * U
+
+
+@pytest.mark.parametrize("layout,L,H,W", [(PM, 16, 31, 100_003), (PLANAR, 9, 9, 1_000_011)], ids=["rows", "planes"])
+def test_sums_over_many_runs(layout, L, H, W):
+    """More tiles for every wavefront than one run in fp32 takes (64, then the 64 lanes: 70 additions one after the other)."""
+    T = 2
+    g = torch.Generator(device=DEV).manual_seed(78)
+    z = torch.randn((1, H, W, L) if layout == PM else (1, L, H, W), device=DEV, generator=g).bfloat16()
+    mask = (torch.rand((1, 1, H, W), device=DEV, generator=g) < 0.9).byte()
+    index, value = torch.empty((1, T, H, W), device=DEV, dtype=torch.uint8), torch.empty((1, T, H, W), device=DEV)
+    counts, share, loss = torch.empty(L + 1, device=DEV, dtype=torch.int64), torch.empty(L, device=DEV), torch.empty(2, device=DEV)
+    sr.sr_list_route_balance(z, L, 1, T, SOFT, layout, mask, index, value, counts, share, loss)
+    on = mask.reshape(-1) != 0
+    rows = (z.reshape(-1, L) if layout == PM else z.reshape(L, -1).t())[on].float()
+    order = torch.sort(rows, dim=1, descending=True, stable=True).indices[:, :T]
+    assert torch.equal(index.reshape(T, -1).t()[on].long(), order)
+    assert torch.equal(counts[:L], torch.bincount(order.reshape(-1), minlength=L)) and int(counts[L]) == rows.shape[0]
+    s = torch.zeros(L, device=DEV, dtype=torch.float64)
+    sq = 0.0
+    for part in rows.split(1 << 20):
+        s += torch.softmax(part.double(), 1).sum(0)
+        sq += float((torch.logsumexp(part.double(), 1) ** 2).sum())
+    s, sq = s / rows.shape[0], sq / rows.shape[0]
+    assert ((share.double() - s).abs() <= s * (L + 1.75 * 16 + 8 + 71) * U).all()
+    assert abs(float(loss[1]) - sq) <= sq * (1 + 150) * U
