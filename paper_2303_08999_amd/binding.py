@@ -444,10 +444,12 @@ def _plain(t, dtype, count, what):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _scratch(workspace, need, like):
+def _scratch(workspace, need, like, stream):
+    """Scratch of the stream that the call runs on: what frees and reuses it later waits for the call."""
     import torch
     if workspace is None:
-        workspace = torch.empty(max(need, 16), device=like.device, dtype=torch.uint8)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            workspace = torch.empty(max(need, 16), device=like.device, dtype=torch.uint8)
     elif not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     return workspace
@@ -470,8 +472,8 @@ def sr_list_route_balance(coeff, L, scale, entries, kind, coeff_layout, mask, in
     """sr_list_route with the atoms' counts (int64, L + 1) and shares (float32, L) and the two losses (float32, 2);
     scratch is made here unless the caller passes it."""
     import torch
-    workspace = _scratch(workspace, sr_list_route_workspace_bytes(L), coeff)
     _here(coeff, mask, index, value, counts, share, loss, workspace)
+    workspace = _scratch(workspace, sr_list_route_workspace_bytes(L), coeff, stream)
     _check(load().sr_list_route_balance(_logits(coeff, coeff_layout), L, scale, entries, kind, coeff_layout, _maybe(mask),
                                         describe(index), describe(value), _plain(counts, torch.int64, L + 1, "counts"),
                                         _plain(share, torch.float32, L, "share"), _plain(loss, torch.float32, 2, "loss"),
@@ -501,9 +503,9 @@ def sr_dict_assemble_list_grad(lr, index, value, dict, L, k, scale, channels, en
                                workspace=None, stream=None):
     """Gradient of sr_dict_assemble_list with respect to the values (``dvalue``) and the dictionary (``ddict``, of the
     dictionary's shape), either of which may be None; scratch is made here unless the caller passes it."""
-    if ddict is not None:
-        workspace = _scratch(workspace, sr_dict_assemble_list_grad_workspace_bytes(L, k), lr)
     _here(lr, index, value, dict, mask, dout, dvalue, ddict, workspace)
+    if ddict is not None:
+        workspace = _scratch(workspace, sr_dict_assemble_list_grad_workspace_bytes(L, k), lr, stream)
     if ddict is not None and not ddict.is_contiguous():
         raise ValueError("ddict must be contiguous")
     _check(load().sr_dict_assemble_list_grad(describe(lr), describe(index), describe(value), describe(_dict4(dict)),

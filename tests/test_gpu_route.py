@@ -472,3 +472,27 @@ def test_sums_over_many_runs(layout, L, H, W):
     s, sq = s / rows.shape[0], sq / rows.shape[0]
     assert ((share.double() - s).abs() <= s * (L + 1.75 * 16 + 8 + 71) * U).all()
     assert abs(float(loss[1]) - sq) <= sq * (1 + 150) * U
+
+
+def test_scratch_made_by_a_call_belongs_to_its_stream(monkeypatch):
+    """(Else the current stream may still write to that memory, or get it again before the call has run.)"""
+    L, T, k, h, w, s = 16, 4, 3, 20, 30, 2
+    g = torch.Generator(device=DEV).manual_seed(79)
+    z, lr = torch.randn((1, L, h * s, w * s), device=DEV, generator=g), torch.rand((1, 3, h, w), device=DEV, generator=g)
+    D, dout = torch.randn((L, k, k), device=DEV, generator=g), torch.randn((1, 3, h * s, w * s), device=DEV, generator=g)
+    index, value = torch.empty((1, T, h * s, w * s), device=DEV, dtype=torch.uint8), torch.empty((1, T, h * s, w * s), device=DEV)
+    outs = []
+    side, make, made = torch.cuda.Stream(), torch.empty, []
+    for stream in (None, side, side.cuda_stream):
+        counts, share, loss = torch.empty(L + 1, device=DEV, dtype=torch.int64), torch.empty(L, device=DEV), torch.empty(2, device=DEV)
+        dv, dd = torch.empty_like(value), torch.empty_like(D)
+        torch.cuda.synchronize()
+        with monkeypatch.context() as m:
+            m.setattr(torch, "empty", lambda *a, **kw: (made.append(torch.cuda.current_stream().cuda_stream), make(*a, **kw))[1])
+            sr.sr_list_route_balance(z, L, 1, T, SOFT, PLANAR, None, index, value, counts, share, loss, stream=stream)
+            sr.sr_dict_assemble_list_grad(lr, index, value, D, L, k, s, 3, T, None, dout, dv, dd, stream=stream)
+        torch.cuda.synchronize()
+        outs.append((counts, share, loss, dv, dd))
+    assert made == [torch.cuda.current_stream().cuda_stream] * 2 + [side.cuda_stream] * 4
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], o))
