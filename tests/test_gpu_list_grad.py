@@ -203,3 +203,27 @@ def test_a_frame_of_many_tiles(oracle):
     assert float((dd.double().reshape(L, -1) - want).norm() / want.norm()) <= 4e-6
     response = (D.reshape(L, -1).double() @ E).gather(0, index.reshape(T, -1))
     assert float((dv.double().reshape(T, -1) - response).norm() / response.norm()) <= 2.0 ** -11
+
+
+@pytest.mark.parametrize("k,T,vd", [(3, 3, "f32"), (5, 8, "f16")])
+def test_errors_do_not_add_up_where_the_gradients_cancel(oracle, k, T, vd):
+    """Gradients of either sign over 900 000 pixels: the sum is a thousandth of its terms' magnitudes, an error of one sign in every
+    product would be as large.  E and the values have 22 bits, what is left out of their product is 2^-22 of it, the fp32 sums
+    of a run round 16 times by 2^-24: each at random beside the terms, so that the sum keeps 4 x 2^-22."""
+    n, C, h, w, s, L = 3, 3, 101, 179, 4, 72
+    g = torch.Generator(device=DEV).manual_seed(52)
+    H, W = h * s, w * s
+    value, index = torch.rand((n, L, H, W), device=DEV, generator=g).topk(T, dim=1)
+    value = (value / value.sum(1, keepdim=True)).to(DT[vd])
+    lr, D = torch.rand((n, C, h, w), device=DEV, generator=g), torch.randn((L, k, k), device=DEV, generator=g) / k
+    dout = torch.randn((n, C, H, W), device=DEV, generator=g) / 64
+    dd = torch.empty_like(D)
+    sr.sr_dict_assemble_list_grad(lr, index.to(torch.uint8), value, D, L, k, s, C, T, None, dout, None, dd)
+    r = k // 2
+    pad = torch.nn.functional.pad(torch.from_numpy(oracle.bicubic(lr.cpu().numpy(), s)).to(DEV).double(), (r, r, r, r), mode="replicate")
+    want = torch.zeros((L, k * k), device=DEV, dtype=torch.float64)
+    for b in range(n):
+        E = torch.stack([(pad[b, :, i // k:i // k + H, i % k:i % k + W] * dout[b].double()).sum(0) for i in range(k * k)], 0).reshape(k * k, -1)
+        phi = torch.zeros((L, H * W), device=DEV, dtype=torch.float64).scatter_add_(0, index[b].reshape(T, -1), value[b].double().reshape(T, -1))
+        want += phi @ E.t().contiguous()
+    assert float((dd.double().reshape(L, -1) - want).norm() / want.norm()) <= 4 * 2.0 ** -22
