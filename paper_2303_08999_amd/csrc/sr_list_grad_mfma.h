@@ -541,8 +541,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
         // atoms 4 q .. 4 q + 3 of place n)
         if (rec && (++held == 4096 / (GM_TW * GM_TH / 4) || last)) {
             held = 0;
-            top = scale;
             const float back = F::ACC ? turn * pow2_field(scale - 14) : 1.0f;
+            scale = top = 15;                        // G is 0 again: the next run's sums owe nothing to this one's
             int id = tid;                            // (hidden: no address of a record is worth a register for the whole tile)
             asm volatile("" : "+v"(id));
 #pragma unroll

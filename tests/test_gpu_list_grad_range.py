@@ -1,0 +1,28 @@
+"""Gradient of the per-pixel list form where operands differ in size, against the 64-bit oracle: bounds as in test_gpu_list_grad.py, an atom's
+ddict against the magnitudes of its own terms, a response against its own atom's."""
+import pytest
+import torch
+
+import paper_2303_08999_amd as sr
+from test_gpu_list_grad import DEV, U
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_run_of_pixels_owes_nothing_to_the_run_before():
+    """A wavefront hands its sums on after 4096 pixels.  Those of the next ones send back 2^-95 of what the first did, to an atom of their
+    own, and all of them alike: they keep their bits.  (An image of ones has E = dout in every place; weights of scale 2 are exact.)"""
+    grid = min(512, 2 * torch.cuda.get_device_properties(0).multi_processor_count)
+    first, W = 32 * 8 * grid, 64                             # rows of 64 pixels: a tile of 8 of them a workgroup, 32 times over
+    H = first + 2 * 8 * grid
+    g = torch.Generator(device=DEV).manual_seed(1)
+    lr = torch.ones((1, 1, H // 2, W // 2), device=DEV)
+    dout = torch.ones((1, 1, H, W), device=DEV)
+    dout[:, :, first:] = 2.0 ** -95 * (1 + torch.rand((1, 1, H - first, W), device=DEV, generator=g))
+    index = torch.zeros((1, 1, H, W), device=DEV, dtype=torch.uint8)
+    index[:, :, first:] = 1
+    dd = torch.empty((2, 3, 3), device=DEV)
+    sr.sr_dict_assemble_list_grad(lr, index, torch.ones((1, 1, H, W), device=DEV, dtype=torch.float16),
+                                  torch.ones((2, 3, 3), device=DEV), 2, 3, 2, 1, 1, None, dout, None, dd)
+    want = torch.stack([dout[0, 0, :first].double().sum(), dout[0, 0, first:].double().sum()]).view(2, 1, 1).expand(2, 3, 3)
+    assert ((dd.double() - want).abs() <= (1 + 24 + 4096) * U * want).all()
