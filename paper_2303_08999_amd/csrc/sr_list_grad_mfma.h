@@ -150,7 +150,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     for (int e = lane; e < F::PHI_B / 16; e += 64) ((lds_u4*)phi)[e] = (u32x4v){0, 0, 0, 0};
     __syncthreads();
     const int dx = exponent_field(fmaxf(fmaxf(dmax[0], dmax[1]), fmaxf(dmax[2], dmax[3])));
-    const float dscale = pow2_field(268 - dx), dback = pow2_field(dx - 14);
+    const float dscale = pow2_field(268 - dx);
     u32x4v Dh[F::DL ? 1 : MT][NS], Dl[F::DL ? 1 : MT][NS];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -391,10 +391,11 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     wave_lds_fence();
 #pragma unroll
                     for (int g = g0; g < g0 + F::RG; ++g) {
-                        const float back = pow2_field(ex[g] - 14);
+                        // both powers of two undone at once: a response has a place in fp32 where one of them alone would lead out of it
+                        const int back = ex[g] + dx - 2 * (127 + 14);
                         float v[TQ];
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) v[r] = *(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])) * back * dback;
+                        for (int r = 0; r < TQ; ++r) v[r] = __builtin_ldexpf(*(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])), back);
                         if (inside[g]) {
                             char* const to = (char*)a.dvalue + tl.list * VB;
                             const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2303_08999_amd as sr
-from test_gpu_list_grad import DEV, U
+from test_gpu_list_grad import DEV, U, check
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +26,11 @@ def test_a_run_of_pixels_owes_nothing_to_the_run_before():
                                   torch.ones((2, 3, 3), device=DEV), 2, 3, 2, 1, 1, None, dout, None, dd)
     want = torch.stack([dout[0, 0, :first].double().sum(), dout[0, 0, first:].double().sum()]).view(2, 1, 1).expand(2, 3, 3)
     assert ((dd.double() - want).abs() <= (1 + 24 + 4096) * U * want).all()
+
+
+@pytest.mark.parametrize("C,k,L", [(1, 5, 72), (3, 3, 40), (1, 7, 100)])
+def test_gradients_near_the_top_of_the_type(oracle, C, k, L):
+    """An image's gradient of 2^112 and small atoms: responses have a place in fp32, and so has everything on the way to them."""
+    def spoil(d):
+        d["dict"] *= 2.0 ** -7
+    check(oracle, 1, C, 10, 33, 2, L, k, 8, "f32", "f32", seed=31, gain=2.0 ** 112, spoil=spoil)
