@@ -9,7 +9,7 @@
 // for its gather.  All of that is a wavefront's own scratch: no barrier but around the up-sampled tile.
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
-// numbers, 22 bits; D likewise with one power of two; R takes the three products that matter.  For G the pixels of a unit share
+// numbers, 22 bits; D likewise, atom by atom; R takes the three products that matter.  For G the pixels of a unit share
 // the largest one's power of two (or up to eight times that: parts below 2^-35 of it are lost; in a unit below 2^-64 of the
 // largest of its run, which a sum in fp32 can hardly hold beside it, below 2^-99 of that one).  fp16 values enter as they are and
 // the sums stay in the matrix instructions; fp32 ones are split as well, and a unit's sums are added unscaled.  Both are fp32, and
@@ -130,7 +130,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
     __shared__ float4 yw[UH];                        // a tile's rows: weights, first LR row
     __shared__ int yb[UH];
     __shared__ __align__(16) unsigned char scratch[4][F::WAVE_B];
-    __shared__ float dmax[4];
+    __shared__ int dback[LP];                        // of an atom: what undoes its power of two, and what is common to every pixel's
     __shared__ u32x4v Dsh[F::DL ? 2 * MT * NS * 64 : 1];
 
     const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, n = lane & 15;
@@ -141,39 +141,39 @@ void k_list_grad_mfma(const ListGradArgs a) {
     const int64_t plane = (int64_t)a.H * a.W;
     const unsigned lmax = (unsigned)a.L - 1u;
 
-    // ---- the dictionary as operands of R: lane (q, n) has atom 16 mt + n, taps 32 s + 8 q and on, times 2^14 / its largest exponent
-    float big = 0.0f;
-    for (int e = tid; e < a.L * KK; e += 256) big = fmaxf(big, fabsf(a.dict[e]));
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
-    if (lane == 0) dmax[wave] = big;
+    // ---- the dictionary as operands of R: lane (q, n) has atom 16 mt + n, taps 32 s + 8 q and on, the atom times a power of two (to
+    // 2^14 .. 2^15)
     for (int e = lane; e < F::PHI_B / 16; e += 64) ((lds_u4*)phi)[e] = (u32x4v){0, 0, 0, 0};
-    __syncthreads();
-    const int dx = exponent_field(fmaxf(fmaxf(dmax[0], dmax[1]), fmaxf(dmax[2], dmax[3])));
-    const float dscale = pow2_field(268 - dx);
     u32x4v Dh[F::DL ? 1 : MT][NS], Dl[F::DL ? 1 : MT][NS];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt) {
+        if (F::DL && (mt & 3) != wave) continue;
+        const int l = 16 * mt + n;
+        float v[NS][8], big = 0.0f;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            if (F::DL && (mt & 3) != wave) continue;
-            const int l = 16 * mt + n;
-            float v[8];
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int j = F::tap(s, q, i);
-                v[i] = l < a.L && j >= 0 ? a.dict[l * KK + j] : 0.0f;
+                v[s][i] = l < a.L && j >= 0 ? a.dict[l * KK + j] : 0.0f;
+                big = fmaxf(big, fabsf(v[s][i]));
             }
+        const int dx = exponent_field(rows_max(big));
+        const float dscale = pow2_field(268 - dx);
+        dback[l] = dx - 2 * (127 + 14);              // (the four lanes of an atom write the same)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
             u32x4v dh, dl;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 unsigned hi, lo;
-                split_pair(v[2 * i], v[2 * i + 1], dscale, hi, lo);
+                split_pair(v[s][2 * i], v[s][2 * i + 1], dscale, hi, lo);
                 dh[i] = hi, dl[i] = lo;
             }
             if (F::DL) Dsh[F::DL ? 2 * (mt * NS + s) * 64 + lane : 0] = dh, Dsh[F::DL ? (2 * (mt * NS + s) + 1) * 64 + lane : 0] = dl;
             else Dh[F::DL ? 0 : mt][s] = dh, Dl[F::DL ? 0 : mt][s] = dl;
         }
+    }
     // where a lane's taps are in the tile, from the wavefront's first row on, in bytes (places without one: the patch's last tap; their
     // responses meet zeros of D, their columns of G are not handed on)
     int tap[NS][NI];
@@ -392,10 +392,10 @@ void k_list_grad_mfma(const ListGradArgs a) {
 #pragma unroll
                     for (int g = g0; g < g0 + F::RG; ++g) {
                         // both powers of two undone at once: a response has a place in fp32 where one of them alone would lead out of it
-                        const int back = ex[g] + dx - 2 * (127 + 14);
                         float v[TQ];
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) v[r] = __builtin_ldexpf(*(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])), back);
+                        for (int r = 0; r < TQ; ++r)
+                            v[r] = __builtin_ldexpf(*(lds_f*)(er + (g - g0) * F::R_B + 4 * (n * F::RP + f.idx[g][r])), ex[g] + dback[f.idx[g][r]]);
                         if (inside[g]) {
                             char* const to = (char*)a.dvalue + tl.list * VB;
                             const unsigned x = (unsigned)Y * (unsigned)a.W + (unsigned)(tl.X0 + x0 + 16 * g + n);

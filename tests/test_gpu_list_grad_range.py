@@ -34,3 +34,11 @@ def test_gradients_near_the_top_of_the_type(oracle, C, k, L):
     def spoil(d):
         d["dict"] *= 2.0 ** -7
     check(oracle, 1, C, 10, 33, 2, L, k, 8, "f32", "f32", seed=31, gain=2.0 ** 112, spoil=spoil)
+
+
+@pytest.mark.parametrize("C,k,L,T", [(3, 5, 72, 8), (1, 3, 40, 4), (1, 7, 100, 12), (3, 5, 128, 3)])
+def test_weak_atoms_beside_strong_ones(oracle, C, k, L, T):
+    """Atoms of a dictionary that is being learnt start at nothing: a response has its precision beside its own atom, not the largest."""
+    def spoil(d):
+        d["dict"] *= 2.0 ** -(9.0 * (torch.arange(L) % 8)).view(L, 1, 1)
+    check(oracle, 1, C, 13, 37, 2, L, k, T, "f32", "f32", seed=33, spoil=spoil)
