@@ -10,8 +10,11 @@
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
 // numbers, 22 bits; D likewise, atom by atom; R takes the three products that matter.  For G the pixels of a unit share
-// the largest one's power of two (or up to eight times that: parts below 2^-35 of it are lost; in a unit below 2^-64 of the
-// largest of its run, which a sum in fp32 can hardly hold beside it, below 2^-99 of that one).  fp16 values enter as they are and
+// the largest one's power of two (or up to four times that); those that are 2^16 and more below it, whose lower parts fp16 would cut
+// off, take it less whole steps of 2^16 and are added after the others, in a product of their own for each distance: an atom that quiet
+// pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16: 421 us, 417 without it;
+// 730 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom listed twice, which
+// goes the same way: what the frequent case takes of registers went first.)  fp16 values enter as they are and
 // the sums stay in the matrix instructions; fp32 ones are split as well, and a unit's sums are added unscaled.  Both are fp32, and
 // handed on in double after at most 4096 pixels of a wavefront.  The matrix instructions cut off below: their sums are a little too low, whatever
 // the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E: a 4K frame's ddict
@@ -61,6 +64,8 @@ struct GradCfg {
     static constexpr int ER_B = ER_0 > VN * 4 ? ER_0 : (VN * 4 + 15) / 16 * 16;
     static constexpr int WAVE_B = PHI_B + ER_B;
     static constexpr bool DL = K == 7 && LP > 80 && !SPLIT;                            // D's operands in LDS, not in 128 registers
+    // Two fp16 numbers hold 2^14 .. 2^15 down to 2^-25: a number that is less than this many powers of two below keeps fp32's half step.
+    static constexpr int STEP = 16;
     static constexpr bool ACC = !SPLIT;            // G is summed by the matrix instructions, under one power of two
     static constexpr int WPE = K == 7 || LP > 80 || SPLIT ? 1 : 2;                     // wavefronts per SIMD (registers, LDS)
     static_assert(LP * 16 * 4 <= ER_B && CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
@@ -84,6 +89,11 @@ __device__ __forceinline__ int row_max(int v) {
     v = max(v, row_turned<0x124>(v));
     v = max(v, row_turned<0x122>(v));
     return max(v, row_turned<0x121>(v));
+}
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = min(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
 }
 __device__ __forceinline__ float rows_max(float v) {
     const unsigned u = __float_as_uint(v);           // magnitudes: their order is that of their bits
@@ -334,7 +344,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
             }
             u32x4v Eh[2][NS], El[2][NS];             // E of the pixel's own scale, high and low parts
-            int ex[2];
+            int ex[2];                               // 0: all of it is 0
 #pragma unroll
             for (int g0 = 0; g0 < 2; g0 += F::RG) {
 #pragma unroll
@@ -360,7 +370,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                         for (int i = NI; i < 8; ++i) E[s][i] = 0.0f;
                     }
                     m = rows_max(m);
-                    ex[g] = exponent_field(m);
+                    ex[g] = m > 0.0f ? exponent_field(m) : 0;
                     const float sc = pow2_field(268 - ex[g]);
 #pragma unroll
                     for (int s = 0; s < NS; ++s)
@@ -415,7 +425,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     // the largest that it has had: under that one it holds less than 2^(15 + 16) times the 2^16 entries of a run,
                     // 2^111 under the smallest
                     es = __builtin_amdgcn_readfirstlane(es);
-                    if (es > scale || (es < scale - 2 && scale > top - 64)) {
+                    if (es > scale || (es > 0 && es < scale - 2 && scale > top - 64)) {
                         const int to = max(min(es + 1, 254), top - 64), by = scale - to;
                         top = max(top, to);
                         const float f1 = pow2_field(127 + by / 2), f2 = pow2_field(127 + by - by / 2);
@@ -430,6 +440,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     es = scale;
                 }
                 float vback = 1.0f;
+                int below[2];
                 unsigned val[2][TQ], vlo[2][F::SPLIT ? TQ : 1];
                 if (F::SPLIT) {
                     float m = 0.0f;
@@ -449,7 +460,10 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    const _Float16 fs = (_Float16)(turn * pow2_field(127 + ex[g] - es));
+                    // a pixel that is n whole steps below the unit's power of two: n steps less, which are made up for when its entries are
+                    // added, after the other ones'
+                    below[g] = ex[g] > 0 ? ((es - ex[g]) & -F::STEP) : 0;
+                    const _Float16 fs = (_Float16)(turn * pow2_field(127 + ex[g] - es + below[g]));
                     const half2v ff = {fs, fs};
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
@@ -470,21 +484,22 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 wave_lds_fence();
                 // ... and back turned: of the 16 places t, four pixels' rows at a time, lane n gets its place's column; lane (q, n) has pixels
                 // 8 q .. 8 q + 7 of place 16 t + n then
-                half8 eh[NT], el[NT];
-                unsigned char* const column = er + (8 * q + n / 4) * F::EP + 8 * (n % 4);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
+                int column = (8 * q + n / 4) * F::EP + 8 * (n % 4);
+                auto turned = [&](int t, half8& high, half8& low) {
                     short4v v[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_turned)(column + 32 * t + 4 * F::EP * (i % 2) + 32 * F::EP * (i / 2)));
-                    eh[t] = __builtin_bit_cast(half8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    el[t] = __builtin_bit_cast(half8, __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3, 4, 5, 6, 7));
-                }
+                        v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_turned)(er + column + 32 * t + 4 * F::EP * (i % 2) + 32 * F::EP * (i / 2)));
+                    high = __builtin_bit_cast(half8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    low = __builtin_bit_cast(half8, __builtin_shufflevector(v[2], v[3], 0, 1, 2, 3, 4, 5, 6, 7));
+                };
+                half8 eh[NT], el[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) turned(t, eh[t], el[t]);
                 const float back = turn * pow2_field(es - 14) * vback;
-                while (true) {
-                    int put[2][TQ];
-                    bool more = false;
+                // Entries to their places, one of those that share one; what has none yet stays in `cur`
+                int put[2][TQ];
+                auto scatter = [&] {
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -493,28 +508,20 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             const bool mine = seen[g][r] == (unsigned)(4 * r + q + 1);
                             put[g][r] = mine ? cur[g][r] : aside;
                             cur[g][r] = mine ? aside : cur[g][r];
-                            more = more || cur[g][r] != aside;
                             *(lds_h*)(phi + put[g][r]) = (unsigned short)val[g][r];
                             if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = (unsigned short)vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0];
                         }
                     wave_lds_fence();
+                };
+                auto left = [&]() -> bool {
+                    bool more = false;
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        const half8 p0 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((16 * mt + n) * F::PP + 8 * q)));
-                        half8 p1;
-                        if (F::SPLIT) p1 = __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((F::PHI_ROWS + 16 * mt + n) * F::PP + 8 * q)));
+                    for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            float4v r = F::ACC ? G[mt][t] : (float4v){0, 0, 0, 0};
-                            if (F::SPLIT) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, eh[t], r, 0, 0, 0);
-                            r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, el[t], r, 0, 0, 0);
-                            r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, eh[t], r, 0, 0, 0);
-                            if (F::ACC) G[mt][t] = r;
-                            else
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) G[mt][t][i] = fmaf(r[i], back, G[mt][t][i]);
-                        }
-                    }
+                        for (int r = 0; r < TQ; ++r) more = more || cur[g][r] != 2 * (LP * F::PP + 16 * g + n);
+                    return __any(more);
+                };
+                auto clear = [&] {
                     wave_lds_fence();
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
@@ -524,17 +531,84 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = 0;
                         }
                     wave_lds_fence();
-                    if (!__any(more)) break;
+                };
+                auto operand = [&](int mt, int part) -> half8 {
+                    return __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((part * F::PHI_ROWS + 16 * mt + n) * F::PP + 8 * q)));
+                };
+                auto product = [&](half8 p0, half8 p1, half8 high, half8 low, float4v r) -> float4v {
+                    if (F::SPLIT) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, high, r, 0, 0, 0);
+                    r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, low, r, 0, 0, 0);
+                    return __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, high, r, 0, 0, 0);
+                };
+                scatter();
+                if (__any(below[0] | below[1])) {                // pixels below the others: not yet
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) *(lds_h*)(phi + cur[g][r]) = (unsigned short)(4 * r + q + 1);
+                        for (int r = 0; r < TQ; ++r) {
+                            const int aside = 2 * (LP * F::PP + 16 * g + n), out = below[g] ? put[g][r] : aside;
+                            *(lds_h*)(phi + out) = 0;
+                            if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + out) = 0;
+                            cur[g][r] = out != aside ? out : cur[g][r];
+                        }
+                    wave_lds_fence();
+                }
+                bool more = left();
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const half8 p0 = operand(mt, 0), p1 = F::SPLIT ? operand(mt, 1) : p0;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const float4v r = product(p0, p1, eh[t], el[t], F::ACC ? G[mt][t] : (float4v){0, 0, 0, 0});
+                        if (F::ACC) G[mt][t] = r;
+                        else
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) G[mt][t][i] = fmaf(r[i], back, G[mt][t][i]);
+                    }
+                }
+                clear();
+                // What is left, if anything: pixels below the others, the nearest ones first, and atoms listed twice.  Every turn adds an entry: of
+                // those that it is for all write their numbers, and one of each place finds its own.
+                while (more) {
+                    int less = 1 << 20;
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r) less = cur[g][r] != 2 * (LP * F::PP + 16 * g + n) ? min(less, below[g]) : less;
+                    less = wave_min(less);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+#pragma unroll
+                        for (int r = 0; r < TQ; ++r)
+                            *(lds_h*)(phi + (below[g] == less ? cur[g][r] : 2 * (LP * F::PP + 16 * g + n))) = (unsigned short)(4 * r + q + 1);
                     wave_lds_fence();
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
                     wave_lds_fence();
+                    scatter();
+                    more = left();
+                    asm volatile("" : "+v"(column));         // (hidden: E is read again; kept, it would take registers of every unit)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        __builtin_amdgcn_sched_barrier(0);   // (one product at a time, for the same reason)
+                        half8 high, low;
+                        turned(t, high, low);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            const float4v r = product(operand(mt, 0), F::SPLIT ? operand(mt, 1) : high, high, low, (float4v){0, 0, 0, 0});
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float v = __builtin_ldexpf(r[i], -less);
+                                // (atoms 4 q + i of the tile times one: the matrix instructions' registers are theirs alone)
+                                if (F::ACC) G[mt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(n == 4 * q + i ? 1.0f : 0.0f, v, G[mt][t], 0, 0, 0);
+                                else G[mt][t][i] = fmaf(v, back, G[mt][t][i]);
+                            }
+                        }
+                    }
+                    clear();
                 }
             }
         }

@@ -42,3 +42,39 @@ def test_weak_atoms_beside_strong_ones(oracle, C, k, L, T):
     def spoil(d):
         d["dict"] *= 2.0 ** -(9.0 * (torch.arange(L) % 8)).view(L, 1, 1)
     check(oracle, 1, C, 13, 37, 2, L, k, T, "f32", "f32", seed=33, spoil=spoil)
+
+
+def apart(d, groups, part):
+    """Lists of different atoms; pixels (and entries) of a part have atoms that no other part has."""
+    L, (n, T, H, W) = d["dict"].shape[0], d["index"].shape
+    size = L // groups
+    t, y, x = torch.arange(T).view(T, 1, 1), torch.arange(H).view(H, 1), torch.arange(W)
+    d["index"] = (part * size + (t + 3 * y + 5 * x) % size).expand(n, T, H, W).to(torch.uint8).contiguous()
+
+
+@pytest.mark.parametrize("ratios", [(2.0 ** -24,), (2.0 ** -26, 2.0 ** -32, 2.0 ** -70), (2.0 ** -12, 2.0 ** -15, 2.0 ** -18), (2.0 ** -95,)],
+                         ids=["24", "26_32_70", "12_15_18", "95"])
+@pytest.mark.parametrize("C,k,L,T,vd", [(3, 5, 72, 8, "f16"), (3, 5, 72, 8, "f32"), (1, 3, 40, 4, "f16"), (1, 3, 40, 9, "f32"),
+                                        (3, 7, 128, 16, "f16"), (3, 7, 100, 12, "f32"), (1, 5, 128, 5, "f16")])
+def test_quiet_pixels_among_loud_ones(oracle, C, k, L, T, vd, ratios):
+    """Single pixels send back next to nothing beside their neighbours, to atoms that nobody else names."""
+    def spoil(d):
+        part = torch.zeros(d["dout"].shape[3], dtype=torch.long)
+        for i, r in enumerate(ratios):
+            part[5 + 7 * i::32] = i + 1
+            d["dout"][..., 5 + 7 * i::32] *= r
+        apart(d, len(ratios) + 1, part)
+    check(oracle, 1, C, 20, 50, 2, L, k, T, vd, "f32", seed=41, gain=16.0, spoil=spoil)
+
+
+@pytest.mark.parametrize("vd", ["f16", "f32"])
+def test_quiet_pixels_that_list_an_atom_twice(oracle, vd):
+    def spoil(d):
+        part = torch.zeros(d["dout"].shape[3], dtype=torch.long)
+        for i, r in enumerate((2.0 ** -26, 2.0 ** -50)):
+            part[5 + 7 * i::32] = i + 1
+            d["dout"][..., 5 + 7 * i::32] *= r
+        apart(d, 3, part)
+        d["index"][:, 3] = d["index"][:, 0]
+        d["index"][:, 5, ::2] = d["index"][:, 0, ::2]
+    check(oracle, 1, 3, 20, 50, 2, 72, 5, 8, vd, "f32", seed=43, spoil=spoil)
