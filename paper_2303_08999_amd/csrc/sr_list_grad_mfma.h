@@ -15,7 +15,9 @@
 // pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16: 421 us, 417 without it;
 // 730 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom listed twice, which
 // goes the same way: what the frequent case takes of registers went first.)  fp16 values enter as they are and
-// the sums stay in the matrix instructions; fp32 ones are split as well, and a unit's sums are added unscaled.  Both are fp32, and
+// the sums stay in the matrix instructions; fp32 ones are split as well, the low part kept 2^11
+// higher, under one power of two: those that are 2^28 and more below the largest wait likewise (softmax lists of logits of deviation 8, where
+// most units have such a value: a 4K frame 804 -> 1520 us); a unit's sums are added unscaled.  Both are fp32, and
 // handed on in double after at most 4096 pixels of a wavefront.  The matrix instructions cut off below: their sums are a little too low, whatever
 // the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E: a 4K frame's ddict
 // is off by 4.9e-7 of its norm, 1.4e-6 before.
@@ -66,6 +68,7 @@ struct GradCfg {
     static constexpr bool DL = K == 7 && LP > 80 && !SPLIT;                            // D's operands in LDS, not in 128 registers
     // Two fp16 numbers hold 2^14 .. 2^15 down to 2^-25: a number that is less than this many powers of two below keeps fp32's half step.
     static constexpr int STEP = 16;
+    static constexpr int VSTEP = 28;               // ... of a value, whose low part is kept 2^11 higher
     static constexpr bool ACC = !SPLIT;            // G is summed by the matrix instructions, under one power of two
     static constexpr int WPE = K == 7 || LP > 80 || SPLIT ? 1 : 2;                     // wavefronts per SIMD (registers, LDS)
     static_assert(LP * 16 * 4 <= ER_B && CM * MAXLRY * MAXLRX <= UN && VN * 4 <= ER_B && MAXLRX <= 64 && 3 * UW <= 256, "stage 1 fits where it goes");
@@ -113,6 +116,15 @@ __device__ __forceinline__ void split_pair(float x, float y, float sc, unsigned&
     const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf(x, sc, -(float)h[0]), fmaf(y, sc, -(float)h[1]));
     __builtin_memcpy(&hi, &h, 4);
     __builtin_memcpy(&lo, &l, 4);
+}
+
+// x, times sc into fp16's range -> a word: the high part, and the low part times 2^11, which has the same exponents
+__device__ __forceinline__ unsigned split_value(float x, float sc) {
+    const auto h = __builtin_amdgcn_cvt_pkrtz(x * sc, 0.0f);
+    const auto both = __builtin_amdgcn_cvt_pkrtz(x * sc, fmaf(x, sc, -(float)h[0]) * 2048.0f);
+    unsigned u;
+    __builtin_memcpy(&u, &both, 4);
+    return u;
 }
 
 // A stored value's bits, and the value
@@ -441,7 +453,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
                 }
                 float vback = 1.0f;
                 int below[2];
-                unsigned val[2][TQ], vlo[2][F::SPLIT ? TQ : 1];
+                int vx = 0, behind = 0;                  // the values' power of two; is there one whole steps below it?
+                unsigned val[2][TQ];
                 if (F::SPLIT) {
                     float m = 0.0f;
 #pragma unroll
@@ -450,13 +463,17 @@ void k_list_grad_mfma(const ListGradArgs a) {
                         for (int r = 0; r < TQ; ++r)
                             if (4 * r + q < a.T) m = fmaxf(m, fabsf(__uint_as_float(f.val[g][r])));
                     m = rows_max(__int_as_float(row_max(__float_as_int(m))));
-                    const int vx = exponent_field(m);
-                    const float vsc = pow2_field(268 - vx);
+                    vx = exponent_field(m);
+                    const float vsc = pow2_field(268 - vx), least = pow2_field(vx - F::VSTEP + 1);
                     vback = pow2_field(vx - 14);
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) split_pair(__uint_as_float(f.val[g][r]), 0.0f, vsc, val[g][r], vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0]);
+                        for (int r = 0; r < TQ; ++r) {
+                            const float v = __uint_as_float(f.val[g][r]);
+                            behind |= fabsf(v) < least && v != 0.0f;
+                            val[g][r] = split_value(v, vsc);
+                        }
                 }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
@@ -509,10 +526,16 @@ void k_list_grad_mfma(const ListGradArgs a) {
                             put[g][r] = mine ? cur[g][r] : aside;
                             cur[g][r] = mine ? aside : cur[g][r];
                             *(lds_h*)(phi + put[g][r]) = (unsigned short)val[g][r];
-                            if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = (unsigned short)vlo[F::SPLIT ? g : 0][F::SPLIT ? r : 0];
+                            if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + put[g][r]) = (unsigned short)(val[g][r] >> 16);
                         }
                     wave_lds_fence();
                 };
+                // how far an entry is behind: its pixel's E, its value
+                auto value_steps = [&](int g, int r) -> int {
+                    const float v = fabsf(__uint_as_float(f.val[g][r]));
+                    return F::SPLIT && v != 0.0f && 4 * r + q < a.T ? (vx - exponent_field(v)) / F::VSTEP * F::VSTEP : 0;
+                };
+                auto steps = [&](int g, int r) -> int { return below[g] + value_steps(g, r); };
                 auto left = [&]() -> bool {
                     bool more = false;
 #pragma unroll
@@ -536,17 +559,18 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     return __builtin_bit_cast(half8, *(const lds_u4*)(phi + 2 * ((part * F::PHI_ROWS + 16 * mt + n) * F::PP + 8 * q)));
                 };
                 auto product = [&](half8 p0, half8 p1, half8 high, half8 low, float4v r) -> float4v {
-                    if (F::SPLIT) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, high, r, 0, 0, 0);
+                    // (values' low parts are 2^11 higher than they are; of E, beside those, what is left 2^11 lower is enough)
+                    if (F::SPLIT) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, high * (_Float16)0x1p-11f, r, 0, 0, 0);
                     r = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, low, r, 0, 0, 0);
                     return __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, high, r, 0, 0, 0);
                 };
                 scatter();
-                if (__any(below[0] | below[1])) {                // pixels below the others: not yet
+                if (__any(below[0] | below[1] | behind)) {       // what is below the rest: not yet
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) {
-                            const int aside = 2 * (LP * F::PP + 16 * g + n), out = below[g] ? put[g][r] : aside;
+                            const int aside = 2 * (LP * F::PP + 16 * g + n), out = steps(g, r) ? put[g][r] : aside;
                             *(lds_h*)(phi + out) = 0;
                             if (F::SPLIT) *(lds_h*)(phi + F::PHI_ROWS * F::PP * 2 + out) = 0;
                             cur[g][r] = out != aside ? out : cur[g][r];
@@ -567,26 +591,31 @@ void k_list_grad_mfma(const ListGradArgs a) {
                     }
                 }
                 clear();
-                // What is left, if anything: pixels below the others, the nearest ones first, and atoms listed twice.  Every turn adds an entry: of
+                // What is left, if anything: what is below the rest, the nearest first, and atoms listed twice.  Every turn adds an entry: of
                 // those that it is for all write their numbers, and one of each place finds its own.
                 while (more) {
                     int less = 1 << 20;
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
-                        for (int r = 0; r < TQ; ++r) less = cur[g][r] != 2 * (LP * F::PP + 16 * g + n) ? min(less, below[g]) : less;
+                        for (int r = 0; r < TQ; ++r) less = cur[g][r] != 2 * (LP * F::PP + 16 * g + n) ? min(less, steps(g, r)) : less;
                     less = wave_min(less);
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int r = 0; r < TQ; ++r)
-                            *(lds_h*)(phi + (below[g] == less ? cur[g][r] : 2 * (LP * F::PP + 16 * g + n))) = (unsigned short)(4 * r + q + 1);
+                            *(lds_h*)(phi + (steps(g, r) == less ? cur[g][r] : 2 * (LP * F::PP + 16 * g + n))) = (unsigned short)(4 * r + q + 1);
                     wave_lds_fence();
 #pragma unroll
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int r = 0; r < TQ; ++r) seen[g][r] = *(lds_h*)(phi + cur[g][r]);
                     wave_lds_fence();
+                    if (F::SPLIT)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+#pragma unroll
+                            for (int r = 0; r < TQ; ++r) val[g][r] = split_value(__uint_as_float(f.val[g][r]), pow2_field(268 - vx + value_steps(g, r)));
                     scatter();
                     more = left();
                     asm volatile("" : "+v"(column));         // (hidden: E is read again; kept, it would take registers of every unit)

@@ -78,3 +78,25 @@ def test_quiet_pixels_that_list_an_atom_twice(oracle, vd):
         d["index"][:, 3] = d["index"][:, 0]
         d["index"][:, 5, ::2] = d["index"][:, 0, ::2]
     check(oracle, 1, 3, 20, 50, 2, 72, 5, 8, vd, "f32", seed=43, spoil=spoil)
+
+
+@pytest.mark.parametrize("quiet", [False, True])
+@pytest.mark.parametrize("C,k,L,T", [(3, 5, 72, 8), (1, 3, 80, 16), (3, 7, 128, 8)])
+def test_small_values_beside_large_ones(oracle, C, k, L, T, quiet):
+    """A steep softmax's list: each place holds a small part of the place before, and has atoms of its own."""
+    def spoil(d):
+        d["value"] = d["value"].abs() + 0.1
+        d["value"] *= 2.0 ** -(90.0 * torch.arange(T) / (T - 1)).view(1, T, 1, 1)
+        apart(d, T, torch.arange(T).view(T, 1, 1))
+        if quiet:
+            d["dout"][..., 3::5] *= 2.0 ** -20
+            d["dout"][..., 4::32] = 0
+    check(oracle, 1, C, 20, 50, 2, L, k, T, "f32", "f32", seed=47, spoil=spoil)
+
+
+def test_an_atom_listed_twice_with_values_of_very_different_sizes(oracle):
+    def spoil(d):
+        d["index"][:, 4:] = d["index"][:, :4]
+        d["value"][:, 4:] *= 2.0 ** -50
+        d["value"][:, 2:4] = 0
+    check(oracle, 1, 3, 20, 50, 2, 72, 5, 8, "f32", "f32", seed=53, spoil=spoil)
