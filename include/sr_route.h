@@ -122,8 +122,8 @@ size_t sr_dict_assemble_list_grad_workspace_bytes(int L, int k);
  *
  * index: atoms below L (others count as atom L - 1); an atom that is listed twice gets both terms.  Finite values only: infinities and NaN in
  * dict, lr, dout or value give unspecified results.  Arithmetic is fp32 or equivalent (fp16 matrix-core products of operands split
- * in two); ddict is summed in fp32 over runs of at most 4096 pixels and in double from there on, and what a pixel whose E is
- * below 2^-100 of the largest in its run adds to it may be lost.
+ * in two, which hold all but 2^-23 of a pixel's largest E, an atom's largest tap and a value); ddict is summed in fp32 over runs of at
+ * most 4096 pixels and in double from there on, and what a pixel whose E is below 2^-100 of the largest in its run adds to it may be lost.
  * An empty call writes zeros to ddict.
  */
 int sr_dict_assemble_list_grad(const sr_tensor* lr, const sr_tensor* index, const sr_tensor* value, const sr_tensor* dict,

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2303_08999_amd as sr
-from test_gpu_list_grad import DEV, U, check
+from test_gpu_list_grad import DEV, U, check, run
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,35 @@ def test_an_atom_listed_twice_with_values_of_very_different_sizes(oracle):
         d["value"][:, 4:] *= 2.0 ** -50
         d["value"][:, 2:4] = 0
     check(oracle, 1, 3, 20, 50, 2, 72, 5, 8, "f32", "f32", seed=53, spoil=spoil)
+
+
+@pytest.mark.parametrize("k", [3, 5, 7])
+def test_products_of_two_numbers(k):
+    """An image of ones (E = dout in every place), atoms of one tap, atoms named once: every result is one product.  Of either operand
+    two fp16 numbers hold all but 2^-23, 2 u; the product of the low parts, 2^-11 each, may be left out: 4 u; a matrix instruction's sum
+    rounds by 2 u at most, of which the last is all that counts: 10 u.  With fp32 values ddict has the same, E beside the low part
+    of a value, 2^-11, within 2^-13: 1 u, and a rounding at the end: 12 u.  fp16 values are whole: 5 u."""
+    L, h, w, T = 128, 16, 40, 2
+    H, W = 2 * h, 2 * w
+    for seed in range(4):
+        g = torch.Generator().manual_seed(70 + seed)
+        sign = lambda shape: torch.randint(0, 2, shape, generator=g) * 2 - 1
+        D = torch.zeros((L, k * k))
+        D[torch.arange(L), torch.arange(L) * 7 % (k * k)] = (1 + torch.rand(L, generator=g)) * sign((L,))
+        index = ((torch.arange(H * W) * 5).view(1, 1, H, W) + torch.arange(T).view(1, T, 1, 1) * 64) % L
+        d = {"lr": torch.ones((1, 1, h, w)), "index": index.to(torch.uint8), "dict": D.view(L, k, k),
+             "dout": (1 + torch.rand((1, 1, H, W), generator=g)) * sign((1, 1, H, W))}
+        for vd in ("f32", "f16"):
+            value = ((1 + torch.rand((1, T, H, W), generator=g)) * sign((1, T, H, W)))
+            once = torch.zeros((1, T, H, W))
+            once.view(T, -1)[0, torch.arange(L) * 13 + seed] = 1       # 13 is prime to L: one pixel for every atom
+            d["value"] = (value * once).to(torch.float16 if vd == "f16" else torch.float32)
+            dv, dd = run(d, 2)
+            tap = D.sum(1).double()[index]
+            want = tap * d["dout"].double()
+            if vd == "f32":
+                assert float(((dv.double() - want).abs() / want.abs()).max()) <= 10 * U
+            want = torch.zeros(L, dtype=torch.float64).scatter_add_(0, index.reshape(-1), (d["value"].double() * d["dout"].double()).reshape(-1))
+            assert (want != 0).all()
+            err = (dd.double().view(L, -1) - want.view(L, 1)).abs() / want.abs().view(L, 1)
+            assert float(err.max()) <= (12 if vd == "f32" else 5) * U, vd
