@@ -24,6 +24,12 @@
 // the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E: a 4K frame's ddict
 // is off by 4.9e-7 of its norm, 1.4e-6 before.
 //
+// Loops: all lanes of a wavefront take the same number of turns, with what is beyond the end done twice or set aside, and nothing that
+// differs between lanes is kept in a register across a loop that some lanes leave early.  This is for safety, not for speed: where this
+// kernel's registers run out the compiler (ROCm 7.2) copies values to accumulation registers, and it has put such copies at the exit of a
+// loop that lanes left one by one, before it switched the lanes on again.  Nothing was copied, and what was read back as an address later
+// was not one: a memory fault, with more than 80 atoms.
+//
 // What bounds it: none of memory (438 MB of a 4K frame of 8 entries, 89 us), vector ALU (180 us), LDS (196 us, of which 54 bank conflicts of the
 // gather and the scatter, whose rows are the lists') and matrix cores (84 us) alone: 415 us with 2 wavefronts per SIMD, whose registers
 // (227) and LDS (81 KB a workgroup) leave no room for a third.  A unit's chain through LDS and the matrix cores is four round trips
@@ -166,7 +172,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
 
     // ---- the dictionary as operands of R: lane (q, n) has atom 16 mt + n, taps 32 s + 8 q and on, the atom times a power of two (to
     // 2^14 .. 2^15)
-    for (int e = lane; e < F::PHI_B / 16; e += 64) ((lds_u4*)phi)[e] = (u32x4v){0, 0, 0, 0};
+    for (int e = 0; e < F::PHI_B / 16; e += 64) ((lds_u4*)phi)[min(e + lane, F::PHI_B / 16 - 1)] = (u32x4v){0, 0, 0, 0};
     u32x4v Dh[F::DL ? 1 : MT][NS], Dl[F::DL ? 1 : MT][NS];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -278,7 +284,7 @@ void k_list_grad_mfma(const ListGradArgs a) {
         const Tile tl = tn;
         const bool last = tile + gridDim.x >= tiles;
         if (!last) tn = tile_at(tile + gridDim.x);
-        // ---- stage 1 of all channels, the values of sr_device.h; every loop has the same number of turns for all lanes.  LR rows and rows
+        // ---- stage 1 of all channels, the values of sr_device.h; every loop has the same number of turns for all lanes (see Loops above).  LR rows and rows
         // after the vertical pass are a wavefront's each, columns of the tile a thread's, whose weights stay in registers.
         const TileOrigin o = tile_origin(tl.Y0, tl.X0, R, UH, UW, a.H, a.W, a.s);
         __syncthreads();                             // the last tile has been used

@@ -270,7 +270,9 @@ __device__ __forceinline__ void load_chunks(Chunk<TZ, VEC> (&z)[NC], const LaneA
         const int last = (L - 1) / (8 * G);          // the last chunk that any lane has atoms in
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            // the lane's plane of the chunk, or the last atom's; from there on as long as there are atoms
+            // the lane's plane of the chunk, or the last atom's; from there on as long as there are atoms.  Offsets have 32 bits and no
+            // sign: they start at a plane that is there, at or after the chunk's first (which `at` points to), and only grow.  Taken back from beyond
+            // the last atom to before that plane, one would stand for 4 GB more: a memory fault.
             const int l = (min(c, last) * G + p.g) * 8;
             unsigned off = p.off - (unsigned)max(l - (L - 1), 0) * (unsigned)stride;
 #pragma unroll
