@@ -365,22 +365,27 @@ hipError_t launch_route_grad(const RouteArgs& a, sr_dtype z, sr_dtype v, int gri
 // pixels; they meet (72 to 256 atoms, fp32 and bfloat16, us a wavefront / lanes): lists 4096 pixels 9.1 / 9.5 and 9.2 / 12.1; with the
 // losses 1024 pixels 17.2 / 21.0, 2048 pixels 21.9 / 21.1 and 43 / 26; gradient 4096 pixels 8.7 / 8.5, 256 atoms 8192 pixels 12.9 / 12.7
 // and 13.1 / 19.6.  Lists come from the same kernel with and without the losses, so that both calls give the same bits: 2048 pixels costs
-// the lists 2.5 us there and spares the losses 17.  Rows of up to 72 atoms, eight of them a load: one token 5.3 / 4.6, losses 10.9 / 11.6.
-int64_t lanes_from(const RouteArgs& r, bool gradient) {
+// the lists 2.5 us there and spares the losses 17.
+// Rows of up to 72 atoms that are aligned 16-byte pieces, eight atoms or four a load, bfloat16, 1 and 1024 of them: 72 atoms 5.3 / 4.6 and
+// 6.3 / 4.8, losses 10.6 / 11.8 and 15.6 / 16.2; 8 atoms 5.2 / 3.9 and 6.2 / 4.1, losses 13.0 / 12.2 and 17.8 / 13.9 (fp32 rows of 8 to 64 alike;
+// of 72, 5.3 / 7.1 and 6.3 / 7.4).  Rows off those pieces, an atom a load, 1024 of them, fp32: 8 atoms 6.2 / 8.1, losses 17.8 / 19.9; 72 atoms
+// 6.3 / 8.6 and 15.6 / 20.8: as planes.
+int64_t lanes_from(const RouteArgs& r, bool vec, bool gradient) {
     if (gradient) return r.L > 128 ? 8192 : 4096;
-    return r.layout == SR_COEFF_PIXEL_MAJOR && r.L <= 8 * LCH && r.L % 8 == 0 ? 1 : 2048;
+    return vec && r.L <= 8 * LCH ? 1 : 2048;
 }
 int lanes_of(LaneArgs& a, const RouteArgs& r, sr_dtype z, sr_dtype v, const void* dz, bool gradient) {
     const bool pm = r.layout == SR_COEFF_PIXEL_MAJOR, pre = r.layout == SR_COEFF_PRE_SHUFFLE;
     const int64_t es = (int64_t)route_esize(z);
     const int G = pm || r.L > 8 * LCH ? 4 : 1;
-    if (r.T > 16 || r.total < lanes_from(r, gradient)) return 0;
+    const bool vec = pm && r.L % 8 == 0 && (uintptr_t)r.z % 16 == 0 && (uintptr_t)dz % 16 == 0;
+    if (r.T > 16 || r.total < lanes_from(r, vec, gradient)) return 0;
     if (G > 1 && 32 * r.lstride * es >= (int64_t)1 << 32) return 0;
     a.r = r;
     a.ipx = pre ? (int64_t)r.h * r.w : r.px;
     a.tiles_per_image = (a.ipx + 64 / G - 1) / (64 / G);
     a.tiles = r.total / a.ipx * a.tiles_per_image;
-    a.vec = pm && r.L % 8 == 0 && (uintptr_t)r.z % 16 == 0 && (uintptr_t)dz % 16 == 0;
+    a.vec = vec;
     a.half_value = v == SR_F16;
     return G;
 }
