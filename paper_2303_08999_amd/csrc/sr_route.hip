@@ -134,9 +134,12 @@ __global__ __launch_bounds__(RNT) void k_route_wave(const RouteArgs a) {
     if (threadIdx.x == 0) *r.squares = sh_sq, *r.live = sh_live;
 }
 
-// The workgroups' sums, and the losses from them: one workgroup, a fixed order.  Latencies are what it takes: a thread has up to AHEAD
-// records' loads under way at a time, all of its records of a call of 72 atoms and 256 records (7.7 us; eight at a time 9.4).
+// The workgroups' sums, and the losses from them: one workgroup, a fixed order.  Latencies are what it takes: a thread has AHEAD records'
+// loads under way at a time, at most 20 (registers: two 64-bit words each, 16 wavefronts on a CU).  launch_finish shares a thread's records
+// out evenly over as few rounds as that leaves.  (131 072 fp16 pixels, the whole call, us, with 8, with 19 whatever the call, so: 16 atoms 16.6, 17.4,
+// 16.0; 40 atoms 20.1, 20.3, 19.4; 72 atoms 22.9, 21.7, 22.1; 128 atoms 36.7, 38.3, 37.0; 256 atoms 61.5, 64.6, 62.2.)
 constexpr int FNT = 1024;
+template <int AHEAD>
 __global__ __launch_bounds__(FNT) void k_route_finish(const void* partial, int records, int L, int T,
                                                       long long* counts, float* share, float* loss) {
     __shared__ double sh_s[FNT];
@@ -144,7 +147,6 @@ __global__ __launch_bounds__(FNT) void k_route_finish(const void* partial, int r
     __shared__ double sh_sq[FNT / 64], sh_f[SR_MAX_ATOMS / 64];
     __shared__ unsigned long long sh_m[FNT / 64];
     const int tid = threadIdx.x, groups = FNT / L, g = tid / L, l = tid - g * L;
-    constexpr int AHEAD = 19;
     double q = 0.0;
     unsigned long long m = 0;
     static_assert(ROUTE_RECORDS <= FNT, "a record a thread");
@@ -278,6 +280,16 @@ __global__ __launch_bounds__(RNT) void k_route_grad_wave(const RouteArgs a) {
     }
 }
 
+void launch_finish(const void* partial, int records, int L, int T, long long* counts, float* share, float* loss, hipStream_t st) {
+    const int groups = FNT / L, each = (records + groups - 1) / groups, rounds = (each + 19) / 20, ahead = rounds ? (each + rounds - 1) / rounds : 0;
+    auto go = [&](auto n) { k_route_finish<decltype(n)::value><<<1, FNT, 0, st>>>(partial, records, L, T, counts, share, loss); };
+    if (ahead <= 4) go(std::integral_constant<int, 4>{});
+    else if (ahead <= 8) go(std::integral_constant<int, 8>{});
+    else if (ahead <= 12) go(std::integral_constant<int, 12>{});
+    else if (ahead <= 16) go(std::integral_constant<int, 16>{});
+    else go(std::integral_constant<int, 20>{});
+}
+
 size_t route_esize(sr_dtype d) { return d == SR_F32 ? 4 : (d == SR_U8 ? 1 : 2); }
 
 bool route_overlap(const void* p, size_t np, const void* q, size_t nq) {
@@ -367,8 +379,8 @@ hipError_t launch_route_grad(const RouteArgs& a, sr_dtype z, sr_dtype v, int gri
 // and 13.1 / 19.6.  Lists come from the same kernel with and without the losses, so that both calls give the same bits: 2048 pixels costs
 // the lists 2.5 us there and spares the losses 17.
 // Rows of up to 72 atoms that are aligned 16-byte pieces, eight atoms or four a load, bfloat16, 1 and 1024 of them: 72 atoms 5.3 / 4.6 and
-// 6.3 / 4.8, losses 10.6 / 11.8 and 15.6 / 16.2; 8 atoms 5.2 / 3.9 and 6.2 / 4.1, losses 13.0 / 12.2 and 17.8 / 13.9 (fp32 rows of 8 to 64 alike;
-// of 72, 5.3 / 7.1 and 6.3 / 7.4).  Rows off those pieces, an atom a load, 1024 of them, fp32: 8 atoms 6.2 / 8.1, losses 17.8 / 19.9; 72 atoms
+// 6.3 / 4.8, losses 10.6 / 11.8 and 15.6 / 16.2; 8 atoms 5.2 / 3.9 and 6.2 / 4.1, losses 13.0 / 12.2 and 17.8 / 13.9 (fp32 rows of 8 to 64,
+// 5.3 / 5.3 and 6.2 / 5.7; of 72, 5.3 / 7.1 and 6.3 / 7.4).  Rows off those pieces, an atom a load, 1024 of them, fp32: 8 atoms 6.2 / 8.1, losses 17.8 / 19.9; 72 atoms
 // 6.3 / 8.6 and 15.6 / 20.8: as planes.
 int64_t lanes_from(const RouteArgs& r, bool vec, bool gradient) {
     if (gradient) return r.L > 128 ? 8192 : 4096;
@@ -466,7 +478,7 @@ int sr_list_route_balance(const sr_tensor* coeff, int L, int scale, int entries,
               : launch_route<true>(a, coeff->dtype, value->dtype, a.records, (hipStream_t)stream);
     }
     if (e == hipSuccess) {
-        k_route_finish<<<1, FNT, 0, (hipStream_t)stream>>>(workspace, empty ? 0 : a.records, L, entries, counts, share, loss);
+        launch_finish(workspace, empty ? 0 : a.records, L, entries, counts, share, loss, (hipStream_t)stream);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
