@@ -14,7 +14,7 @@
  * A logit of -infinity masks its atom: p_l = 0, and the atom is listed only where fewer than
  * `entries` others are there, with the value 0.  A pixel with no other logit has values 0 and the
  * atoms 0, 1, ...; it takes no part in counts, shares and losses, and its gradient is 0.
- * -0 and +0 are equal.  NaN or +infinity logits give unspecified values (and, through the sums,
+ * -0 and +0 are equal, and either may be listed for the other.  NaN or +infinity logits give unspecified values (and, through the sums,
  * shares and losses), but always different atoms below L.
  *
  * All rules of sr_dict.h hold: device memory of the caller, every check on the host before

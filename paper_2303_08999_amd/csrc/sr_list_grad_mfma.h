@@ -14,15 +14,15 @@
 // summed in fp32 8.6e-8).  For G the pixels of a unit share
 // the largest one's power of two (or up to four times that); those that are 2^16 and more below it, whose lower parts fp16 would cut
 // off, take it less whole steps of 2^16 and are added after the others, in a product of their own for each distance: an atom that quiet
-// pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16: 421 us, 417 without it;
-// 730 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom listed twice, which
+// pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16: 422 us, 417 without it;
+// 750 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom listed twice, which
 // goes the same way: what the frequent case takes of registers went first.)  fp16 values enter as they are and
 // the sums stay in the matrix instructions; fp32 ones are split as well, the low part kept 2^11
 // higher, under one power of two: those that are 2^28 and more below the largest wait likewise (softmax lists of logits of deviation 8, where
-// most units have such a value: a 4K frame 804 -> 1520 us); a unit's sums are added unscaled.  Both are fp32, and
+// most units have such a value: a 4K frame 814 -> 1540 us); a unit's sums are added unscaled.  Both are fp32, and
 // handed on in double after at most 4096 pixels of a wavefront.  The matrix instructions cut off below: their sums are a little too low, whatever
 // the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E: a 4K frame's ddict
-// is off by 4.9e-7 of its norm, 1.4e-6 before.
+// is off by 4.3e-7 to 5.3e-7 of its norm, 1.4e-6 without.
 //
 // Loops: all lanes of a wavefront take the same number of turns, with what is beyond the end done twice or set aside, and nothing that
 // differs between lanes is kept in a register across a loop that some lanes leave early.  This is for safety, not for speed: where this
@@ -30,10 +30,11 @@
 // loop that lanes left one by one, before it switched the lanes on again.  Nothing was copied, and what was read back as an address later
 // was not one: a memory fault, with more than 80 atoms.
 //
-// What bounds it: none of memory (438 MB of a 4K frame of 8 entries, 89 us), vector ALU (180 us), LDS (196 us, of which 54 bank conflicts of the
-// gather and the scatter, whose rows are the lists') and matrix cores (84 us) alone: 415 us with 2 wavefronts per SIMD, whose registers
-// (227) and LDS (81 KB a workgroup) leave no room for a third.  A unit's chain through LDS and the matrix cores is four round trips
-// long.  7x7 atoms of 65 to 128: one wavefront per SIMD, half a megapixel of 16 entries 524 us.
+// What bounds it: none of memory (438 MB of a 4K frame of 8 entries, 89 us), vector ALU (188 us), LDS (204 us, of which 58 bank conflicts of the
+// gather and the scatter, whose rows are the lists') and matrix cores (84 us) alone: 422 us with 2 wavefronts per SIMD, whose registers
+// (235) and LDS (81 KB a workgroup) leave no room for a third.  A unit's chain through LDS and the matrix cores is four round trips
+// long.  One wavefront per SIMD where the registers end: 7x7 atoms, more than 80 atoms, fp32 values (a
+// 1080p frame of 16 entries of 128 atoms of 7x7 484 us; 8 entries of 72 in fp32 227 us, in fp16 129).
 #pragma once
 #include "sr_list_grad.h"
 

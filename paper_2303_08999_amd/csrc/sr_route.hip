@@ -1,7 +1,9 @@
 // The router: per-pixel lists from logits, the atoms' load and losses, and the gradient (include/sr_route.h).
 //
 // Here: checks, and the kernels that take every case, a wavefront for a pixel: a lane holds every 64th atom, the largest is
-// found `entries` times over by a reduction of 64-bit keys (order of the logit, then the lower atom).
+// found `entries` times over by a reduction of 64-bit keys (order of the logit, then the lower atom): fast for few pixels (lanes_from), and
+// what is there for lists of more than 16 entries: a 1080p frame of 72 fp16 logits 5.5 ms for 17 entries (16 entries on the lanes 0.13),
+// with the losses 6.0 (0.19), gradient 5.6 (0.19).
 #include <stdint.h>
 
 #include "sr_route_lanes.h"

@@ -313,7 +313,7 @@ template <int G> __device__ __forceinline__ float lanes_max(float v, int step) {
 }
 
 // What bounds it: with 72 fp16 logits a 4K frame moves 1.39 GB, 284 us at a large copy's 4.9 TB/s, and takes 1323 vector instructions a
-// wavefront of 64 pixels (8 medians a logit; 279 us if nothing else ran): 322 us.  A median per place of the list is what one lane can do a key in;
+// wavefront of 64 pixels (8 medians a logit; 279 us if nothing else ran): 314 to 330 us.  A median per place of the list is what one lane can do a key in;
 // lists kept apart by wavefront (k_route_wave) take a reduction over 64 lanes per entry.
 // The losses keep every atom's share in a register as well, 2 wavefronts per SIMD instead of 4: 2.1 Mpixel of bfloat16 logits 102 us and 8 for the
 // last sum, of 66 us that its bytes take.
