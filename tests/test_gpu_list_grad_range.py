@@ -132,3 +132,29 @@ def test_products_of_two_numbers(k):
             assert (want != 0).all()
             err = (dd.double().view(L, -1) - want.view(L, 1)).abs() / want.abs().view(L, 1)
             assert float(err.max()) <= (12 if vd == "f32" else 5) * U, vd
+
+
+@pytest.mark.parametrize("C,k,L,T,vd", [(3, 5, 72, 8, "f16"), (1, 3, 40, 16, "f32"), (3, 7, 128, 16, "f16"), (1, 7, 90, 5, "f32")])
+def test_one_atom_in_every_place_of_a_list(oracle, C, k, L, T, vd):
+    """Some pixels list one atom alone, some two in turn; quiet pixels, pixels of zeros and padding among them."""
+    def spoil(d):
+        d["index"][:] = torch.where(torch.arange(d["index"].shape[3]) % 3 == 0, d["index"][:, :1], d["index"])
+        d["index"][:, 2::2, ::3] = d["index"][:, :1, ::3]
+        d["dout"][..., 4::32] *= 2.0 ** -30
+        d["dout"][..., 9::32] = 0
+    check(oracle, 1, C, 20, 50, 2, L, k, T, vd, "f32", True, seed=59, spoil=spoil)
+
+
+@pytest.mark.parametrize("C,k,L,T", [(3, 5, 72, 8), (1, 3, 40, 4), (3, 7, 128, 16)])
+def test_small_fp16_values_beside_large_ones(oracle, C, k, L, T):
+    """Down to fp16's subnormal numbers, which are taken as they are: each place of a list has atoms of its own."""
+    def spoil(d):
+        d["value"] = ((d["value"].float().abs() + 0.1) * 2.0 ** -(22.0 * torch.arange(T) / (T - 1)).view(1, T, 1, 1)).half()
+        apart(d, T, torch.arange(T).view(T, 1, 1))
+    check(oracle, 1, C, 20, 50, 2, L, k, T, "f16", "f32", seed=61, spoil=spoil)
+
+
+@pytest.mark.parametrize("k,vd", [(3, "f32"), (5, "f16"), (5, "f32"), (7, "f32")])
+def test_gradients_near_the_bottom_of_the_type(oracle, k, vd):
+    """An image's gradient of 2^-118: results keep their bits down to where fp32 ends (fp16 values: dvalue is 0, ddict is not)."""
+    check(oracle, 1, 3, 10, 33, 2, 72, k, 8, vd, "f32", seed=67, gain=2.0 ** -118)
