@@ -21,8 +21,8 @@
 // higher, under one power of two: those that are 2^28 and more below the largest wait likewise (softmax lists of logits of deviation 8, where
 // most units have such a value: a 4K frame 814 -> 1540 us); a unit's sums are added unscaled.  Both are fp32, and
 // handed on in double after at most 4096 pixels of a wavefront.  The matrix instructions cut off below: their sums are a little too low, whatever
-// the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E: a 4K frame's ddict
-// is off by 4.3e-7 to 5.3e-7 of its norm, 1.4e-6 without.
+// the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E, in a workgroup and from one workgroup to
+// the next (in images of two rows a tile has one wavefront's work; without it fp32 values' ddict is off by 2.2e-6 there): a 4K frame's ddict is off by 4.3e-7 to 5.3e-7 of its norm, 1.4e-6 without.
 //
 // Loops: all lanes of a wavefront take the same number of turns, with what is beyond the end done twice or set aside, and nothing that
 // differs between lanes is kept in a register across a loop that some lanes leave early.  This is for safety, not for speed: where this
@@ -219,7 +219,8 @@ void k_list_grad_mfma(const ListGradArgs a) {
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int t = 0; t < NT; ++t) G[mt][t] = (float4v){0, 0, 0, 0};
-    const float turn = wave & 1 ? -1.0f : 1.0f;      // odd wavefronts sum -E
+    // every other wavefront sums -E, of its workgroup and of those that are at the same rows of the tiles
+    const float turn = (wave ^ blockIdx.x) & 1 ? -1.0f : 1.0f;
     double* const rec = a.partial ? a.partial + (size_t)blockIdx.x * a.L * KK : nullptr;
     bool first = true;
     int held = 0, scale = 15, top = 15;              // G times 2^(scale - 14) is the sum (ACC); the largest scale that this G has had

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2303_08999_amd as sr
-from test_gpu_list_grad import DEV, U, check, run
+from test_gpu_list_grad import DEV, DT, U, check, run
 
 pytestmark = pytest.mark.gpu
 
@@ -158,3 +158,24 @@ def test_small_fp16_values_beside_large_ones(oracle, C, k, L, T):
 def test_gradients_near_the_bottom_of_the_type(oracle, k, vd):
     """An image's gradient of 2^-118: results keep their bits down to where fp32 ends (fp16 values: dvalue is 0, ddict is not)."""
     check(oracle, 1, 3, 10, 33, 2, 72, k, 8, vd, "f32", seed=67, gain=2.0 ** -118)
+
+
+@pytest.mark.parametrize("n,w,k,T,vd", [(1, 450000, 3, 3, "f32"), (1, 450000, 5, 8, "f16"), (400, 600, 5, 8, "f16")])
+def test_errors_do_not_add_up_in_images_of_two_rows(oracle, n, w, k, T, vd):
+    """As test_errors_do_not_add_up_where_the_gradients_cancel has it, 900 000 pixels and 4 x 2^-22 of the norm, but of a tile's rows two
+    are there, one wavefront's."""
+    C, s, L, H, W = 1, 2, 72, 2, 2 * w
+    g = torch.Generator(device=DEV).manual_seed(1)
+    value, index = torch.rand((n, L, H, W), device=DEV, generator=g).topk(T, dim=1)
+    value = (value / value.sum(1, keepdim=True)).to(DT[vd])
+    lr, D = torch.rand((n, C, 1, w), device=DEV, generator=g), torch.randn((L, k, k), device=DEV, generator=g) / k
+    dout = torch.randn((n, C, H, W), device=DEV, generator=g) / 64
+    dd = torch.empty_like(D)
+    sr.sr_dict_assemble_list_grad(lr, index.to(torch.uint8), value, D, L, k, s, C, T, None, dout, None, dd)
+    r = k // 2
+    pad = torch.nn.functional.pad(torch.from_numpy(oracle.bicubic(lr.cpu().numpy(), s)).to(DEV).double(), (r, r, r, r), mode="replicate")
+    E = torch.stack([(pad[:, :, i // k:i // k + H, i % k:i % k + W] * dout.double()).sum(1) for i in range(k * k)], 0).reshape(k * k, -1)
+    phi = torch.zeros((L, n * H * W), device=DEV, dtype=torch.float64)
+    phi.scatter_add_(0, index.permute(1, 0, 2, 3).reshape(T, -1), value.double().permute(1, 0, 2, 3).reshape(T, -1))
+    want = phi @ E.t().contiguous()
+    assert float((dd.double().reshape(L, -1) - want).norm() / want.norm()) <= 4 * 2.0 ** -22
