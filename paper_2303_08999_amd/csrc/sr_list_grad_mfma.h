@@ -9,20 +9,21 @@
 // for its gather.  All of that is a wavefront's own scratch: no barrier but around the up-sampled tile.
 //
 // Precision: fp16 products with fp32 sums.  E is scaled pixel by pixel by a power of two (to 2^14 .. 2^15) and split in two fp16
-// numbers, each the nearest: 2^-23 is left.  D likewise, atom by atom; R takes three products, and leaves out the low parts' (2^-22 of a term
-// at most, 2^-24.6 as the operands fall: dvalue of a crop is off by 4.9e-8 of its norm, 4.7e-8 with the fourth, which takes a 4K frame 9 us;
-// summed in fp32 8.6e-8).  For G the pixels of a unit share
-// the largest one's power of two (or up to four times that); those that are 2^16 and more below it, whose lower parts fp16 would cut
-// off, take it less whole steps of 2^16 and are added after the others, in a product of their own for each distance: an atom that quiet
-// pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16: 422 us, 417 without it;
-// 750 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom listed twice, which
-// goes the same way: what the frequent case takes of registers went first.)  fp16 values enter as they are and
-// the sums stay in the matrix instructions; fp32 ones are split as well, the low part kept 2^11
-// higher, under one power of two: those that are 2^28 and more below the largest wait likewise (softmax lists of logits of deviation 8, where
-// most units have such a value: a 4K frame 814 -> 1540 us); a unit's sums are added unscaled.  Both are fp32, and
-// handed on in double after at most 4096 pixels of a wavefront.  The matrix instructions cut off below: their sums are a little too low, whatever
-// the sign, which adds up over a frame where the gradients cancel.  So every other wavefront sums -E, in a workgroup and from one workgroup to
-// the next (in images of two rows a tile has one wavefront's work; without it fp32 values' ddict is off by 2.2e-6 there): a 4K frame's ddict is off by 4.3e-7 to 5.3e-7 of its norm, 1.4e-6 without.
+// numbers, each the nearest: 2^-23 is left.  D likewise, atom by atom; R takes three products, and leaves out the low parts' (2^-22 of a
+// term at most, 2^-24.6 as the operands fall: dvalue of a crop is off by 4.9e-8 of its norm, 4.7e-8 with the fourth, which takes a 4K frame
+// 9 us; summed in fp32 8.6e-8).
+// For G the pixels of a unit share the largest one's power of two (or up to four times that).  Those that are 2^16 and more below it, whose
+// lower parts fp16 would cut off, take it less whole steps of 2^16 and are added after the others, in a product of their own for each
+// distance: an atom that quiet pixels alone name has its bits, down to 2^-100 of the run's largest E.  (4K frame of 8 entries of 72 in fp16:
+// 422 us, 417 without it; 750 where every unit has one such pixel, 1030 where it has two distances of them, 720 where every unit has an atom
+// listed twice, which goes the same way: what the frequent case takes of registers went first.)
+// fp16 values enter as they are and the sums stay in the matrix instructions.  fp32 ones are split as well, the low part kept 2^11 higher, under
+// one power of two: those that are 2^28 and more below the largest wait likewise (softmax lists of logits of deviation 8, where most units have
+// such a value: a 4K frame 814 -> 1540 us); a unit's sums are added unscaled.  Both are fp32, and handed on in double after at most 4096
+// pixels of a wavefront.
+// The matrix instructions cut off below: their sums are a little too low, whatever the sign, which adds up over a frame where the gradients
+// cancel.  So every other wavefront sums -E, in a workgroup and from one workgroup to the next (in images of two rows a tile has one
+// wavefront's work; without it fp32 values' ddict is off by 2.2e-6 of its norm there): a 4K frame's is off by 4.3e-7 to 5.3e-7, 1.4e-6 without.
 //
 // Loops: all lanes of a wavefront take the same number of turns, with what is beyond the end done twice or set aside, and nothing that
 // differs between lanes is kept in a register across a loop that some lanes leave early.  This is for safety, not for speed: where this
