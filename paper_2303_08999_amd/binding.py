@@ -19,14 +19,19 @@ SR_COEFF_PLANAR, SR_COEFF_PRE_SHUFFLE, SR_COEFF_PIXEL_MAJOR, SR_COEFF_BLOCKED = 
 SR_COEFF_VALUES, SR_COEFF_LOGITS = 0, 1
 SR_RUNS_NOTHING, SR_RUNS_GENERIC, SR_RUNS_STREAMING, SR_RUNS_SLOTS = 0, 1, 2, 3
 SR_ROUTE_SOFTMAX, SR_ROUTE_CHOSEN, SR_ROUTE_VALUES = 0, 1, 2
+SR_ACT_NONE, SR_ACT_RELU, SR_ACT_GELU, SR_ACT_SILU, SR_ACT_SIGMOID = 0, 1, 2, 3, 4
 SR_MAX_ATOMS = 256
+SR_MAX_FEATURES, SR_MAX_GRADS = 65536, 4096
 
 EXPORTS = ("sr_dict_assemble", "sr_dict_assemble_selective", "sr_dict_assemble_ex", "sr_dict_assemble_list", "sr_dict_assemble_list_ex",
            "sr_bicubic_upsample", "sr_dict_assemble_plan", "sr_dict_assemble_tile", "sr_dict_assemble_launch_shape", "sr_dict_assemble_walk", "sr_dict_assemble_runs", "sr_dict_assemble_list_walk", "sr_strerror", "sr_version",
            "sr_probe_read", "sr_probe_mix", "sr_probe_mix_tiled", "sr_probe_mix_tiled_bytes", "sr_probe_mix_tiled_paced", "sr_probe_stream", "sr_probe_pattern", "sr_probe_policy", "sr_probe_policy_bits",
            "sr_atom_gram_workspace_bytes", "sr_atom_gram", "sr_atom_gram_static", "sr_select_atoms",
            "sr_list_route", "sr_list_route_workspace_bytes", "sr_list_route_balance", "sr_list_route_grad",
-           "sr_dict_assemble_list_grad_workspace_bytes", "sr_dict_assemble_list_grad")
+           "sr_dict_assemble_list_grad_workspace_bytes", "sr_dict_assemble_list_grad",
+           "sr_layer_linear_workspace_bytes", "sr_layer_linear", "sr_layer_linear_grad_workspace_bytes", "sr_layer_linear_grad",
+           "sr_layer_gated_workspace_bytes", "sr_layer_gated", "sr_layer_gated_grad_workspace_bytes", "sr_layer_gated_grad",
+           "sr_grad_clip_workspace_bytes", "sr_grad_clip")
 
 
 class sr_tensor(ctypes.Structure):
@@ -100,6 +105,17 @@ def load():
     lib.sr_list_route_grad.argtypes = [T, T, T, i, i, i, i, i, T, vp, vp, T, vp]
     lib.sr_dict_assemble_list_grad_workspace_bytes.argtypes = [i, i]
     lib.sr_dict_assemble_list_grad.argtypes = [T, T, T, T, i, i, i, i, i, T, T, T, T, vp, sz, vp]
+    ll = ctypes.c_longlong
+    lib.sr_layer_linear_workspace_bytes.argtypes = [ll, i, i, i]
+    lib.sr_layer_linear.argtypes = [T, T, T, i, T, T, vp, sz, vp]
+    lib.sr_layer_linear_grad_workspace_bytes.argtypes = [ll, i, i, i, i]
+    lib.sr_layer_linear_grad.argtypes = [T, T, T, i, T, T, T, T, vp, sz, vp]
+    lib.sr_layer_gated_workspace_bytes.argtypes = [ll, i, i, i]
+    lib.sr_layer_gated.argtypes = [T, T, T, i, T, vp, sz, vp]
+    lib.sr_layer_gated_grad_workspace_bytes.argtypes = [ll, i, i, i]
+    lib.sr_layer_gated_grad.argtypes = [T, T, T, i, T, T, T, T, vp, sz, vp]
+    lib.sr_grad_clip_workspace_bytes.argtypes = [i]
+    lib.sr_grad_clip.argtypes = [T, T, i, ctypes.c_double, vp, vp, sz, vp]
     lib.sr_strerror.restype = ctypes.c_char_p
     lib.sr_version.argtypes = []
     for name in EXPORTS:
@@ -515,3 +531,173 @@ def sr_dict_assemble_list_grad(lr, index, value, dict, L, k, scale, channels, en
                                              0 if workspace is None else workspace.numel() * workspace.element_size(),
                                              _stream(stream)))
     return dvalue, ddict
+
+
+def _code(dtype):
+    if not _codes:
+        _bind_torch()
+    code = _codes.get(dtype)
+    if code is None:
+        raise TypeError(f"dtype {dtype} is not float32/float16/bfloat16")
+    return code
+
+
+def _rows(t) -> sr_tensor:
+    """Descriptor of rows of features: [N][H][W][C], or with fewer axes in front ([rows][C], [N][rows][C])."""
+    shape = t.shape
+    if not 2 <= len(shape) <= 4 or not t.is_contiguous():
+        raise ValueError("expected a contiguous [N][H][W][C] tensor, or [rows][C]")
+    n, h, w, c = (1,) * (4 - len(shape)) + tuple(shape)
+    return sr_tensor((t.data_ptr() if n and h and w and c else 0) or None, _code(t.dtype), n, c, h, w)
+
+
+def _matrix(t) -> sr_tensor:
+    """Descriptor of a weight [O][C] or a bias [O]."""
+    shape = t.shape
+    if not 1 <= len(shape) <= 2 or not t.is_contiguous():
+        raise ValueError("a weight is a contiguous [out][in] tensor, a bias a contiguous vector")
+    h, w = (1,) * (2 - len(shape)) + tuple(shape)
+    return sr_tensor((t.data_ptr() if h and w else 0) or None, _code(t.dtype), 1, 1, h, w)
+
+
+def _maybe_rows(t):
+    return None if t is None else _rows(t)
+
+
+def _maybe_matrix(t):
+    return None if t is None else _matrix(t)
+
+
+def _room(workspace, need, like, stream):
+    """A call's scratch, its address and size; none where none is needed and none is given."""
+    if workspace is None and not need:
+        return None, None, 0
+    workspace = _scratch(workspace, need, like, stream)
+    return workspace, ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
+
+
+def sr_layer_linear_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
+    return int(load().sr_layer_linear_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+
+
+def sr_layer_linear(x, weight, bias, act, residual, y, workspace=None, stream=None):
+    """y = act(x weight^T + bias) + residual over rows of features (include/sr_layer.h); ``bias`` and ``residual`` may be
+    None; scratch is made here unless the caller passes it."""
+    _here(x, weight, bias, residual, y, workspace)
+    dx, dy = _rows(x), _rows(y)
+    need = load().sr_layer_linear_workspace_bytes(dx.n * dx.h * dx.w, dx.c, dy.c, dx.dtype)
+    workspace, room, size = _room(workspace, need, x, stream)
+    _check(_lib.sr_layer_linear(dx, _matrix(weight), _maybe_matrix(bias), act, _maybe_rows(residual), dy, room, size, _stream(stream)))
+    return y
+
+
+def sr_layer_linear_grad_workspace_bytes(rows: int, in_features: int, out_features: int, dtype, act: int) -> int:
+    return int(load().sr_layer_linear_grad_workspace_bytes(rows, in_features, out_features, _code(dtype), act))
+
+
+def sr_layer_linear_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace=None, stream=None):
+    """Gradient of sr_layer_linear with respect to features, weight and bias, each of which may be None."""
+    _here(x, weight, bias, dy, dx, dweight, dbias, workspace)
+    rx, ry = _rows(x), _rows(dy)
+    need = load().sr_layer_linear_grad_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype, act)
+    workspace, room, size = _room(workspace, need, x, stream)
+    _check(_lib.sr_layer_linear_grad(rx, _matrix(weight), _maybe_matrix(bias), act, ry, _maybe_rows(dx), _maybe_matrix(dweight),
+                                     _maybe_matrix(dbias), room, size, _stream(stream)))
+    return dx, dweight, dbias
+
+
+def sr_layer_gated_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
+    return int(load().sr_layer_gated_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+
+
+def sr_layer_gated(x, weight, bias, act, y, workspace=None, stream=None):
+    """y = act(x Wg^T + bg) (x Wu^T + bu), ``weight`` [2 * out][in] being Wg on top of Wu (include/sr_layer.h)."""
+    _here(x, weight, bias, y, workspace)
+    rx, ry = _rows(x), _rows(y)
+    need = load().sr_layer_gated_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype)
+    workspace, room, size = _room(workspace, need, x, stream)
+    _check(_lib.sr_layer_gated(rx, _matrix(weight), _maybe_matrix(bias), act, ry, room, size, _stream(stream)))
+    return y
+
+
+def sr_layer_gated_grad_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
+    return int(load().sr_layer_gated_grad_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+
+
+def sr_layer_gated_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace=None, stream=None):
+    """Gradient of sr_layer_gated with respect to features, weight and bias, each of which may be None."""
+    _here(x, weight, bias, dy, dx, dweight, dbias, workspace)
+    rx, ry = _rows(x), _rows(dy)
+    need = load().sr_layer_gated_grad_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype)
+    workspace, room, size = _room(workspace, need, x, stream)
+    _check(_lib.sr_layer_gated_grad(rx, _matrix(weight), _maybe_matrix(bias), act, ry, _maybe_rows(dx), _maybe_matrix(dweight),
+                                    _maybe_matrix(dbias), room, size, _stream(stream)))
+    return dx, dweight, dbias
+
+
+def _dense(t):
+    """Whether a tensor's elements fill one piece of memory, in whatever order of its axes."""
+    if t.is_contiguous():
+        return True
+    at = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != at:
+            return False
+        at *= size
+    return True
+
+
+class sr_tensor_list:
+    """Descriptions of a list of tensors, made once and used for as long as they are where they are (the tensors are kept
+    alive).  All on one device, of any number of axes, stored without gaps in any order of them: a list is gone through
+    element by element."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (sr_tensor * max(1, len(self.tensors)))()
+        self.strides = [t.stride() for t in self.tensors]
+        self.device = self.tensors[0].get_device() if self.tensors else -1
+        for d, t in zip(self.array, self.tensors):
+            if not t.is_cuda or t.get_device() != self.device:
+                raise ValueError(f"a tensor is on {t.device}: expected all of them on one device")
+            if not _dense(t):
+                raise ValueError("expected tensors without gaps")
+            shape = tuple(t.shape)
+            lead = 1
+            for n in shape[:-3]:
+                lead *= n
+            d.data, d.dtype = (t.data_ptr() if t.numel() else 0) or None, _code(t.dtype)
+            d.n, d.c, d.h, d.w = (lead,) + (1,) * (3 - len(shape)) + shape[-3:]
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def sr_grad_clip_workspace_bytes(tensors: int) -> int:
+    return int(load().sr_grad_clip_workspace_bytes(int(tensors)))
+
+
+def sr_grad_clip(grads, outs, max_norm, norm, workspace=None, stream=None):
+    """The norm over all ``grads`` and the factor to at most ``max_norm``, into ``norm`` (float32, 2), and the gradients times that
+    factor into ``outs`` (``grads`` itself: in place; None: the norm alone).  Both are lists of tensors, or sr_tensor_list."""
+    import torch
+    given = grads
+    if not isinstance(grads, sr_tensor_list):
+        grads = sr_tensor_list(grads)
+    if outs is given:
+        outs = grads
+    elif outs is not None and not isinstance(outs, sr_tensor_list):
+        outs = sr_tensor_list(outs)
+    if outs is not None and outs is not grads:
+        if len(outs) != len(grads):
+            raise ValueError("as many outputs as gradients")
+        if outs.strides != grads.strides:
+            raise ValueError("an output is stored in another order than its gradient")
+    for a in (grads, outs):
+        if a is not None and len(a) and a.device != torch.cuda.current_device():
+            raise ValueError("a list is not on the current device")
+    _here(norm, workspace)
+    workspace = _scratch(workspace, sr_grad_clip_workspace_bytes(len(grads)), norm, stream)
+    _check(load().sr_grad_clip(grads.array, None if outs is None else outs.array, len(grads), max_norm, _plain(norm, torch.float32, 2, "norm"),
+                               ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return outs, norm

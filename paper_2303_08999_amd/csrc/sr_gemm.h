@@ -1,0 +1,298 @@
+// Products for the layers of include/sr_layer.h: C[m][n] = sum_k A(m, k) B(n, k) on the matrix cores, with what a layer does to C
+// before it is stored.
+//
+// Operands of one type, fp32, fp16 or bfloat16; sums in fp32.  An operand is stored with k running fastest (KC: a layer's rows and
+// its weight in the forward product) or with the other index running fastest (RC: the weight in dx = dz W, both in dW = dz^T x).
+// A workgroup makes a BM x BN tile of C.  128 bytes of k (64 values, 32 of fp32) of both operands go to LDS at a time, two buffers in
+// turn: while one is multiplied the next is under way, straight from memory to LDS.  RC operands are turned by the LDS
+// reads (16-bit types) or read value by value (fp32, whose matrix instructions are slow enough for that).
+//
+// LDS: KC as [row][8 pieces of 16 bytes], piece p of row r in place p ^ (r & 7), so that the 16 or 32 rows a read takes at one k lie in
+// different banks; RC as [k][row], its chunks of 16 rows exchanged by some bits of k for the same reason.
+//
+// The matrix instructions get B as their first operand: a lane then holds consecutive n of one m, and the tile goes through LDS
+// once more, 32 rows of a wavefront's part at a time, to be finished and stored in pieces of 8 values of a row.
+#pragma once
+#include <stdint.h>
+
+#include "sr_launch.h"
+#include "../../include/sr_layer.h"
+
+namespace srd {
+
+using u32x4g = __attribute__((ext_vector_type(4))) unsigned;
+using u32x4u = __attribute__((ext_vector_type(4), aligned(2))) unsigned;      // in memory, at any element
+using f32x4g = __attribute__((ext_vector_type(4))) float;
+using f32x16g = __attribute__((ext_vector_type(16))) float;
+using half8g = __attribute__((ext_vector_type(8))) _Float16;
+using bf8g = __attribute__((ext_vector_type(8))) __bf16;
+using s16x4g = __attribute__((ext_vector_type(4))) short;
+
+enum { GEMM_KC_KC = 0, GEMM_KC_RC = 1, GEMM_RC_RC = 2 };          // A, B
+// What is done to C: z = C + bias
+enum {
+    GEMM_STORE = 0,        // out = act(z) + extra
+    GEMM_SLOPE = 1,        // out = extra act'(z)
+    GEMM_GATED = 2,        // out = act(z_gate) z_up
+    GEMM_GATED_SLOPE = 3,  // out[n] = extra z_up act'(z_gate), out[half + n] = extra act(z_gate)
+    GEMM_PARTIAL = 4       // C itself, fp32, to partial[split]
+};
+
+struct GemmArgs {
+    const void* a;
+    const void* b;
+    int64_t lda, ldb;          // elements from one row of the stored matrix to the next
+    int m, n, k;               // n: of C; for the gated forms of their halves
+    int half;                  // gated forms: row of B where the second half starts
+    int tiles_m, tiles_n, splits;
+    int ksplit;                // of k a split takes, a multiple of 128 bytes of it
+    int mode, act;
+    const void* bias;          // [n], or null
+    const void* extra;         // residual or dy, [m][ld_extra], or null
+    void* out;
+    int64_t ld_extra, ld_out;
+    float* partial;            // [splits][m][n]
+    float* sums;               // RC_RC: [splits][m] sums of A over k, or null ...
+    void* sums_out;            // ... or, of one split, [m] in the operands' type
+};
+
+// Tiles: 0: 64 x 64, 1: 128 x 128, 2: 256 x 256 (operands on 16-byte pieces only).
+template <typename T> hipError_t launch_gemm(const GemmArgs& g, int layout, bool aligned, int tile, hipStream_t st);
+inline int gemm_tile_rows(int tile) { return 64 << tile; }
+
+// z of the split sums, and what the epilogue would have done: elements [m][n], sums over the splits in double
+template <typename T> hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st);
+// Few rows: one pass over the weights (layout KC_KC; modes STORE and GATED)
+template <typename T> hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st);
+constexpr int SKINNY_ROWS = 64;
+
+// ---- values ---------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float act_exp(float z) { return __builtin_amdgcn_exp2f(z * LOG2E); }
+__device__ __forceinline__ float sigmoid_of(float z) { return 1.0f / (1.0f + act_exp(-z)); }
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.0f + erff(z * 0.70710678118654752440f)); }
+// z to act(z), or to act'(z); the branches are uniform
+__device__ __forceinline__ void act8(int act, float z[8]) {
+    if (act == SR_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = z[i] <= 0.0f ? 0.0f : z[i];        // NaN stays
+    } else if (act == SR_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] *= normal_cdf(z[i]);
+    } else if (act == SR_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = z[i] / (1.0f + act_exp(-z[i]));
+    } else if (act == SR_ACT_SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = sigmoid_of(z[i]);
+    }
+}
+// values and slopes of z
+__device__ __forceinline__ void slope8(int act, const float z[8], float value[8], float slope[8]) {
+    if (act == SR_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) value[i] = z[i] <= 0.0f ? 0.0f : z[i], slope[i] = z[i] > 0.0f ? 1.0f : 0.0f;
+    } else if (act == SR_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float c = normal_cdf(z[i]);
+            value[i] = z[i] * c;
+            slope[i] = fmaf(z[i] * 0.39894228040143267794f, act_exp(-0.5f * z[i] * z[i]), c);
+        }
+    } else if (act == SR_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = sigmoid_of(z[i]);
+            value[i] = z[i] * s;
+            slope[i] = s * fmaf(z[i], 1.0f - s, 1.0f);
+        }
+    } else if (act == SR_ACT_SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = sigmoid_of(z[i]);
+            value[i] = s;
+            slope[i] = s * (1.0f - s);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) value[i] = z[i], slope[i] = 1.0f;
+    }
+}
+
+__device__ __forceinline__ float gm_get(const float* p) { return *p; }
+__device__ __forceinline__ float gm_get(const __half* p) { return (float)*(const _Float16*)p; }
+__device__ __forceinline__ float gm_get(const bf16raw* p) { return __uint_as_float((unsigned)p->bits << 16); }
+__device__ __forceinline__ void gm_put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void gm_put(__half* p, float v) { *(_Float16*)p = (_Float16)v; }
+__device__ __forceinline__ void gm_put(bf16raw* p, float v) { *(__bf16*)p = (__bf16)v; }
+
+__device__ __forceinline__ void gm_get8(const float* p, float v[8]) {
+    const u32x4u a = ((const u32x4u*)p)[0], b = ((const u32x4u*)p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]), v[4 + i] = __uint_as_float(b[i]);
+}
+__device__ __forceinline__ void gm_get8(const __half* p, float v[8]) {
+    const half8g a = __builtin_bit_cast(half8g, (u32x4g)*(const u32x4u*)p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+}
+__device__ __forceinline__ void gm_get8(const bf16raw* p, float v[8]) {
+    const u32x4g a = *(const u32x4u*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(a[i] << 16), v[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void gm_put8(float* p, const float v[8]) {
+    u32x4u a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]), b[i] = __float_as_uint(v[4 + i]);
+    ((u32x4u*)p)[0] = a;
+    ((u32x4u*)p)[1] = b;
+}
+__device__ __forceinline__ void gm_put8(__half* p, const float v[8]) {
+    half8g a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = (_Float16)v[i];
+    *(u32x4u*)p = __builtin_bit_cast(u32x4g, a);
+}
+__device__ __forceinline__ void gm_put8(bf16raw* p, const float v[8]) {
+    bf8g a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = (__bf16)v[i];
+    *(u32x4u*)p = __builtin_bit_cast(u32x4g, a);
+}
+// as many of 8 as there are
+template <typename T> __device__ __forceinline__ void gm_get_some(const T* p, int count, float v[8]) {
+    if (count >= 8) {
+        gm_get8(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < count ? gm_get(p + i) : 0.0f;
+    }
+}
+template <typename T> __device__ __forceinline__ void gm_put_some(T* p, int count, const float v[8]) {
+    if (count >= 8) {
+        gm_put8(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) gm_put(p + i, v[i]);
+    }
+}
+
+// 16 bytes of a row of which `count` elements are there (0 or less: none), zeros behind them
+template <typename T> __device__ __forceinline__ u32x4g gm_piece(const T* p, int count) {
+    constexpr int E = 16 / sizeof(T);
+    if (count >= E) return *(const u32x4u*)p;
+    u32x4g v = {0, 0, 0, 0};
+    if (count > 0) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < count) {
+                if constexpr (sizeof(T) == 4) v[i] = ((const unsigned*)p)[i];
+                else v[i / 2] |= (unsigned)((const unsigned short*)p)[i] << 16 * (i % 2);
+            }
+    }
+    return v;
+}
+
+// The first `count` elements of a piece that is there, but may end in what is not the row's
+template <typename T> __device__ __forceinline__ u32x4g gm_cut(u32x4g v, int count) {
+    constexpr int E = 16 / sizeof(T);
+    if (count < E)
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i >= count) {
+                if constexpr (sizeof(T) == 4) v[i] = 0;
+                else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+    return v;
+}
+
+// One step of k on a pair of 16-byte fragments: MT = 32: 32 x 32, 2 pieces of k; MT = 16: 16 x 16, 4 pieces.
+template <int MT> struct AccOf { typedef f32x16g type; };
+template <> struct AccOf<16> { typedef f32x4g type; };
+template <typename T, int MT> __device__ __forceinline__ void gm_mul(typename AccOf<MT>::type& c, u32x4g a, u32x4g b) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (MT == 32) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+            else c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+        }
+    } else if constexpr (__is_same(T, __half)) {
+        if constexpr (MT == 32) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8g, a), __builtin_bit_cast(half8g, b), c, 0, 0, 0);
+        else c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8g, a), __builtin_bit_cast(half8g, b), c, 0, 0, 0);
+    } else {
+        if constexpr (MT == 32) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8g, a), __builtin_bit_cast(bf8g, b), c, 0, 0, 0);
+        else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8g, a), __builtin_bit_cast(bf8g, b), c, 0, 0, 0);
+    }
+}
+template <typename T> __device__ __forceinline__ float gm_sum_piece(u32x4g a) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            s += __uint_as_float(a[i]);
+        } else if constexpr (__is_same(T, __half)) {
+            using half2g = __attribute__((ext_vector_type(2))) _Float16;
+            const half2g h = __builtin_bit_cast(half2g, (unsigned)a[i]);
+            s += (float)h[0] + (float)h[1];
+        } else {
+            s += __uint_as_float(a[i] << 16) + __uint_as_float(a[i] & 0xffff0000u);
+        }
+    }
+    return s;
+}
+
+// What a layer does to 8 columns from `col` on of row `row` of C: z in, the outputs stored.  For the gated forms u is the same
+// columns of the second half.
+template <typename T>
+__device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int col, float z[8], float u[8], const float bz[8], const float bu[8]) {
+    const int count = g.n - col;
+    float e[8];
+    if (g.extra) gm_get_some((const T*)g.extra + row * g.ld_extra + col, count, e);
+    T* const out = (T*)g.out + row * g.ld_out + col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] += bz[i];
+    if (g.mode == GEMM_STORE) {
+        act8(g.act, z);
+        if (g.extra) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] += e[i];
+        }
+        gm_put_some(out, count, z);
+    } else if (g.mode == GEMM_SLOPE) {
+        float value[8], slope[8];
+        slope8(g.act, z, value, slope);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = e[i] * slope[i];
+        gm_put_some(out, count, z);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] += bu[i];
+        if (g.mode == GEMM_GATED) {
+            act8(g.act, z);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] *= u[i];
+            gm_put_some(out, count, z);
+        } else {
+            float value[8], slope[8];
+            slope8(g.act, z, value, slope);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                z[i] = e[i] * u[i] * slope[i];
+                u[i] = e[i] * value[i];
+            }
+            gm_put_some(out, count, z);
+            gm_put_some(out + g.half, count, u);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void gm_bias8(const GemmArgs& g, int col, bool gated, float bz[8], float bu[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bz[i] = bu[i] = 0.0f;
+    if (!g.bias || col >= g.n) return;
+    gm_get_some((const T*)g.bias + col, g.n - col, bz);
+    if (gated) gm_get_some((const T*)g.bias + g.half + col, g.n - col, bu);
+}
+
+}  // namespace srd

@@ -1,0 +1,319 @@
+// Layers and their gradients (include/sr_layer.h): checks, which kernels a call is made of, and their workspace.
+//
+// A gradient is three products: z made anew, with dz = dy act'(z) as its epilogue, stored in the workspace; dx = dz W; dW = dz^T x, whose
+// workgroups of the first column of tiles sum dz over the rows on the way (db).  Without an activation dy is dz.
+#include <stdint.h>
+#include <type_traits>
+
+#include "sr_gemm.h"
+
+namespace srd {
+namespace {
+
+constexpr int GPU_CUS = 256;                 // of a gfx950 in one partition; the plan is the same wherever the sizes are asked for
+
+size_t layer_esize(int d) { return d == SR_F32 ? 4 : 2; }
+bool layer_type(int d) { return d == SR_F32 || d == SR_F16 || d == SR_BF16; }
+bool layer_act(int a) { return a >= SR_ACT_NONE && a <= SR_ACT_SIGMOID; }
+bool features(int64_t c) { return c >= 1 && c <= SR_MAX_FEATURES; }
+constexpr long long MOST_ROWS = 0x7fffffffLL - 256;
+
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Span { const void* p; size_t n; };
+size_t bytes_of(const sr_tensor* t) { return (size_t)t->n * t->c * t->h * t->w * layer_esize(t->dtype); }
+Span span(const sr_tensor* t) { return t ? Span{t->data, bytes_of(t)} : Span{nullptr, 0}; }
+bool overlap(const Span& a, const Span& b) {
+    const uintptr_t p = (uintptr_t)a.p, q = (uintptr_t)b.p;
+    return a.p && b.p && a.n && b.n && p < q + b.n && q < p + a.n;
+}
+template <int NO, int NI>
+bool any_overlap(const Span (&out)[NO], const Span (&in)[NI]) {
+    for (int i = 0; i < NO; ++i) {
+        for (int j = 0; j < NI; ++j)
+            if (overlap(out[i], in[j])) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return true;
+    }
+    return false;
+}
+
+// How one product is cut: tile (-1: the kernel for few rows), splits of k.
+struct Cut { int tile, splits, ksplit; };
+Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
+    const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
+    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {-1, 1, 0};
+    const int64_t nn = gated ? 2 * n : n;
+    auto tiles = [&](int t) { const int64_t s = 64 << t; return ((m + s - 1) / s) * ((nn + s - 1) / s); };
+    int tile = tiles(2) >= 3 * GPU_CUS / 4 ? 2 : tiles(1) >= GPU_CUS ? 1 : 0;
+    int64_t splits = 1;
+    if (tiles(tile) < 2 * GPU_CUS && steps >= 16) {
+        if (layout == GEMM_RC_RC) tile = tiles(2) >= 32 ? 2 : m > 64 || n > 64 ? 1 : 0;
+        const int64_t want = (2 * GPU_CUS + tiles(tile) - 1) / tiles(tile);
+        splits = want < steps / 8 ? want : steps / 8;
+    }
+    const int64_t each = (steps + splits - 1) / splits;
+    splits = steps ? (steps + each - 1) / each : 1;
+    return {tile, (int)(splits < 1 ? 1 : splits), (int)(each * bk)};
+}
+
+// Scratch of a split product: its partial results, and (dW) its partial sums of dz
+size_t partial_bytes(const Cut& c, int64_t m, int64_t width) { return c.splits > 1 ? up256((size_t)c.splits * m * width * 4) : 0; }
+
+template <typename F> hipError_t by_type(int d, F f) {
+    return d == SR_F32 ? f((float*)nullptr) : d == SR_F16 ? f((__half*)nullptr) : f((bf16raw*)nullptr);
+}
+
+// One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, where
+// sums_out is set, of the sums).
+hipError_t product(GemmArgs g, int dtype, int layout, void* ws, hipStream_t st) {
+    const size_t es = layer_esize(dtype);
+    const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
+    Cut c = cut_of(g.m, g.n, g.k, es, layout, gated);
+    const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda * es % 16 == 0 && g.ldb * es % 16 == 0;
+    g.splits = c.splits;
+    g.ksplit = c.ksplit;
+    return by_type(dtype, [&](auto t) -> hipError_t {
+        using T = std::remove_pointer_t<decltype(t)>;
+        if (c.tile < 0 && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
+        int tile = c.tile < 0 ? 0 : c.tile;
+        if (!aligned && tile > 1) tile = 1;
+        const int side = gemm_tile_rows(tile);
+        g.tiles_m = (g.m + side - 1) / side;
+        if (g.splits == 1) {
+            g.tiles_n = g.out ? (int)(((int64_t)(gated ? 2 : 1) * g.n + side - 1) / side) : 1;      // without: the sums of dz alone
+            if (g.ksplit == 0) g.ksplit = g.k;
+            return launch_gemm<T>(g, layout, aligned, tile, st);
+        }
+        GemmArgs p = g;
+        p.mode = GEMM_PARTIAL;
+        p.n = gated ? 2 * g.half : g.n;
+        p.tiles_n = g.out ? (p.n + side - 1) / side : 1;
+        p.partial = g.partial = g.out ? (float*)ws : nullptr;
+        if (g.sums_out) {
+            p.sums = g.sums = (float*)((char*)ws + partial_bytes(c, g.m, p.n));
+            p.sums_out = nullptr;
+        }
+        const hipError_t e = launch_gemm<T>(p, layout, aligned, tile, st);
+        return e != hipSuccess ? e : launch_gemm_finish<T>(g, st);
+    });
+}
+
+int64_t rows_of(const sr_tensor* t) { return (int64_t)t->n * t->h * t->w; }
+
+struct Layer {
+    int64_t rows;
+    int in, out, wide, dtype;
+    bool gated;
+};
+
+size_t forward_scratch(const Layer& l) {
+    const Cut c = cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated);
+    return partial_bytes(c, l.rows, l.wide);
+}
+// dz, rows on 16-byte pieces
+int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (l.wide + e - 1) / e * e; }
+size_t dz_bytes(const Layer& l, int act) { return l.gated || act != SR_ACT_NONE ? up256((size_t)l.rows * dz_row(l) * layer_esize(l.dtype)) : 0; }
+size_t grad_scratch(const Layer& l, int act) {
+    const size_t es = layer_esize(l.dtype), dz = dz_bytes(l, act);
+    const Cut x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false), w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
+    size_t most = dz ? forward_scratch(l) : 0;
+    if (partial_bytes(x, l.rows, l.in) > most) most = partial_bytes(x, l.rows, l.in);
+    const size_t dw = partial_bytes(w, l.wide, l.in) + (w.splits > 1 ? up256((size_t)w.splits * l.wide * 4) : 0);
+    return dz + (dw > most ? dw : most);
+}
+
+bool layer_sizes(Layer& l, long long rows, int in, int out, int dtype, bool gated) {
+    if (rows < 0 || rows > MOST_ROWS || !features(in) || !features(out) || !layer_type(dtype)) return false;
+    l = Layer{rows, in, out, gated ? 2 * out : out, dtype, gated};
+    return true;
+}
+
+bool is_matrix(const sr_tensor* t, int rows, int cols) { return t->n == 1 && t->c == 1 && t->h == rows && t->w == cols; }
+bool same_rows(const sr_tensor* t, const sr_tensor* x) { return t->n == x->n && t->h == x->h && t->w == x->w; }
+
+// What all four calls check.  `y` is the forward call's output or dy; rest: further tensors with the rows of x and y's features (or null).
+int layer_args(Layer& l, const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* y,
+               const sr_tensor* residual, bool gated) {
+    if (!x || !weight || !y) return SR_ERR_NULL;
+    if (!layer_type(x->dtype) || !layer_act(act)) return SR_ERR_UNSUPPORTED;
+    for (const sr_tensor* t : {weight, bias, y, residual})
+        if (t && t->dtype != x->dtype) return SR_ERR_UNSUPPORTED;
+    for (const sr_tensor* t : {x, weight, bias, y, residual})
+        if (t && (t->n < 0 || t->c < 0 || t->h < 0 || t->w < 0)) return SR_ERR_SHAPE;
+    if (!features(x->c) || !features(y->c)) return SR_ERR_UNSUPPORTED;
+    if ((int64_t)x->n * x->h > MOST_ROWS || (int64_t)x->n * x->h * x->w > MOST_ROWS) return SR_ERR_UNSUPPORTED;
+    layer_sizes(l, rows_of(x), x->c, y->c, x->dtype, gated);
+    if (!is_matrix(weight, l.wide, l.in) || (bias && !is_matrix(bias, 1, l.wide)) || !same_rows(y, x)) return SR_ERR_SHAPE;
+    if (residual && (!same_rows(residual, x) || residual->c != y->c)) return SR_ERR_SHAPE;
+    const size_t es = layer_esize(l.dtype);
+    for (const sr_tensor* t : {weight, bias}) {
+        if (t && !t->data) return SR_ERR_NULL;
+        if (t && (uintptr_t)t->data % es) return SR_ERR_ALIGN;
+    }
+    if (l.rows)
+        for (const sr_tensor* t : {x, y, residual}) {
+            if (t && !t->data) return SR_ERR_NULL;
+            if (t && (uintptr_t)t->data % es) return SR_ERR_ALIGN;
+        }
+    return SR_OK;
+}
+int scratch_args(const void* workspace, size_t bytes, size_t need) {
+    if (need && (!workspace || bytes < need)) return SR_ERR_SHAPE;
+    return need && (uintptr_t)workspace % 16 ? SR_ERR_ALIGN : SR_OK;
+}
+
+GemmArgs forward_args(const Layer& l, const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act) {
+    GemmArgs g = {};
+    g.a = x->data;
+    g.b = weight->data;
+    g.lda = g.ldb = l.in;
+    g.m = (int)l.rows;
+    g.n = g.half = l.out;
+    g.k = l.in;
+    g.act = act;
+    g.bias = bias ? bias->data : nullptr;
+    g.ld_extra = g.ld_out = l.out;
+    return g;
+}
+
+int forward(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* residual, sr_tensor* y, bool gated,
+            void* workspace, size_t workspace_bytes, void* stream) {
+    Layer l;
+    int st = layer_args(l, x, weight, bias, act, y, residual, gated);
+    if (st != SR_OK) return st;
+    const size_t need = forward_scratch(l);
+    st = scratch_args(workspace, workspace_bytes, need);
+    if (st != SR_OK) return st;
+    const Span out[] = {span(y), {need ? workspace : nullptr, need}}, in[] = {span(x), span(weight), span(bias), span(residual)};
+    if (any_overlap(out, in)) return SR_ERR_ALIAS;
+    if (!l.rows) return SR_OK;
+    GemmArgs g = forward_args(l, x, weight, bias, act);
+    g.mode = gated ? GEMM_GATED : GEMM_STORE;
+    g.extra = residual ? residual->data : nullptr;
+    g.out = y->data;
+    return product(g, l.dtype, GEMM_KC_KC, workspace, (hipStream_t)stream) == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
+}
+
+int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* dy,
+             sr_tensor* dx, sr_tensor* dweight, sr_tensor* dbias, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
+    Layer l;
+    int st = layer_args(l, x, weight, bias, act, dy, nullptr, gated);
+    if (st != SR_OK) return st;
+    if (!dx && !dweight && !dbias) return SR_ERR_NULL;
+    for (const sr_tensor* t : {dx, dweight, dbias})
+        if (t && t->dtype != x->dtype) return SR_ERR_UNSUPPORTED;
+    if ((dx && (!same_rows(dx, x) || dx->c != x->c)) || (dweight && !is_matrix(dweight, l.wide, l.in)) || (dbias && !is_matrix(dbias, 1, l.wide)))
+        return SR_ERR_SHAPE;
+    const size_t es = layer_esize(l.dtype);
+    for (const sr_tensor* t : {l.rows ? dx : nullptr, dweight, dbias}) {
+        if (t && !t->data) return SR_ERR_NULL;
+        if (t && (uintptr_t)t->data % es) return SR_ERR_ALIGN;
+    }
+    const size_t need = grad_scratch(l, act), dz = dz_bytes(l, act);
+    st = scratch_args(workspace, workspace_bytes, need);
+    if (st != SR_OK) return st;
+    const Span out[] = {span(dx), span(dweight), span(dbias), {need ? workspace : nullptr, need}};
+    const Span in[] = {span(x), span(weight), span(bias), span(dy)};
+    if (any_overlap(out, in)) return SR_ERR_ALIAS;
+
+    hipStream_t s = (hipStream_t)stream;
+    void* const rest = (char*)workspace + dz;
+    const void* z = dy->data;
+    int64_t ldz = l.out;
+    hipError_t e = hipSuccess;
+    if (dz) {
+        GemmArgs g = forward_args(l, x, weight, bias, act);
+        g.mode = gated ? GEMM_GATED_SLOPE : GEMM_SLOPE;
+        g.extra = dy->data;
+        g.out = workspace;
+        g.ld_out = ldz = dz_row(l);
+        z = workspace;
+        if (l.rows) e = product(g, l.dtype, GEMM_KC_KC, rest, s);
+    }
+    if (dx && l.rows && e == hipSuccess) {
+        GemmArgs g = {};
+        g.a = z;
+        g.lda = ldz;
+        g.b = weight->data;
+        g.ldb = l.in;
+        g.m = (int)l.rows;
+        g.n = l.in;
+        g.k = l.wide;
+        g.mode = GEMM_STORE;
+        g.out = dx->data;
+        g.ld_out = l.in;
+        e = product(g, l.dtype, GEMM_KC_RC, rest, s);
+    }
+    if ((dweight || dbias) && e == hipSuccess) {
+        GemmArgs g = {};
+        g.a = z;
+        g.lda = ldz;
+        g.b = x->data;
+        g.ldb = l.in;
+        g.m = l.wide;
+        g.n = l.in;
+        g.k = (int)l.rows;
+        g.mode = GEMM_STORE;
+        g.out = dweight ? dweight->data : nullptr;
+        g.ld_out = l.in;
+        g.sums_out = dbias ? dbias->data : nullptr;
+        e = product(g, l.dtype, GEMM_RC_RC, rest, s);
+    }
+    return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
+}
+
+}  // namespace
+}  // namespace srd
+
+using namespace srd;
+
+extern "C" __attribute__((visibility("default")))
+size_t sr_layer_linear_workspace_bytes(long long rows, int in, int out, int dtype) {
+    Layer l;
+    return layer_sizes(l, rows, in, out, dtype, false) ? forward_scratch(l) : 0;
+}
+
+extern "C" __attribute__((visibility("default")))
+int sr_layer_linear(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* residual,
+                    sr_tensor* y, void* workspace, size_t workspace_bytes, void* stream) {
+    return forward(x, weight, bias, act, residual, y, false, workspace, workspace_bytes, stream);
+}
+
+extern "C" __attribute__((visibility("default")))
+size_t sr_layer_linear_grad_workspace_bytes(long long rows, int in, int out, int dtype, int act) {
+    Layer l;
+    return layer_act(act) && layer_sizes(l, rows, in, out, dtype, false) ? grad_scratch(l, act) : 0;
+}
+
+extern "C" __attribute__((visibility("default")))
+int sr_layer_linear_grad(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* dy,
+                         sr_tensor* dx, sr_tensor* dweight, sr_tensor* dbias,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    return gradient(x, weight, bias, act, dy, dx, dweight, dbias, false, workspace, workspace_bytes, stream);
+}
+
+extern "C" __attribute__((visibility("default")))
+size_t sr_layer_gated_workspace_bytes(long long rows, int in, int out, int dtype) {
+    Layer l;
+    return layer_sizes(l, rows, in, out, dtype, true) ? forward_scratch(l) : 0;
+}
+
+extern "C" __attribute__((visibility("default")))
+int sr_layer_gated(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, sr_tensor* y,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+    return forward(x, weight, bias, act, nullptr, y, true, workspace, workspace_bytes, stream);
+}
+
+extern "C" __attribute__((visibility("default")))
+size_t sr_layer_gated_grad_workspace_bytes(long long rows, int in, int out, int dtype) {
+    Layer l;
+    return layer_sizes(l, rows, in, out, dtype, true) ? grad_scratch(l, SR_ACT_NONE) : 0;
+}
+
+extern "C" __attribute__((visibility("default")))
+int sr_layer_gated_grad(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* dy,
+                        sr_tensor* dx, sr_tensor* dweight, sr_tensor* dbias,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    return gradient(x, weight, bias, act, dy, dx, dweight, dbias, true, workspace, workspace_bytes, stream);
+}

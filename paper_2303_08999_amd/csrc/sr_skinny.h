@@ -1,0 +1,175 @@
+// Products of few rows with a weight (sr_gemm.h), and the sums of split products.
+#pragma once
+#include "sr_gemm.h"
+
+namespace srd {
+namespace {
+
+constexpr int SKW = 8;             // wavefronts of a workgroup
+
+// Up to 16 RF rows.  A workgroup makes 16 columns (of both halves, where there are two) and reads their weights once: straight from memory
+// into the matrix instructions' first operand, a lane 16 bytes of one of the 16 rows, so that four lanes take 64 bytes of a row together.  Its
+// eight wavefronts take every eighth step of k and add up in LDS.  Bound by the weights' way from memory and, for small ones, by the launch.
+template <typename T, bool GATED, int RF, bool ALIGNED>
+__global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
+    constexpr int E = 16 / sizeof(T), H = GATED ? 2 : 1, AHEAD = RF > 2 ? 2 : 4;
+    __shared__ __align__(16) float sh[SKW * H * RF * 256];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16, r = lane % 16;
+    const int kc = lane / 16 * E;
+    const T* pb[H];
+    const T* pa[RF];
+    {
+        const int n = n0 + r < g.n ? n0 + r : g.n - 1;
+#pragma unroll
+        for (int h = 0; h < H; ++h) pb[h] = (const T*)g.b + (int64_t)(n + h * g.half) * g.ldb + kc;
+#pragma unroll
+        for (int f = 0; f < RF; ++f) pa[f] = (const T*)g.a + (int64_t)(16 * f + r < g.m ? 16 * f + r : g.m - 1) * g.lda + kc;
+    }
+    f32x4g acc[H][RF];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int f = 0; f < RF; ++f) acc[h][f] = f32x4g{0.0f, 0.0f, 0.0f, 0.0f};
+    auto piece = [&](const T* p, int k) -> u32x4g {
+        if constexpr (ALIGNED) return kc + k < g.k ? *(const u32x4g*)(p + k) : u32x4g{0, 0, 0, 0};
+        else return gm_piece(p + k, g.k - kc - k);
+    };
+    for (int k = wave * 4 * E; k < g.k; k += SKW * 4 * E * AHEAD) {
+        u32x4g vb[AHEAD][H], va[AHEAD][RF];
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {
+            const int at = k + s * SKW * 4 * E;
+#pragma unroll
+            for (int h = 0; h < H; ++h) vb[s][h] = piece(pb[h], at);
+#pragma unroll
+            for (int f = 0; f < RF; ++f) va[s][f] = piece(pa[f], at);
+        }
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s)
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) gm_mul<T, 16>(acc[h][f], vb[s][h], va[s][f]);
+    }
+    // [wave][half][row][16 columns]
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int f = 0; f < RF; ++f) *(f32x4g*)(sh + ((wave * H + h) * RF * 16 + f * 16 + r) * 16 + lane / 16 * 4) = acc[h][f];
+    __syncthreads();
+    for (int i = threadIdx.x; i < H * RF * 256; i += SKW * 64) {
+        float s = sh[i];
+#pragma unroll
+        for (int w = 1; w < SKW; ++w) s += sh[w * H * RF * 256 + i];
+        sh[i] = s;                                         // read by this thread alone
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * RF; i += SKW * 64) {
+        const int m = i / 2, c = i % 2 * 8, col = n0 + c;
+        if (m >= g.m || col >= g.n) continue;
+        float z[8], u[8], bz[8], bu[8];
+        gm_bias8<T>(g, col, GATED, bz, bu);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            z[e] = sh[m * 16 + c + e];
+            u[e] = GATED ? sh[RF * 256 + m * 16 + c + e] : 0.0f;
+        }
+        gm_finish8<T>(g, m, col, z, u, bz, bu);
+    }
+}
+
+// 8 columns of a row for a group of SL threads, each every SL-th split, in double; what follows is as in the tile kernel.  Behind the rows of C
+// come the octets of `sums` (its splits' rows of g.m values), stored as they are.
+struct FinishArgs {
+    GemmArgs g;
+    int width;                 // of a row of partial: n, or 2 half
+    int octets;                // of a row of C
+    int64_t all;               // octets of C
+};
+template <typename T, int SL>
+__global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
+    const GemmArgs& g = f.g;
+    constexpr int PER = 256 / SL;
+    __shared__ double sh[SL > 1 ? 16 * 256 : 1];
+    const int slot = threadIdx.x % PER, slice = threadIdx.x / PER;
+    const int64_t o = (int64_t)blockIdx.x * PER + slot;
+    const bool in_sums = o >= f.all;
+    const int64_t row = in_sums ? 0 : o / f.octets;
+    const int col = (int)(in_sums ? o - f.all : o - row * f.octets) * 8;
+    const bool gated = !in_sums && (g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE);
+    const int count = (in_sums ? g.m : g.n) - col;
+    const bool any = count > 0 && (!in_sums || g.sums);
+    const float* const p = in_sums ? g.sums + col : g.partial + row * f.width + col;
+    const int64_t step = in_sums ? g.m : (int64_t)g.m * f.width;
+    double zd[8], ud[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) zd[i] = ud[i] = 0.0;
+    if (any) {
+#pragma unroll 4
+        for (int s = slice; s < g.splits; s += SL) {
+            float v[8];
+            gm_get_some(p + s * step, count, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) zd[i] += (double)v[i];
+            if (gated) {
+                gm_get_some(p + s * step + g.half, count, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ud[i] += (double)v[i];
+            }
+        }
+    }
+    if constexpr (SL > 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sh[(i * SL + slice) * PER + slot] = zd[i], sh[((8 + i) * SL + slice) * PER + slot] = ud[i];
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                for (int s = 1; s < SL; ++s) zd[i] += sh[(i * SL + s) * PER + slot], ud[i] += sh[((8 + i) * SL + s) * PER + slot];
+        }
+    }
+    if (!any || slice != 0) return;
+    float z[8], u[8], bz[8], bu[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = (float)zd[i], u[i] = (float)ud[i];
+    if (in_sums) {
+        gm_put_some((T*)g.sums_out + col, count, z);
+    } else {
+        gm_bias8<T>(g, col, gated, bz, bu);
+        gm_finish8<T>(g, row, col, z, u, bz, bu);
+    }
+}
+
+template <typename T, bool GATED, int RF>
+hipError_t start_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
+    const int blocks = (g.n + 15) / 16;
+    if (aligned) k_skinny<T, GATED, RF, true><<<blocks, SKW * 64, 0, st>>>(g);
+    else k_skinny<T, GATED, RF, false><<<blocks, SKW * 64, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
+    if (g.mode == GEMM_GATED)
+        return g.m <= 16 ? start_skinny<T, true, 1>(g, aligned, st) : g.m <= 32 ? start_skinny<T, true, 2>(g, aligned, st) : start_skinny<T, true, 4>(g, aligned, st);
+    return g.m <= 16 ? start_skinny<T, false, 1>(g, aligned, st) : g.m <= 32 ? start_skinny<T, false, 2>(g, aligned, st) : start_skinny<T, false, 4>(g, aligned, st);
+}
+
+template <typename T>
+hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st) {
+    FinishArgs f;
+    f.g = g;
+    const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
+    f.width = gated ? 2 * g.half : g.n;
+    f.octets = (g.n + 7) / 8;
+    f.all = (int64_t)(g.partial ? g.m : 0) * f.octets;
+    const int64_t all = f.all + (g.sums ? (g.m + 7) / 8 : 0);
+    if (g.splits <= 16) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
+    else k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
+    return hipGetLastError();
+}
+
+}  // namespace srd

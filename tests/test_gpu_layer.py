@@ -1,0 +1,336 @@
+"""Layers over rows and their gradients through the C ABI against the 64-bit oracle on the same stored values.
+
+Tolerances, u = 2^-24.  Products of the stored values are exact for 16-bit types and rounded once (u) for fp32.  A matrix
+instruction adds 16 products (fp32: 2) to a sum; whatever it does inside, each of its partial sums is taken to be off by 2 u of the
+sum of magnitudes M, so K products are within steps(K) = (K / 4 + 16) u M, fp32: (2 K + 16) u M; sums split over workgroups only have
+fewer steps.  Activations: the exponential's argument is rounded twice and its constant once, 1.733 |z| u, the instruction adds 2 u, sum,
+quotient and product one each: (1.75 |z| + 8) u relative; erf is within 4 u of 1, so gelu is within 4 u |z|, its slope adds the exponential's
+z^2 / 2: (4 + 2 z^2 exp(-z^2 / 2)) u in all is below 8 u (|z| + 1).  One bound for all of them: a value is within u (1.75 |z| + 8) (|value| + |z| + 1), a
+slope the same with |slope| + 1.  Slopes are below 1.13, second derivatives below 0.8: z's own error counts that much.  A rounding to type t is off by
+eps_t / 2 of the value, or half of t's smallest step."""
+import math
+
+import pytest
+import torch
+
+import paper_2303_08999_amd as sr
+from oracle import layer_oracle as lo
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SMALLEST = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}
+
+
+class Guarded:
+    """A tensor between two strips of NaN that a call must neither use nor touch."""
+
+    def __init__(self, shape, dtype, shift=0, fill=None):
+        numel = math.prod(shape)
+        self.raw = torch.full((numel + 1024,), float("nan"), device=DEV, dtype=dtype)
+        self.lo, self.hi = 512 + shift, 512 + shift + numel
+        self.t = self.raw[self.lo:self.hi].view(shape)
+        if fill is not None:
+            self.t.copy_(fill)
+
+    def check(self):
+        assert self.raw[:self.lo].isnan().all() and self.raw[self.hi:].isnan().all(), "written outside of the tensor"
+
+
+def half_step(t, v):
+    return torch.finfo(DT[t]).eps / 2 * v.abs() + SMALLEST[t] / 2
+
+
+def steps(t, K):
+    return ((2 * K if t == "f32" else K / 4) + 16) * U
+
+
+def inputs(P, C, O, t, gated, seed, bias=True, residual=False):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)
+    wide = 2 * O if gated else O
+    d = {"x": r(P, C), "w": r(wide, C) / math.sqrt(C), "b": r(wide) / 2 if bias else None, "dy": r(P, O) / 8,
+         "res": r(P, O) if residual else None}
+    return {k: None if v is None else v.to(DT[t]) for k, v in d.items()}
+
+
+def wide64(d):
+    return {k: None if v is None else v.double() for k, v in d.items()}
+
+
+def z_error(t, e):
+    """z and what it may be off by."""
+    C = e["x"].shape[1]
+    z = lo.affine(e["x"], e["w"], e["b"])
+    M = lo.affine(e["x"].abs(), e["w"].abs(), None if e["b"] is None else e["b"].abs())
+    return z, steps(t, C) * M
+
+
+def act_error(z, v):
+    return U * (1.75 * z.abs() + 8) * (v.abs() + z.abs() + 1)
+
+
+def forward_bound(t, e, kind, gated):
+    z, ez = z_error(t, e)
+    if gated:
+        (g, u), (eg, eu) = z.chunk(2, 1), ez.chunk(2, 1)
+        v = lo.act(kind, g)
+        want = v * u
+        ev = 1.13 * eg + act_error(g, v)
+        err = ev * u.abs() + (v.abs() + ev) * eu + 2 * U * want.abs()
+    else:
+        v = lo.act(kind, z)
+        err = 1.13 * ez + (act_error(z, v) if kind else 0)
+        want = v
+        if e["res"] is not None:
+            want = v + e["res"]
+            err = err + U * want.abs()
+    return want, err + half_step(t, want.abs() + err)
+
+
+def slope_error(kind, z, ez):
+    s = lo.slope(kind, z)
+    if kind == lo.NONE:
+        return s, torch.zeros_like(z)
+    err = 0.8 * ez + U * (1.75 * z.abs() + 8) * (s.abs() + 1)
+    if kind == lo.RELU:
+        err = torch.where(z.abs() <= ez, torch.ones_like(z), torch.zeros_like(z))
+    return s, err
+
+
+def dz_bound(t, e, kind, gated):
+    if not gated and kind == lo.NONE:
+        return e["dy"], torch.zeros_like(e["dy"])
+    z, ez = z_error(t, e)
+    dy = e["dy"]
+    if gated:
+        (g, u), (eg, eu) = z.chunk(2, 1), ez.chunk(2, 1)
+        s, es = slope_error(kind, g, eg)
+        v = lo.act(kind, g)
+        ev = 1.13 * eg + (act_error(g, v) if kind else 0)
+        want = torch.cat([dy * u * s, dy * v], 1)
+        err = torch.cat([dy.abs() * (u.abs() * es + eu * (s.abs() + es)), dy.abs() * ev], 1) + 3 * U * want.abs()
+    else:
+        s, es = slope_error(kind, z, ez)
+        want = dy * s
+        err = dy.abs() * es + U * want.abs()
+    return want, err + half_step(t, want.abs() + err)
+
+
+def behind_bound(t, e, dz, edz):
+    x, w = e["x"], e["w"]
+    out = []
+    for want, err, mag, K in ((dz @ w, edz @ w.abs(), dz.abs() @ w.abs(), w.shape[0]),
+                              (dz.t() @ x, edz.t() @ x.abs(), dz.abs().t() @ x.abs(), x.shape[0]),
+                              (dz.sum(0), edz.sum(0), dz.abs().sum(0), x.shape[0])):
+        err = err + (2 * K + 16 if want.dim() == 1 else steps(t, K) / U) * U * (mag + err)
+        out.append((want, err + half_step(t, want.abs() + err)))
+    return out
+
+
+def compare(what, got, want, bound):
+    got = got.double()
+    bad = ~((got - want).abs() <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} off, worst {float(((got - want).abs() / bound).max()):.2f} of the bound"
+
+
+def run_forward(d, t, kind, gated, shift=0):
+    P, O = d["dy"].shape
+    dev = {k: None if v is None else Guarded(v.shape, v.dtype, shift, v) for k, v in d.items()}
+    y = Guarded((P, O), DT[t], shift)
+    get = lambda k: dev[k] and dev[k].t
+    if gated:
+        sr.sr_layer_gated(get("x"), get("w"), get("b"), kind, y.t)
+    else:
+        sr.sr_layer_linear(get("x"), get("w"), get("b"), kind, get("res"), y.t)
+    torch.cuda.synchronize()
+    for v in (*dev.values(), y):
+        if v is not None:
+            v.check()
+    return y.t
+
+
+def run_grad(d, t, kind, gated, shift=0, want=(True, True, True)):
+    dev = {k: None if v is None else Guarded(v.shape, v.dtype, shift, v) for k, v in d.items()}
+    wide = d["w"].shape[0]
+    out = [Guarded(s, DT[t], shift) if on else None for s, on in zip((d["x"].shape, d["w"].shape, (wide,)), want)]
+    get = lambda k: dev[k] and dev[k].t
+    call = sr.sr_layer_gated_grad if gated else sr.sr_layer_linear_grad
+    call(get("x"), get("w"), get("b"), kind, get("dy"), *(o and o.t for o in out))
+    torch.cuda.synchronize()
+    for v in (*dev.values(), *out):
+        if v is not None:
+            v.check()
+    return [o and o.t for o in out]
+
+
+def check_forward(P, C, O, t, kind, gated, seed=1, bias=True, residual=False, shift=0, spoil=None):
+    d = inputs(P, C, O, t, gated, seed, bias, residual)
+    if spoil:
+        spoil(d)
+    want, bound = forward_bound(t, wide64(d), kind, gated)
+    compare("y", run_forward(d, t, kind, gated, shift), want, bound)
+
+
+def check_grad(P, C, O, t, kind, gated, seed=1, bias=True, shift=0, spoil=None):
+    d = inputs(P, C, O, t, gated, seed, bias)
+    if spoil:
+        spoil(d)
+    e = wide64(d)
+    bounds = behind_bound(t, e, *dz_bound(t, e, kind, gated))
+    got = run_grad(d, t, kind, gated, shift)
+    for name, g, (want, bound) in zip(("dx", "dweight", "dbias"), got, bounds):
+        compare(name, g, want, bound)
+    return d, got
+
+
+# rows from one to several tiles, features below, at and above what a load, a matrix step and a tile hold
+SHAPES = [(1, 1, 1), (1, 8, 8), (1, 2048, 33), (3, 5, 7), (16, 64, 72), (17, 72, 64), (33, 40, 130), (64, 129, 31), (65, 64, 64), (100, 27, 121),
+          (127, 136, 40), (128, 64, 128), (129, 128, 129), (200, 1000, 264), (257, 200, 257), (300, 65, 1), (1000, 72, 96), (515, 1536, 520),
+          (4099, 64, 72), (90, 4100, 65), (2049, 8, 16)]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "P%dC%dO%d" % s)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_forward(gated, shape, t):
+    kind = (shape[0] + shape[1]) % 5
+    check_forward(*shape, t, kind, gated, seed=sum(shape), bias=shape[0] % 2 == 1, residual=not gated and shape[1] % 2 == 0)
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "P%dC%dO%d" % s)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_gradients(gated, shape, t):
+    check_grad(*shape, t, (shape[0] + shape[2]) % 5, gated, seed=sum(shape), bias=shape[0] % 2 == 1)
+
+
+@pytest.mark.parametrize("kind", range(5))
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_every_activation(t, gated, kind):
+    check_forward(150, 72, 88, t, kind, gated)
+    check_forward(20, 72, 88, t, kind, gated)
+    check_grad(150, 72, 88, t, kind, gated)
+
+
+@pytest.mark.parametrize("shift", [1, 4, 7])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_addresses_off_16_bytes(gated, t, shift):
+    """The header promises any address that is aligned to an element."""
+    for P in (9, 140, 300):
+        check_forward(P, 64, 72, t, lo.GELU, gated, shift=shift, residual=not gated)
+        check_grad(P, 64, 72, t, lo.SILU, gated, shift=shift)
+
+
+@pytest.mark.parametrize("shape,t", [((16400, 520, 264), "bf16"), ((8200, 264, 1030), "f16"), ((3000, 1032, 776), "f32"), ((70000, 40, 24), "bf16"),
+                                     ((66000, 64, 72), "f32"), ((2100, 2056, 2568), "f16")], ids=str)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_large_tiles_and_long_sums(gated, shape, t):
+    check_forward(*shape, t, lo.SILU, gated, residual=not gated)
+    check_grad(*shape, t, lo.GELU if not gated else lo.SILU, gated)
+    if not gated:
+        check_grad(*shape, t, lo.NONE, gated)
+
+
+def test_what_is_not_asked_for_is_not_written_and_changes_nothing():
+    for gated in (False, True):
+        for shape in ((70, 40, 24), (5000, 72, 64), (7, 64, 9)):
+            d = inputs(*shape, "f16", gated, 3)
+            every = run_grad(d, "f16", lo.SILU, gated)
+            for want in ((True, False, False), (False, True, False), (False, False, True), (True, False, True), (True, True, False)):
+                for a, b in zip(run_grad(d, "f16", lo.SILU, gated, want=want), every):
+                    assert a is None or torch.equal(a, b)
+
+
+def test_no_rows():
+    for gated in (False, True):
+        d = inputs(0, 40, 24, "bf16", gated, 1)
+        assert run_forward(d, "bf16", lo.GELU, gated).shape == (0, 24)
+        dx, dw, db = run_grad(d, "bf16", lo.GELU, gated)
+        assert dx.shape == (0, 40) and (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+@pytest.mark.parametrize("P,C", [(9, 100), (200, 100), (200, 128), (700, 2000)])
+def test_infinities_and_nan_stay_in_their_rows(gated, P, C):
+    """A row's NaN reaches that row of y alone; of a padded K or a clamped row nothing gets anywhere."""
+    for t in ("f32", "bf16"):
+        d = inputs(P, C, 70, t, gated, 5)
+        clean = run_forward(d, t, lo.SILU, gated).clone()
+        d["x"][3, C - 1] = float("nan")
+        d["x"][P - 1, 0] = float("inf")
+        y = run_forward(d, t, lo.SILU, gated)
+        rows = torch.ones(P, dtype=torch.bool, device=DEV)
+        rows[3] = rows[P - 1] = False
+        assert torch.equal(y[rows], clean[rows]) and y[3].isnan().all()
+        d["w"][5] = float("nan")                                     # ... and a weight's row that column
+        y = run_forward(d, t, lo.SILU, gated)
+        cols = torch.arange(70, device=DEV) != 5
+        assert torch.equal(y[rows][:, cols], clean[rows][:, cols]) and y[:, 5].isnan().all()
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_large_and_small_values(t):
+    """Saturated activations, and gradients as small as the type holds."""
+    def spoil(d):
+        d["x"] *= 30
+    for kind in range(5):
+        check_forward(90, 64, 40, t, kind, False, spoil=spoil)
+        check_grad(90, 64, 40, t, kind, False, spoil=spoil)
+
+    def faint(d):
+        d["dy"] *= 2.0 ** -16 if t == "f16" else 2.0 ** -80
+    check_grad(90, 64, 40, t, lo.GELU, False, spoil=faint)
+    check_grad(90, 64, 40, t, lo.SILU, True, spoil=faint)
+
+
+def test_runs_give_the_same_bits():
+    for shape in ((3000, 72, 64), (40, 520, 33), (9000, 256, 256)):
+        for gated in (False, True):
+            d = inputs(*shape, "bf16", gated, 8)
+            a, b = run_forward(d, "bf16", lo.GELU, gated), run_forward(d, "bf16", lo.GELU, gated)
+            assert torch.equal(a, b)
+            for x, y in zip(run_grad(d, "bf16", lo.GELU, gated), run_grad(d, "bf16", lo.GELU, gated)):
+                assert torch.equal(x, y)
+
+
+def test_images_as_rows():
+    """[N][H][W][C] is what its rows are."""
+    d = inputs(2 * 5 * 7, 24, 40, "f16", False, 4)
+    y, y4 = torch.empty(70, 40, device=DEV, dtype=torch.float16), torch.empty(2, 5, 7, 40, device=DEV, dtype=torch.float16)
+    sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.RELU, None, y)
+    sr.sr_layer_linear(d["x"].view(2, 5, 7, 24), d["w"], d["b"], lo.RELU, None, y4)
+    assert torch.equal(y.view(2, 5, 7, 40), y4)
+
+
+def test_other_streams_and_captured_graphs():
+    """On a stream of the caller's; captured with workspaces of their own and replayed with other work in between."""
+    P, C, O = 3000, 136, 72
+    d = inputs(P, C, O, "bf16", True, 6)
+    want = [run_forward(d, "bf16", lo.SILU, True)] + run_grad(d, "bf16", lo.SILU, True)
+    outs = [torch.zeros_like(v) for v in want]
+    ws = torch.empty(sr.sr_layer_gated_grad_workspace_bytes(P, C, O, torch.bfloat16), device=DEV, dtype=torch.uint8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.SILU, outs[0], stream=side)
+    sr.sr_layer_gated_grad(d["x"], d["w"], d["b"], lo.SILU, d["dy"], *outs[1:], workspace=ws, stream=side.cuda_stream)
+    side.synchronize()
+    for a, b in zip(outs, want):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.SILU, outs[0])
+        sr.sr_layer_gated_grad(d["x"], d["w"], d["b"], lo.SILU, d["dy"], *outs[1:], workspace=ws)
+    for i in range(4):
+        for o in outs:
+            o.zero_()
+        ws.fill_(255)                                                # what is there before a call is meaningless
+        d["x"].mul_(1.0 if i % 2 else -1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = [run_forward(d, "bf16", lo.SILU, True)] + run_grad(d, "bf16", lo.SILU, True)
+        for a, b in zip(outs, now):
+            assert torch.equal(a, b), f"replay {i}"
