@@ -56,9 +56,10 @@ struct GemmArgs {
     void* sums_out;            // ... or, of one split, [m] in the operands' type
 };
 
-// Tiles: 0: 64 x 64, 1: 128 x 128, 2: 256 x 256 (operands on 16-byte pieces only).
+// Tiles: 0: 64 x 64, 1: 128 x 128, 2: 256 x 128, 3: 256 x 256 (2 and 3: operands on 16-byte pieces only).
 template <typename T> hipError_t launch_gemm(const GemmArgs& g, int layout, bool aligned, int tile, hipStream_t st);
-inline int gemm_tile_rows(int tile) { return 64 << tile; }
+inline int gemm_tile_rows(int tile) { return tile < 2 ? 64 << tile : 256; }
+inline int gemm_tile_cols(int tile) { return tile < 1 ? 64 : tile < 3 ? 128 : 256; }
 
 // z of the split sums, and what the epilogue would have done: elements [m][n], sums over the splits in double
 template <typename T> hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st);
@@ -68,53 +69,58 @@ constexpr int SKINNY_ROWS = 64;
 
 // ---- values ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float act_exp(float z) { return __builtin_amdgcn_exp2f(z * LOG2E); }
-__device__ __forceinline__ float sigmoid_of(float z) { return 1.0f / (1.0f + act_exp(-z)); }
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * (1.0f + erff(z * 0.70710678118654752440f)); }
-// z to act(z), or to act'(z); the branches are uniform
-__device__ __forceinline__ void act8(int act, float z[8]) {
+__device__ __forceinline__ float sigmoid_of(float z) { return __builtin_amdgcn_rcpf(1.0f + act_exp(-z)); }
+// The normal distribution's integral up to z, and its density without 1 / sqrt(2 pi), by Abramowitz and Stegun 7.1.26: with x = |z| / sqrt 2, t =
+// 1 / (1 + p x), erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) within 1.5e-7.  A third of the time of erff, and the exponential is the density.
+__device__ __forceinline__ float normal_cdf(float z, float& density) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752440f, 1.0f));
+    density = __builtin_amdgcn_exp2f(z * z * (-0.5f * LOG2E));
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f) * density;
+    return z < 0.0f ? q : 1.0f - q;
+}
+template <int U, typename F> __device__ __forceinline__ void each8(float (&z)[U][8], F f) {
+#pragma unroll
+    for (int r = 0; r < U; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(z[r][i], r, i);
+}
+// z to act(z); the branches are uniform
+template <int U> __device__ __forceinline__ void act8(int act, float (&z)[U][8]) {
     if (act == SR_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = z[i] <= 0.0f ? 0.0f : z[i];        // NaN stays
+        each8<U>(z, [](float& v, int, int) { v = v <= 0.0f ? 0.0f : v; });              // NaN stays
     } else if (act == SR_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] *= normal_cdf(z[i]);
+        each8<U>(z, [](float& v, int, int) { float d; v *= normal_cdf(v, d); });
     } else if (act == SR_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = z[i] / (1.0f + act_exp(-z[i]));
+        each8<U>(z, [](float& v, int, int) { v *= sigmoid_of(v); });
     } else if (act == SR_ACT_SIGMOID) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = sigmoid_of(z[i]);
+        each8<U>(z, [](float& v, int, int) { v = sigmoid_of(v); });
     }
 }
-// values and slopes of z
-__device__ __forceinline__ void slope8(int act, const float z[8], float value[8], float slope[8]) {
+// z to act'(z), and the values
+template <int U> __device__ __forceinline__ void slope8(int act, float (&z)[U][8], float (&value)[U][8]) {
     if (act == SR_ACT_RELU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) value[i] = z[i] <= 0.0f ? 0.0f : z[i], slope[i] = z[i] > 0.0f ? 1.0f : 0.0f;
+        each8<U>(z, [&](float& v, int r, int i) { value[r][i] = v <= 0.0f ? 0.0f : v, v = v > 0.0f ? 1.0f : 0.0f; });
     } else if (act == SR_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = normal_cdf(z[i]);
-            value[i] = z[i] * c;
-            slope[i] = fmaf(z[i] * 0.39894228040143267794f, act_exp(-0.5f * z[i] * z[i]), c);
-        }
+        each8<U>(z, [&](float& v, int r, int i) {
+            float d;
+            const float c = normal_cdf(v, d);
+            value[r][i] = v * c;
+            v = fmaf(v * 0.39894228040143267794f, d, c);
+        });
     } else if (act == SR_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float s = sigmoid_of(z[i]);
-            value[i] = z[i] * s;
-            slope[i] = s * fmaf(z[i], 1.0f - s, 1.0f);
-        }
+        each8<U>(z, [&](float& v, int r, int i) {
+            const float s = sigmoid_of(v);
+            value[r][i] = v * s;
+            v = s * fmaf(v, 1.0f - s, 1.0f);
+        });
     } else if (act == SR_ACT_SIGMOID) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float s = sigmoid_of(z[i]);
-            value[i] = s;
-            slope[i] = s * (1.0f - s);
-        }
+        each8<U>(z, [&](float& v, int r, int i) {
+            const float s = sigmoid_of(v);
+            value[r][i] = s;
+            v = s * (1.0f - s);
+        });
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) value[i] = z[i], slope[i] = 1.0f;
+        each8<U>(z, [&](float& v, int r, int i) { value[r][i] = v, v = 1.0f; });
     }
 }
 
@@ -225,65 +231,16 @@ template <typename T, int MT> __device__ __forceinline__ void gm_mul(typename Ac
         else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8g, a), __builtin_bit_cast(bf8g, b), c, 0, 0, 0);
     }
 }
-template <typename T> __device__ __forceinline__ float gm_sum_piece(u32x4g a) {
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            s += __uint_as_float(a[i]);
-        } else if constexpr (__is_same(T, __half)) {
-            using half2g = __attribute__((ext_vector_type(2))) _Float16;
-            const half2g h = __builtin_bit_cast(half2g, (unsigned)a[i]);
-            s += (float)h[0] + (float)h[1];
-        } else {
-            s += __uint_as_float(a[i] << 16) + __uint_as_float(a[i] & 0xffff0000u);
-        }
-    }
-    return s;
-}
-
-// What a layer does to 8 columns from `col` on of row `row` of C: z in, the outputs stored.  For the gated forms u is the same
-// columns of the second half.
-template <typename T>
-__device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int col, float z[8], float u[8], const float bz[8], const float bu[8]) {
-    const int count = g.n - col;
-    float e[8];
-    if (g.extra) gm_get_some((const T*)g.extra + row * g.ld_extra + col, count, e);
-    T* const out = (T*)g.out + row * g.ld_out + col;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] += bz[i];
-    if (g.mode == GEMM_STORE) {
-        act8(g.act, z);
-        if (g.extra) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] += e[i];
-        }
-        gm_put_some(out, count, z);
-    } else if (g.mode == GEMM_SLOPE) {
-        float value[8], slope[8];
-        slope8(g.act, z, value, slope);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = e[i] * slope[i];
-        gm_put_some(out, count, z);
+// of the one or two values in 32 bits of a fragment
+template <typename T> __device__ __forceinline__ float gm_sum(unsigned v) {
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(v);
+    } else if constexpr (__is_same(T, __half)) {
+        using half2g = __attribute__((ext_vector_type(2))) _Float16;
+        const half2g h = __builtin_bit_cast(half2g, v);
+        return (float)h[0] + (float)h[1];
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] += bu[i];
-        if (g.mode == GEMM_GATED) {
-            act8(g.act, z);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= u[i];
-            gm_put_some(out, count, z);
-        } else {
-            float value[8], slope[8];
-            slope8(g.act, z, value, slope);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[i] = e[i] * u[i] * slope[i];
-                u[i] = e[i] * value[i];
-            }
-            gm_put_some(out, count, z);
-            gm_put_some(out + g.half, count, u);
-        }
+        return __uint_as_float(v << 16) + __uint_as_float(v & 0xffff0000u);
     }
 }
 template <typename T>
@@ -295,4 +252,79 @@ __device__ __forceinline__ void gm_bias8(const GemmArgs& g, int col, bool gated,
     if (gated) gm_get_some((const T*)g.bias + g.half + col, g.n - col, bu);
 }
 
+// 8 values of a row as they are stored, of which `count` are there
+template <typename T> struct Raw8 {
+    u32x4g v[sizeof(T) / 2];
+    __device__ __forceinline__ void get(const T* p, int count) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = gm_piece(p + i * (16 / sizeof(T)), count - i * (int)(16 / sizeof(T)));
+    }
+    __device__ __forceinline__ void values(float e[8]) const {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(T) == 4) {
+                    e[4 * i + j] = __uint_as_float(v[i][j]);
+                } else if constexpr (__is_same(T, __half)) {
+                    using half2g = __attribute__((ext_vector_type(2))) _Float16;
+                    const half2g h = __builtin_bit_cast(half2g, (unsigned)v[i][j]);
+                    e[2 * j] = (float)h[0], e[2 * j + 1] = (float)h[1];
+                } else {
+                    e[2 * j] = __uint_as_float(v[i][j] << 16), e[2 * j + 1] = __uint_as_float(v[i][j] & 0xffff0000u);
+                }
+            }
+    }
+};
+
+// What a layer does to 8 U values of C, z in, output out; e: of `extra`.  For the gated forms u is the same columns of the second half, and
+// becomes the second output.
+template <bool GATED, int U>
+__device__ __forceinline__ void gm_finish(const GemmArgs& g, float (&z)[U][8], float (&u)[U][8], const float (&e)[U][8], const float bz[8], const float bu[8]) {
+#pragma unroll
+    for (int r = 0; r < U; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            z[r][i] += bz[i];
+            if constexpr (GATED) u[r][i] += bu[i];
+        }
+    if (g.mode == (GATED ? GEMM_GATED : GEMM_STORE)) {
+        act8<U>(g.act, z);
+#pragma unroll
+        for (int r = 0; r < U; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (GATED) z[r][i] *= u[r][i];
+                else z[r][i] += e[r][i];
+            }
+    } else {
+        float value[U][8];
+        slope8<U>(g.act, z, value);
+#pragma unroll
+        for (int r = 0; r < U; ++r)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (GATED) {
+                    z[r][i] *= e[r][i] * u[r][i];
+                    u[r][i] = e[r][i] * value[r][i];
+                } else {
+                    z[r][i] *= e[r][i];
+                }
+            }
+    }
+}
+// The same for 8 columns from `col` on of row `row`, with the loads and the stores
+template <typename T, bool GATED>
+__device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int col, float (&z)[1][8], float (&u)[1][8]) {
+    const int count = g.n - col;
+    float e[1][8], bz[8], bu[8];
+    gm_bias8<T>(g, col, GATED, bz, bu);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[0][i] = 0.0f;
+    if (g.extra) gm_get_some((const T*)g.extra + row * g.ld_extra + col, count, e[0]);
+    gm_finish<GATED, 1>(g, z, u, e, bz, bu);
+    T* const out = (T*)g.out + row * g.ld_out + col;
+    gm_put_some(out, count, z[0]);
+    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[0]);
+}
 }  // namespace srd

@@ -12,14 +12,26 @@ using lds_f4g = __attribute__((address_space(3))) f32x4g;
 using lds_s4g = __attribute__((address_space(3))) s16x4g;
 using lds_floatg = __attribute__((address_space(3))) float;
 
-// MT: rows of a matrix instruction.  A wavefront makes WM x WN.
-template <int TILE> struct GemmShape;
-template <> struct GemmShape<0> { static constexpr int BM = 64, BN = 64, WM = 32, WN = 32, MT = 16, OCC = 3; };
-template <> struct GemmShape<1> { static constexpr int BM = 128, BN = 128, WM = 64, WN = 64, MT = 32, OCC = 2; };
-template <> struct GemmShape<2> { static constexpr int BM = 256, BN = 256, WM = 128, WN = 64, MT = 32, OCC = 2; };
+// MT: rows of a matrix instruction.  A wavefront makes WM x WN; the matrix instructions read (WM + WN) / (WM WN) of a tile's values from LDS, so that
+// 64 x 64 need more of it than it gives, 128 x 128 three quarters.  PIPE: the loop for one wavefront a SIMD.
+template <int TILE, typename T> struct GemmShape;
+template <typename T> struct GemmShape<0, T> { static constexpr int BM = 64, BN = 64, WM = 32, WN = 32, MT = 16, OCC = 3; static constexpr bool PIPE = false; };
+template <typename T> struct GemmShape<1, T> { static constexpr int BM = 128, BN = 128, WM = 64, WN = 64, MT = 32, OCC = 2; static constexpr bool PIPE = false; };
+template <typename T> struct GemmShape<2, T> { static constexpr int BM = 256, BN = 128, WM = 128, WN = 64, MT = sizeof(T) == 2 ? 16 : 32, OCC = 1; static constexpr bool PIPE = true; };
+// 16-bit types: instructions of 16 rows (8192^3, fp16: 801 us, of 32 rows 876); fp32: of 32 (8192 x 4096 x 4096: 1857 us, of 16 rows 2115)
+template <typename T> struct GemmShape<3, T> { static constexpr int BM = 256, BN = 256, WM = 128, WN = 128, MT = sizeof(T) == 2 ? 16 : 32, OCC = 1; static constexpr bool PIPE = true; };
+
+template <int TILE, typename T>
+constexpr int gemm_threads = GemmShape<TILE, T>::BM / GemmShape<TILE, T>::WM * (GemmShape<TILE, T>::BN / GemmShape<TILE, T>::WN) * 64;
+
+// What this wavefront has sent to LDS is there, then what all of them have, and all of them have read what they asked for.
+__device__ __forceinline__ void landed() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+}
 
 // One operand's part in LDS: R rows, 128 bytes of k.
-template <typename T, int R, int NW, bool RC, int MT>
+template <typename T, int R, int NW, bool RC, int MT, bool GATED = false>
 struct Operand {
     static constexpr int E = 16 / sizeof(T), BK = 128 / sizeof(T), BYTES = R * 128, LOADS = BYTES / 1024 / NW;
     static constexpr int RB = R * sizeof(T);              // bytes of a k in LDS (RC)
@@ -32,49 +44,51 @@ struct Operand {
         else return MT == 32 ? (k >> 2 & 1) << 1 : k >> 2 & 3;
     }
 
-    const char* base[LOADS];    // uniform: of the first row (KC) or k (RC) that load i takes
-    int off[LOADS];             // of this lane from it, bytes
-    int place;                  // KC: k of its piece; RC: k of the lane within the load
+    const char* base;           // uniform: of the tile's first row and k
+    int64_t second;             // gated: from there to the same row of the second half, bytes
+    unsigned off[LOADS];        // of this lane's piece of load i from it, bytes (KC: at most 256 rows of 2^17 values)
+    int place;                  // KC: k of its piece; RC: k of the lane within load 0
     int row[RC ? LOADS : 1];    // RC: first of its piece's rows, from the tile's first
 
-    // Row r of the tile is row `row_of(r)` of the stored matrix, and none is past `last`.
+    // Row r of the tile is row `row0 + row_of(r)` of the stored matrix (KC), which is there.
     template <typename RowOf>
-    __device__ __forceinline__ void init(const void* p, int64_t ld, int row0, int rows, int wave, int lane, int k0, bool aligned, RowOf row_of) {
-        const char* q = (const char*)p;
+    __device__ __forceinline__ void init(const void* p, int64_t ld, int row0, int rows, int wave, int lane, int k0, bool aligned, int64_t half, RowOf row_of) {
+        second = half * ld * (int)sizeof(T);
+        base = (const char*)p + (RC ? (int64_t)k0 * ld + row0 : (int64_t)row0 * ld + k0) * (int)sizeof(T);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int pos = (i * NW + wave) * 1024;
+            const int pos = (i * NW + wave) * 1024 + lane * 16;
             if constexpr (!RC) {
-                const int r = pos / 128 + lane / 8;
-                const int first = row_of(pos / 128), mine = row_of(r);
-                const int piece = (lane & 7) ^ (lane / 8);                   // a load's first row is a multiple of 8
-                base[i] = q + ((int64_t)first * ld + k0) * (int)sizeof(T);
-                off[i] = (int)((mine - first) * ld) * (int)sizeof(T) + piece * 16;
-                place = piece * E;
+                const int r = pos / 128, piece = (lane & 7) ^ (r & 7);
+                off[i] = (unsigned)row_of(r) * (unsigned)(ld * (int)sizeof(T)) + piece * 16;
+                if (i == 0) place = piece * E;
             } else {
-                const int k = (pos + lane * 16) / RB, k1 = pos / RB, slot = (pos + lane * 16) % RB;
+                const int k = pos / RB, slot = pos % RB;
                 const int chunk = (slot / CB) ^ turn(k);
                 int r = chunk * 16 + (slot % CB) / (int)sizeof(T);
                 row[i] = r;
                 if (aligned) r = row0 + r < rows ? r : (rows - 1) / E * E - row0;      // what is past the last row is not stored
-                base[i] = q + ((int64_t)(k0 + k1) * ld + row0) * (int)sizeof(T);
-                off[i] = (int)((k - k1) * ld + r) * (int)sizeof(T);
+                off[i] = ((unsigned)k * (unsigned)ld + (unsigned)r) * (unsigned)sizeof(T);
                 if (i == 0) place = k;
             }
         }
     }
-    __device__ __forceinline__ void advance(int64_t bytes) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) base[i] += bytes;
+    __device__ __forceinline__ void advance(int64_t bytes) { base += bytes; }
+    // gated: whether load i takes rows of the second half (a load's 8 rows are of one)
+    static __device__ __forceinline__ bool other(int i, int wave) { return GATED && ((i * NW + wave) * 8 / MT & 1); }
+    __device__ __forceinline__ const char* from(int i, int wave) const { return GATED && other(i, wave) ? base + second : base; }
+    // Straight to LDS; the whole of it is there.  Written out, because the compiler lets every turning LDS read wait for all loads to LDS that it
+    // knows of, whatever they write: landed() is what waits for these.  The instruction takes the place from m0, a wait state behind its writing.
+    __device__ __forceinline__ void fetch(char* lds, int wave, int i) const {
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                     :: "v"(off[i]), "s"(from(i, wave)), "{m0}"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024)) : "memory");
     }
-    // Straight to LDS; the whole of it is there.
     __device__ __forceinline__ void fetch(char* lds, int wave) const {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            __builtin_amdgcn_global_load_lds((gl_void)(base[i] + (unsigned)off[i]), (lds_void)(lds + (i * NW + wave) * 1024), 16, 0, 0);
+        for (int i = 0; i < LOADS; ++i) fetch(lds, wave, i);
     }
     // By way of registers: `k` values of k are left, rows behind the last are zeros where pieces may be cut
-    __device__ __forceinline__ void load(u32x4g v[LOADS], int k, int row0, int rows, bool aligned) const {
+    __device__ __forceinline__ void load(u32x4g v[LOADS], int wave, int k, int row0, int rows, bool aligned) const {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             int count;
@@ -84,8 +98,9 @@ struct Operand {
                 const int at = place + i * (NW * 1024 / RB);
                 count = at >= k ? 0 : aligned ? E : rows - row0 - row[i];
             }
-            if (aligned) v[i] = gm_cut<T>(count > 0 ? *(const u32x4g*)(base[i] + off[i]) : u32x4g{0, 0, 0, 0}, count);
-            else v[i] = gm_piece((const T*)(base[i] + off[i]), count);
+            const char* const p = from(i, wave) + off[i];
+            if (aligned) v[i] = gm_cut<T>(count > 0 ? *(const u32x4g*)p : u32x4g{0, 0, 0, 0}, count);
+            else v[i] = gm_piece((const T*)p, count);
         }
     }
     __device__ __forceinline__ void park(char* lds, int wave, int lane, const u32x4g v[LOADS]) const {
@@ -142,16 +157,16 @@ struct Reader {
 };
 
 template <typename T, int LAYOUT, bool GATED, bool ALIGNED, int TILE>
-__global__ __launch_bounds__(GemmShape<TILE>::BM / GemmShape<TILE>::WM * (GemmShape<TILE>::BN / GemmShape<TILE>::WN) * 64, GemmShape<TILE>::OCC)
+__global__ __launch_bounds__((gemm_threads<TILE, T>), (GemmShape<TILE, T>::OCC))
 void k_gemm(const GemmArgs g) {
-    using S = GemmShape<TILE>;
+    using S = GemmShape<TILE, T>;
     constexpr int BM = S::BM, BN = S::BN, WM = S::WM, WN = S::WN, MT = S::MT;
     constexpr int NWN = BN / WN, NW = BM / WM * NWN, FM = WM / MT, FN = WN / MT;
     constexpr bool ARC = LAYOUT == GEMM_RC_RC, BRC = LAYOUT != GEMM_KC_KC;
     using OpA = Operand<T, BM, NW, ARC, MT>;
-    using OpB = Operand<T, BN, NW, BRC, MT>;
+    using OpB = Operand<T, BN, NW, BRC, MT, GATED>;
     constexpr int BK = OpA::BK, STEPS = 8 * MT / 64;
-    constexpr int PATCH = 32 * (WN + 4) * 4;              // a wavefront's part of the way out
+    constexpr int PR = S::PIPE ? 64 : 32, STRIDE = WN + 4, PATCH = PR * STRIDE * 4;      // a wavefront's part of the way out: rows, bytes
     constexpr int STAGE = OpA::BYTES + OpB::BYTES, LDS = 2 * STAGE > NW * PATCH ? 2 * STAGE : NW * PATCH;
     __shared__ __align__(1024) char lds[LDS];
     using Acc = typename AccOf<MT>::type;
@@ -175,11 +190,11 @@ void k_gemm(const GemmArgs g) {
 
     OpA oa;
     OpB ob;
-    oa.init(g.a, g.lda, m0, g.m, wave, lane, k0, ALIGNED, [&](int r) { return m0 + r < g.m ? m0 + r : g.m - 1; });
+    oa.init(g.a, g.lda, m0, g.m, wave, lane, k0, ALIGNED, 0, [&](int r) { return m0 + r < g.m ? r : g.m - 1 - m0; });
     // gated: every MT rows of the first half are followed by the same MT of the second
-    ob.init(g.b, g.ldb, n0, g.n, wave, lane, k0, ALIGNED, [&](int r) {
-        const int c = n0 + (GATED ? r / (2 * MT) * MT + r % MT : r);
-        return (c < g.n ? c : g.n - 1) + (GATED && (r & MT) ? g.half : 0);
+    ob.init(g.b, g.ldb, n0, g.n, wave, lane, k0, ALIGNED, g.half, [&](int r) {
+        const int c = GATED ? r / (2 * MT) * MT + r % MT : r;
+        return n0 + c < g.n ? c : g.n - 1 - n0;
     });
     const int64_t step_a = (ARC ? g.lda * BK : (int64_t)BK) * (int)sizeof(T), step_b = (BRC ? g.ldb * BK : (int64_t)BK) * (int)sizeof(T);
 
@@ -191,9 +206,22 @@ void k_gemm(const GemmArgs g) {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = Acc(0.0f);
-    float sum[ARC ? FM : 1];
+    // Sums of A over k (dz over the rows): by a matrix instruction with ones (every n the same), or, where that has no registers left and for
+    // fp32, by each lane for its k between the matrix instructions
+    constexpr bool ONES = sizeof(T) == 2 && !S::PIPE;
+    using Sum = std::conditional_t<ONES, Acc, float>;
+    Sum sum[ARC ? FM : 1];
 #pragma unroll
-    for (int i = 0; i < (ARC ? FM : 1); ++i) sum[i] = 0.0f;
+    for (int i = 0; i < (ARC ? FM : 1); ++i) sum[i] = Sum(0.0f);
+    auto add_sum = [&](int i, u32x4g f) {
+        constexpr unsigned one = __is_same(T, __half) ? 0x3c003c00u : 0x3f803f80u;
+        if constexpr (ONES) {
+            gm_mul<T, MT>(sum[i], u32x4g{one, one, one, one}, f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[i] += gm_sum<T>(f[j]);
+        }
+    };
 
     auto multiply = [&](const char* s, bool sums) {
 #pragma unroll
@@ -210,7 +238,7 @@ void k_gemm(const GemmArgs g) {
             if constexpr (ARC)
                 if (sums)
 #pragma unroll
-                    for (int i = 0; i < FM; ++i) sum[i] += gm_sum_piece<T>(fa[i]);
+                    for (int i = 0; i < FM; ++i) add_sum(i, fa[i]);
         }
     };
 
@@ -225,8 +253,8 @@ void k_gemm(const GemmArgs g) {
                 u32x4g va[OpA::LOADS], vb[OpB::LOADS];
                 oa.advance(step_a * full);
                 ob.advance(step_b * full);
-                oa.load(va, tail, m0, g.m, true);
-                ob.load(vb, tail, n0, g.n, true);
+                oa.load(va, wave, tail, m0, g.m, true);
+                ob.load(vb, wave, tail, n0, g.n, true);
                 oa.park(lds, wave, lane, va);
                 ob.park(lds + OpA::BYTES, wave, lane, vb);
                 oa.advance(-step_a * full);
@@ -238,9 +266,75 @@ void k_gemm(const GemmArgs g) {
                 ob.advance(step_b);
                 --left;
             }
+            if constexpr (S::PIPE) {
+                // One wavefront a SIMD: while the matrix instructions of a step go on it reads the fragments of the next.  In a tile's last step everyone has read all of it: the tile behind the next may overwrite
+                // it, and the next one, started a tile's time before, is there.
+                static_assert(STEPS >= 2 && STEPS % 2 == 0, "fragments of two steps in turn");
+                constexpr int NM = FM * FN, NR = FM + FN, NL = OpA::LOADS + OpB::LOADS;
+                u32x4g fa[2][FM], fb[2][FN];
+                auto read = [&](int into, const char* s, int step, int q) {
+                    if (q < FM) fa[into][q] = ra(s, q, step);
+                    else fb[into][q - FM] = rb(s + OpA::BYTES, q - FM, step);
+                };
+                // The reads in the first half of a step, so that they are there when it ends; the loads all through it: one in every fourth instruction of
+                // 16 rows, 8192^3 767 us; in every second 791; half of them in the step after 827.
+                auto step = [&](int now, const char* s, int next, auto load) {
+#pragma unroll
+                    for (int q = 0; q < NM; ++q) {
+                        gm_mul<T, MT>(acc[q / FN][q % FN], fb[now][q % FN], fa[now][q / FN]);
+                        if constexpr (SUMS) {
+#pragma unroll
+                            for (int d = q * 4 * FM / NM; d < (q + 1) * 4 * FM / NM; ++d) sum[d / 4] += gm_sum<T>(fa[now][d / 4][d % 4]);
+                        }
+                        const int r0 = 2 * q * NR / NM, r1 = 2 * (q + 1) * NR / NM, l0 = q * NL / NM, l1 = (q + 1) * NL / NM;
+                        if ((r1 > r0 && r0 < NR) || l1 > l0) {
+                            __builtin_amdgcn_sched_barrier(0);       // this order is kept
+#pragma unroll
+                            for (int r = r0; r < r1; ++r)
+                                if (r < NR) read(now ^ 1, s, next, r);
+#pragma unroll
+                            for (int l = l0; l < l1; ++l) load(l);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
+                };
+                auto none = [](int) {};
+                auto fetch = [&](char* s, int q) {
+                    if (q < OpA::LOADS) oa.fetch(s, wave, q);
+                    else ob.fetch(s + OpA::BYTES, wave, q - OpA::LOADS);
+                };
+                auto advance = [&] {
+                    oa.advance(step_a);
+                    ob.advance(step_b);
+                };
+                // `later`: the tile behind the next is still to be fetched
+                auto tile = [&](auto later) {
+                    char *const now = lds + buf * STAGE, *const next = lds + (buf ^ 1) * STAGE;
+#pragma unroll
+                    for (int i = 0; i + 1 < STEPS; ++i) step(i & 1, now, i + 1, none);
+                    landed();
+                    step(1, next, 0, [&](int q) {
+                        if constexpr (decltype(later)::value) fetch(now, q);
+                    });
+                    advance();
+                    buf ^= 1;
+                };
+                landed();
+                if (full + (tail ? 1 : 0) > 0) {
+#pragma unroll
+                    for (int q = 0; q < NR; ++q) read(0, lds, 0, q);
+                    if (left > 0) {
+#pragma unroll
+                        for (int q = 0; q < NL; ++q) fetch(lds + STAGE, q);
+                        advance();
+                        for (; left > 1; --left) tile(std::true_type{});
+                        tile(std::false_type{});
+                    }
+                    tile(std::false_type{});
+                }
+            } else
             for (int t = full + (tail ? 1 : 0); t > 0; --t) {
-                __builtin_amdgcn_s_waitcnt(0);           // this wavefront's part of the tile is in LDS
-                __syncthreads();                         // everyone's is, and nobody reads the other buffer any more
+                landed();                                // everyone's part of the tile is in LDS, and nobody reads the other buffer any more
                 char* const other = lds + (buf ^ 1) * STAGE;
                 if (left > 0) {
                     oa.fetch(other, wave);
@@ -256,8 +350,8 @@ void k_gemm(const GemmArgs g) {
             const int tiles = full + (tail ? 1 : 0);
             u32x4g va[OpA::LOADS], vb[OpB::LOADS];
             auto load = [&](int t) {
-                oa.load(va, kn - t * BK, m0, g.m, false);
-                ob.load(vb, kn - t * BK, n0, g.n, false);
+                oa.load(va, wave, kn - t * BK, m0, g.m, false);
+                ob.load(vb, wave, kn - t * BK, n0, g.n, false);
                 oa.advance(step_a);
                 ob.advance(step_b);
             };
@@ -284,15 +378,21 @@ void k_gemm(const GemmArgs g) {
     __syncthreads();
 
     if constexpr (ARC) {
-        if (sums) {                                       // over the lanes that hold other k of the same rows
+        if (sums) {
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
+                float v;
+                if constexpr (ONES) {
+                    v = sum[i][0];
+                } else {
+                    v = sum[i];                            // over the lanes that hold other k of the same rows
 #pragma unroll
-                for (int d = 32; d >= MT; d >>= 1) sum[i] += __shfl_xor(sum[i], d);
+                    for (int d = 32; d >= MT; d >>= 1) v += __shfl_xor(v, d);
+                }
                 const int m = m0 + wm + i * MT + lane;
                 if (lane < MT && m < g.m) {
-                    if (g.sums) g.sums[(int64_t)split * g.m + m] = sum[i];
-                    else gm_put((T*)g.sums_out + m, sum[i]);
+                    if (g.sums) g.sums[(int64_t)split * g.m + m] = v;
+                    else gm_put((T*)g.sums_out + m, v);
                 }
             }
         }
@@ -300,13 +400,25 @@ void k_gemm(const GemmArgs g) {
 
     if (g.mode == GEMM_PARTIAL ? !g.partial : !g.out) return;
 
-    // The way out: 32 rows of the wavefront's part at a time, lane by lane 8 columns of a row.
-    constexpr int STRIDE = WN + 4, OUT = GATED ? WN / 2 : WN, LR = OUT / 8, RI = 64 / LR, PF = 32 / MT;
+    // The way out: PR rows of the wavefront's part at a time, a lane 8 columns of U rows, what is to be added to them or multiplied with on its way
+    // while the U rows before are finished.
+    constexpr int OUT = GATED ? WN / 2 : WN, LR = OUT / 8, RI = 64 / LR, PF = PR / MT, U = PR / RI < 4 ? PR / RI : 4, CHUNKS = PR / RI / U;
     float* const patch = (float*)(lds + wave * PATCH);
     const int lc = lane % LR * 8, lr = lane / LR;
     // in the patch a wavefront's columns come as MT of the first half, MT of the second
     const int pc = GATED ? lc / MT * 2 * MT + lc % MT : lc;
-    const int col = n0 + (GATED ? wn / 2 : wn) + lc;
+    const int col = n0 + (GATED ? wn / 2 : wn) + lc, count = g.n - col;
+    const int row = m0 + wm + lr;
+    const bool extra = g.extra && g.mode != GEMM_PARTIAL;
+    Raw8<T> next[U];
+    auto ask = [&](int c) {
+#pragma unroll
+        for (int r = 0; r < U; ++r) {
+            const int m = row + (c * U + r) * RI;
+            next[r].get((const T*)g.extra + (int64_t)m * g.ld_extra + col, m < g.m ? count : 0);
+        }
+    };
+    if (extra) ask(0);
     float bz[8], bu[8];
     if (g.mode != GEMM_PARTIAL) gm_bias8<T>(g, col, GATED, bz, bu);
 #pragma unroll
@@ -326,18 +438,44 @@ void k_gemm(const GemmArgs g) {
             }
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-        for (int it = 0; it < 32 / RI; ++it) {
-            const int r = it * RI + lr, m = m0 + wm + p * 32 + r;
-            float z[8], u[8];
-            *(f32x4g*)z = *(const f32x4g*)(patch + r * STRIDE + pc);
-            *(f32x4g*)(z + 4) = *(const f32x4g*)(patch + r * STRIDE + pc + 4);
-            if constexpr (GATED) {
-                *(f32x4g*)u = *(const f32x4g*)(patch + r * STRIDE + pc + MT);
-                *(f32x4g*)(u + 4) = *(const f32x4g*)(patch + r * STRIDE + pc + MT + 4);
+        for (int c = 0; c < CHUNKS; ++c) {
+            float z[U][8], u[U][8], e[U][8];
+#pragma unroll
+            for (int r = 0; r < U; ++r) {
+                const float* const s = patch + ((c * U + r) * RI + lr) * STRIDE + pc;
+                *(f32x4g*)z[r] = *(const f32x4g*)s;
+                *(f32x4g*)(z[r] + 4) = *(const f32x4g*)(s + 4);
+                if constexpr (GATED) {
+                    *(f32x4g*)u[r] = *(const f32x4g*)(s + MT);
+                    *(f32x4g*)(u[r] + 4) = *(const f32x4g*)(s + MT + 4);
+                }
             }
-            if (m < g.m && col < g.n) {
-                if (g.mode == GEMM_PARTIAL) gm_put_some(g.partial + ((int64_t)split * g.m + m) * g.n + col, g.n - col, z);
-                else gm_finish8<T>(g, m, col, z, u, bz, bu);
+            const int first = row + (p * CHUNKS + c) * U * RI;
+            if (g.mode == GEMM_PARTIAL) {
+#pragma unroll
+                for (int r = 0; r < U; ++r)
+                    if (first + r * RI < g.m && count > 0) gm_put_some(g.partial + ((int64_t)split * g.m + first + r * RI) * g.n + col, count, z[r]);
+                continue;
+            }
+            if (extra) {
+#pragma unroll
+                for (int r = 0; r < U; ++r) next[r].values(e[r]);
+                if (p * CHUNKS + c + 1 < FM / PF * CHUNKS) ask(p * CHUNKS + c + 1);
+            } else {
+#pragma unroll
+                for (int r = 0; r < U; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[r][i] = 0.0f;
+            }
+            gm_finish<GATED, U>(g, z, u, e, bz, bu);
+#pragma unroll
+            for (int r = 0; r < U; ++r) {
+                const int m = first + r * RI;
+                if (m < g.m && count > 0) {
+                    T* const out = (T*)g.out + (int64_t)m * g.ld_out + col;
+                    gm_put_some(out, count, z[r]);
+                    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[r]);
+                }
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -346,17 +484,16 @@ void k_gemm(const GemmArgs g) {
 
 template <typename T, int LAYOUT, bool GATED, bool ALIGNED, int TILE>
 hipError_t start_gemm(const GemmArgs& g, hipStream_t st) {
-    using S = GemmShape<TILE>;
     const int64_t blocks = (int64_t)g.tiles_m * g.tiles_n * g.splits;
     if (blocks < 1 || blocks > 0x7fffffff) return hipErrorInvalidValue;
-    k_gemm<T, LAYOUT, GATED, ALIGNED, TILE><<<(int)blocks, S::BM / S::WM * (S::BN / S::WN) * 64, 0, st>>>(g);
+    k_gemm<T, LAYOUT, GATED, ALIGNED, TILE><<<(int)blocks, gemm_threads<TILE, T>, 0, st>>>(g);
     return hipGetLastError();
 }
 template <typename T, int LAYOUT, bool GATED>
 hipError_t pick_gemm(const GemmArgs& g, bool aligned, int tile, hipStream_t st) {
     if (!aligned) return tile == 0 ? start_gemm<T, LAYOUT, GATED, false, 0>(g, st) : start_gemm<T, LAYOUT, GATED, false, 1>(g, st);
-    return tile == 0 ? start_gemm<T, LAYOUT, GATED, true, 0>(g, st)
-         : tile == 1 ? start_gemm<T, LAYOUT, GATED, true, 1>(g, st) : start_gemm<T, LAYOUT, GATED, true, 2>(g, st);
+    return tile == 0 ? start_gemm<T, LAYOUT, GATED, true, 0>(g, st) : tile == 1 ? start_gemm<T, LAYOUT, GATED, true, 1>(g, st)
+         : tile == 2 ? start_gemm<T, LAYOUT, GATED, true, 2>(g, st) : start_gemm<T, LAYOUT, GATED, true, 3>(g, st);
 }
 
 }  // namespace

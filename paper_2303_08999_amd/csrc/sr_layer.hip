@@ -40,21 +40,41 @@ bool any_overlap(const Span (&out)[NO], const Span (&in)[NI]) {
 
 // How one product is cut: tile (-1: the kernel for few rows), splits of k.
 struct Cut { int tile, splits, ksplit; };
+
+// Microseconds of c workgroups of a tile on each compute unit, each with `steps` of 128 bytes of k: what one alone takes a step, what each takes
+// where `share` of them keep a unit busy, and what a round of them takes beside that.  Measured with 1, 2, 4 and 8 workgroups a unit and k
+// from 64 to 8192.
+double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
+    static const double alone[2][4] = {{0.30, 0.58, 0.79, 1.28}, {0.62, 2.05, 3.70, 7.25}}, full[2][4] = {{0.19, 0.485, 0.79, 1.28}, {0.47, 1.84, 3.70, 7.25}};
+    static const double round[4] = {3.0, 5.0, 9.0, 13.0};
+    static const int share[4] = {4, 2, 1, 1};
+    const int f = es == 4;
+    const int64_t whole = c / share[tile], rest = c % share[tile];
+    double us = (double)whole * (share[tile] * full[f][tile] * (double)steps + round[tile]);
+    if (rest) us += (rest * full[f][tile] > alone[f][tile] ? rest * full[f][tile] : alone[f][tile]) * (double)steps + round[tile];
+    return us;
+}
+// The cut that should take least.  Split sums cost their way through memory, written and read in fp32 at 4.5 bytes a ps, and a launch.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {-1, 1, 0};
     const int64_t nn = gated ? 2 * n : n;
-    auto tiles = [&](int t) { const int64_t s = 64 << t; return ((m + s - 1) / s) * ((nn + s - 1) / s); };
-    int tile = tiles(2) >= 3 * GPU_CUS / 4 ? 2 : tiles(1) >= GPU_CUS ? 1 : 0;
-    int64_t splits = 1;
-    if (tiles(tile) < 2 * GPU_CUS && steps >= 16) {
-        if (layout == GEMM_RC_RC) tile = tiles(2) >= 32 ? 2 : m > 64 || n > 64 ? 1 : 0;
-        const int64_t want = (2 * GPU_CUS + tiles(tile) - 1) / tiles(tile);
-        splits = want < steps / 8 ? want : steps / 8;
+    Cut best = {0, 1, 0};
+    double least = 1e300;
+    for (int tile = 0; tile < 4; ++tile) {
+        const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
+        auto look = [&](int64_t splits) {
+            if (splits < 1 || (splits > 1 && (splits > steps / 4 || splits > 1024))) return;
+            const int64_t each = steps ? (steps + splits - 1) / splits : 0;
+            splits = steps ? (steps + each - 1) / each : 1;
+            double us = tile_time(tile, (tiles * splits + GPU_CUS - 1) / GPU_CUS, each, es);
+            if (splits > 1) us += 3.0 + 8.0 * (double)splits * (double)m * (double)nn / 4.5e6;
+            if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk)};
+        };
+        for (int s = 1; s <= 8; ++s) look(s);
+        for (int c = 1; c <= 8 && tiles; ++c) look(c * GPU_CUS / tiles);
     }
-    const int64_t each = (steps + splits - 1) / splits;
-    splits = steps ? (steps + each - 1) / each : 1;
-    return {tile, (int)(splits < 1 ? 1 : splits), (int)(each * bk)};
+    return best;
 }
 
 // Scratch of a split product: its partial results, and (dW) its partial sums of dz
@@ -78,17 +98,17 @@ hipError_t product(GemmArgs g, int dtype, int layout, void* ws, hipStream_t st) 
         if (c.tile < 0 && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
         int tile = c.tile < 0 ? 0 : c.tile;
         if (!aligned && tile > 1) tile = 1;
-        const int side = gemm_tile_rows(tile);
-        g.tiles_m = (g.m + side - 1) / side;
+        const int rows = gemm_tile_rows(tile), cols = gemm_tile_cols(tile);
+        g.tiles_m = (g.m + rows - 1) / rows;
         if (g.splits == 1) {
-            g.tiles_n = g.out ? (int)(((int64_t)(gated ? 2 : 1) * g.n + side - 1) / side) : 1;      // without: the sums of dz alone
+            g.tiles_n = g.out ? (int)(((int64_t)(gated ? 2 : 1) * g.n + cols - 1) / cols) : 1;      // without: the sums of dz alone
             if (g.ksplit == 0) g.ksplit = g.k;
             return launch_gemm<T>(g, layout, aligned, tile, st);
         }
         GemmArgs p = g;
         p.mode = GEMM_PARTIAL;
         p.n = gated ? 2 * g.half : g.n;
-        p.tiles_n = g.out ? (p.n + side - 1) / side : 1;
+        p.tiles_n = g.out ? (p.n + cols - 1) / cols : 1;
         p.partial = g.partial = g.out ? (float*)ws : nullptr;
         if (g.sums_out) {
             p.sums = g.sums = (float*)((char*)ws + partial_bytes(c, g.m, p.n));

@@ -68,14 +68,13 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
     for (int i = threadIdx.x; i < 32 * RF; i += SKW * 64) {
         const int m = i / 2, c = i % 2 * 8, col = n0 + c;
         if (m >= g.m || col >= g.n) continue;
-        float z[8], u[8], bz[8], bu[8];
-        gm_bias8<T>(g, col, GATED, bz, bu);
+        float z[1][8], u[1][8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            z[e] = sh[m * 16 + c + e];
-            u[e] = GATED ? sh[RF * 256 + m * 16 + c + e] : 0.0f;
+            z[0][e] = sh[m * 16 + c + e];
+            u[0][e] = GATED ? sh[RF * 256 + m * 16 + c + e] : 0.0f;
         }
-        gm_finish8<T>(g, m, col, z, u, bz, bu);
+        gm_finish8<T, GATED>(g, m, col, z, u);
     }
 }
 
@@ -130,15 +129,12 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
         }
     }
     if (!any || slice != 0) return;
-    float z[8], u[8], bz[8], bu[8];
+    float z[1][8], u[1][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = (float)zd[i], u[i] = (float)ud[i];
-    if (in_sums) {
-        gm_put_some((T*)g.sums_out + col, count, z);
-    } else {
-        gm_bias8<T>(g, col, gated, bz, bu);
-        gm_finish8<T>(g, row, col, z, u, bz, bu);
-    }
+    for (int i = 0; i < 8; ++i) z[0][i] = (float)zd[i], u[0][i] = (float)ud[i];
+    if (in_sums) gm_put_some((T*)g.sums_out + col, count, z[0]);
+    else if (gated) gm_finish8<T, true>(g, row, col, z, u);
+    else gm_finish8<T, false>(g, row, col, z, u);
 }
 
 template <typename T, bool GATED, int RF>

@@ -128,6 +128,10 @@ def test_workspace_sizes(lib):
             assert f(*args, *more) == 0
     assert lib.sr_layer_linear_grad_workspace_bytes(100, 64, 64, sr.SR_F16, 7) == 0
     assert lib.sr_layer_linear_workspace_bytes(1, 2048, 2048, sr.SR_BF16) == 0
+    for f, more in ((lib.sr_layer_linear_workspace_bytes, ()), (lib.sr_layer_gated_workspace_bytes, ()),
+                    (lib.sr_layer_linear_grad_workspace_bytes, (sr.SR_ACT_GELU,)), (lib.sr_layer_gated_grad_workspace_bytes, ())):
+        assert f(0, 64, 72, sr.SR_F16, *more) == 0                      # no rows
+        f((1 << 31) - 257, 65536, 65536, sr.SR_F32, *more)              # the largest sizes there are
     # the gradient of z: rows of 16-byte pieces
     assert lib.sr_layer_gated_grad_workspace_bytes(100000, 64, 33, sr.SR_BF16) >= 100000 * 72 * 2
     assert lib.sr_layer_linear_grad_workspace_bytes(100000, 64, 33, sr.SR_BF16, sr.SR_ACT_RELU) >= 100000 * 40 * 2
