@@ -66,6 +66,19 @@ template <typename T> hipError_t launch_gemm_finish(const GemmArgs& g, hipStream
 // Few rows: one pass over the weights (layout KC_KC; modes STORE and GATED)
 template <typename T> hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st);
 constexpr int SKINNY_ROWS = 64;
+// Many rows, a small weight (layouts KC_KC and KC_RC, every mode but PARTIAL; the output's rows without gaps): what a launch is made of, waves = 0 if
+// the case is none for it.  np: columns of a half in LDS; steps: of 64 bytes of k.
+struct ThinShape { int np, steps, waves; };
+inline ThinShape thin_shape(int64_t n, int64_t k, size_t es, bool gated, bool both) {
+    const int64_t group = gated ? 32 : 64, np = (n + group - 1) / group * group, steps = (k * (int64_t)es + 63) / 64;
+    if (steps < 1 || steps > 4 || n > 512) return {0, 0, 0};
+    for (int waves = 4; waves >= 2; waves /= 2) {
+        const int64_t patch = (32 * (both ? 2 * n : n) * (int64_t)es + 15) / 16 * 16;
+        if (np * (gated ? 2 : 1) * (steps * 64 + 20) + waves * patch <= 65536) return {(int)np, (int)steps, waves};
+    }
+    return {0, 0, 0};
+}
+template <typename T> hipError_t launch_thin(const GemmArgs& g, int layout, hipStream_t st);
 
 // ---- values ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float act_exp(float z) { return __builtin_amdgcn_exp2f(z * LOG2E); }
@@ -277,17 +290,10 @@ template <typename T> struct Raw8 {
     }
 };
 
-// What a layer does to 8 U values of C, z in, output out; e: of `extra`.  For the gated forms u is the same columns of the second half, and
+// What a layer does to 8 U values of z, outputs in its place; e: of `extra`.  For the gated forms u is the same columns of the second half, and
 // becomes the second output.
 template <bool GATED, int U>
-__device__ __forceinline__ void gm_finish(const GemmArgs& g, float (&z)[U][8], float (&u)[U][8], const float (&e)[U][8], const float bz[8], const float bu[8]) {
-#pragma unroll
-    for (int r = 0; r < U; ++r)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            z[r][i] += bz[i];
-            if constexpr (GATED) u[r][i] += bu[i];
-        }
+__device__ __forceinline__ void gm_finish(const GemmArgs& g, float (&z)[U][8], float (&u)[U][8], const float (&e)[U][8]) {
     if (g.mode == (GATED ? GEMM_GATED : GEMM_STORE)) {
         act8<U>(g.act, z);
 #pragma unroll
@@ -322,7 +328,12 @@ __device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int c
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[0][i] = 0.0f;
     if (g.extra) gm_get_some((const T*)g.extra + row * g.ld_extra + col, count, e[0]);
-    gm_finish<GATED, 1>(g, z, u, e, bz, bu);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        z[0][i] += bz[i];
+        if constexpr (GATED) u[0][i] += bu[i];
+    }
+    gm_finish<GATED, 1>(g, z, u, e);
     T* const out = (T*)g.out + row * g.ld_out + col;
     gm_put_some(out, count, z[0]);
     if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[0]);

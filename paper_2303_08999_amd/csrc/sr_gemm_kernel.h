@@ -467,7 +467,14 @@ void k_gemm(const GemmArgs g) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) e[r][i] = 0.0f;
             }
-            gm_finish<GATED, U>(g, z, u, e, bz, bu);
+#pragma unroll
+            for (int r = 0; r < U; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    z[r][i] += bz[i];
+                    if constexpr (GATED) u[r][i] += bu[i];
+                }
+            gm_finish<GATED, U>(g, z, u, e);
 #pragma unroll
             for (int r = 0; r < U; ++r) {
                 const int m = first + r * RI;

@@ -38,7 +38,8 @@ bool any_overlap(const Span (&out)[NO], const Span (&in)[NI]) {
     return false;
 }
 
-// How one product is cut: tile (-1: the kernel for few rows), splits of k.
+// How one product is cut: tile (or the kernel for few rows, or for a small weight), splits of k.
+constexpr int SKINNY = -1, THIN = -2;
 struct Cut { int tile, splits, ksplit; };
 
 // Microseconds of c workgroups of a tile on each compute unit, each with `steps` of 128 bytes of k: what one alone takes a step, what each takes
@@ -54,10 +55,13 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
     if (rest) us += (rest * full[f][tile] > alone[f][tile] ? rest * full[f][tile] : alone[f][tile]) * (double)steps + round[tile];
     return us;
 }
+// From here on rows with a weight that fits go to the kernel for them.
+constexpr int64_t THIN_FROM = 4096;
 // The cut that should take least.  Split sums cost their way through memory, written and read in fp32 at 4.5 bytes a ps, and a launch.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
-    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {-1, 1, 0};
+    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0};
+    if (layout != GEMM_RC_RC && m >= THIN_FROM && thin_shape(n, k, es, gated, true).waves) return {THIN, 1, 0};
     const int64_t nn = gated ? 2 * n : n;
     Cut best = {0, 1, 0};
     double least = 1e300;
@@ -95,8 +99,9 @@ hipError_t product(GemmArgs g, int dtype, int layout, void* ws, hipStream_t st) 
     g.ksplit = c.ksplit;
     return by_type(dtype, [&](auto t) -> hipError_t {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (c.tile < 0 && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
-        int tile = c.tile < 0 ? 0 : c.tile;
+        if (c.tile == SKINNY && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
+        if (c.tile == THIN && g.ld_out == (g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n)) return launch_thin<T>(g, layout, st);
+        int tile = c.tile >= 0 ? c.tile : c.tile == THIN ? 1 : 0;
         if (!aligned && tile > 1) tile = 1;
         const int rows = gemm_tile_rows(tile), cols = gemm_tile_cols(tile);
         g.tiles_m = (g.m + rows - 1) / rows;

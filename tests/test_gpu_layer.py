@@ -235,6 +235,34 @@ def test_large_tiles_and_long_sums(gated, shape, t):
         check_grad(*shape, t, lo.NONE, gated)
 
 
+# a small weight under many rows: every number of 64-byte steps of a row, rows that are no pieces of 16 bytes, outputs that are no fours
+THIN = [(4096, 1, 1), (4097, 27, 121), (5003, 64, 72), (4100, 31, 33), (9999, 128, 4), (4111, 8, 130), (6000, 33, 64), (4127, 100, 5), (4128, 72, 64), (20001, 16, 31),
+        (4099, 127, 63), (131077, 12, 20), (4100, 24, 300), (4500, 65, 200)]
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("shape", THIN, ids=lambda s: "P%dC%dO%d" % s)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_many_rows_and_a_small_weight(gated, shape, t):
+    P, C, O = shape
+    for kind, shift in ((lo.NONE, 0), (P % 4 + 1, P % 3)):
+        check_forward(P, C, O, t, kind, gated, bias=kind > 0, residual=not gated, shift=shift)
+        check_grad(P, C, O, t, kind, gated, bias=kind > 0, shift=shift)
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_a_row_of_nan_among_many(gated):
+    for C, O in ((27, 121), (64, 72), (100, 5)):
+        d = inputs(4200, C, O, "f32", gated, 5)
+        clean = run_forward(d, "f32", lo.SILU, gated).clone()
+        for row in (0, 777, 4199):
+            d["x"][row] = float("nan")
+        y = run_forward(d, "f32", lo.SILU, gated)
+        rows = torch.ones(4200, dtype=torch.bool, device=DEV)
+        rows[0] = rows[777] = rows[4199] = False
+        assert torch.equal(y[rows], clean[rows]) and y[~rows].isnan().all()
+
+
 def test_what_is_not_asked_for_is_not_written_and_changes_nothing():
     for gated in (False, True):
         for shape in ((70, 40, 24), (5000, 72, 64), (7, 64, 9)):
