@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsrdict.so")
@@ -107,13 +108,13 @@ def load():
     lib.sr_dict_assemble_list_grad.argtypes = [T, T, T, T, i, i, i, i, i, T, T, T, T, vp, sz, vp]
     ll = ctypes.c_longlong
     lib.sr_layer_linear_workspace_bytes.argtypes = [ll, i, i, i]
-    lib.sr_layer_linear.argtypes = [T, T, T, i, T, T, vp, sz, vp]
+    lib.sr_layer_linear.argtypes = [vp, vp, vp, i, vp, vp, vp, sz, vp]
     lib.sr_layer_linear_grad_workspace_bytes.argtypes = [ll, i, i, i, i]
-    lib.sr_layer_linear_grad.argtypes = [T, T, T, i, T, T, T, T, vp, sz, vp]
+    lib.sr_layer_linear_grad.argtypes = [vp, vp, vp, i, vp, vp, vp, vp, vp, sz, vp]
     lib.sr_layer_gated_workspace_bytes.argtypes = [ll, i, i, i]
-    lib.sr_layer_gated.argtypes = [T, T, T, i, T, vp, sz, vp]
+    lib.sr_layer_gated.argtypes = [vp, vp, vp, i, vp, vp, sz, vp]
     lib.sr_layer_gated_grad_workspace_bytes.argtypes = [ll, i, i, i]
-    lib.sr_layer_gated_grad.argtypes = [T, T, T, i, T, T, T, T, vp, sz, vp]
+    lib.sr_layer_gated_grad.argtypes = [vp, vp, vp, i, vp, vp, vp, vp, vp, sz, vp]
     lib.sr_grad_clip_workspace_bytes.argtypes = [i]
     lib.sr_grad_clip.argtypes = [T, T, i, ctypes.c_double, vp, vp, sz, vp]
     lib.sr_strerror.restype = ctypes.c_char_p
@@ -126,14 +127,16 @@ def load():
 
 
 _codes = {}          # torch dtype -> sr_dtype
+_current_device = None   # the current device's ordinal
 _raw_stream = None   # (device ordinal) -> hipStream_t of the device's current stream, without a Stream object
 
 
 def _bind_torch():
     """What a call needs of torch, looked up once: looking it up in every call was a third of the 8.4 us that a call with
     four tensors spent before the library (a small frame takes the GPU about as long)."""
-    global _raw_stream
+    global _raw_stream, _current_device
     import torch
+    _current_device = torch.cuda.current_device
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     if raw is not None:
         get_device = torch.cuda.current_device
@@ -533,6 +536,9 @@ def sr_dict_assemble_list_grad(lr, index, value, dict, L, k, scale, channels, en
     return dvalue, ddict
 
 
+_at = ctypes.byref
+
+
 def _code(dtype):
     if not _codes:
         _bind_torch()
@@ -542,38 +548,73 @@ def _code(dtype):
     return code
 
 
-def _rows(t) -> sr_tensor:
-    """Descriptor of rows of features: [N][H][W][C], or with fewer axes in front ([rows][C], [N][rows][C])."""
+# A layer's call describes up to seven tensors: all of them in one array, made anew by each call and filled at once (a structure for each
+# took 13 us a call, this 6; a token's layer takes the GPU 5).
+_Slots = sr_tensor * 7
+_fill5, _fill7 = (struct.Struct("@" + "Qiiiii4x" * n).pack_into for n in (5, 7))
+_NONE = (0, 0, 0, 0, 0, 0)
+_B1, _B2, _B3, _B4, _B5, _B6 = (i * ctypes.sizeof(sr_tensor) for i in range(1, 7))
+
+
+def _rows(t, device):
+    """Description of rows of features: [N][H][W][C], or with fewer axes in front ([rows][C], [N][rows][C])."""
     shape = t.shape
-    if not 2 <= len(shape) <= 4 or not t.is_contiguous():
+    n = h = 1
+    if len(shape) == 2:
+        w, c = shape
+    elif len(shape) == 4:
+        n, h, w, c = shape
+    elif len(shape) == 3:
+        h, w, c = shape
+    else:
         raise ValueError("expected a contiguous [N][H][W][C] tensor, or [rows][C]")
-    n, h, w, c = (1,) * (4 - len(shape)) + tuple(shape)
-    return sr_tensor((t.data_ptr() if n and h and w and c else 0) or None, _code(t.dtype), n, c, h, w)
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous [N][H][W][C] tensor, or [rows][C]")
+    if t.get_device() != device:
+        raise ValueError(f"a tensor is on {t.device}: expected the current device")
+    return t.data_ptr(), _codes.get(t.dtype) if t.dtype in _codes else _code(t.dtype), n, c, h, w
 
 
-def _matrix(t) -> sr_tensor:
-    """Descriptor of a weight [O][C] or a bias [O]."""
+def _matrix(t, device):
+    """Description of a weight [O][C] or a bias [O]; none of None."""
+    if t is None:
+        return _NONE
     shape = t.shape
-    if not 1 <= len(shape) <= 2 or not t.is_contiguous():
+    if len(shape) == 2:
+        h, w = shape
+    elif len(shape) == 1:
+        h, (w,) = 1, shape
+    else:
         raise ValueError("a weight is a contiguous [out][in] tensor, a bias a contiguous vector")
-    h, w = (1,) * (2 - len(shape)) + tuple(shape)
-    return sr_tensor((t.data_ptr() if h and w else 0) or None, _code(t.dtype), 1, 1, h, w)
+    if not t.is_contiguous():
+        raise ValueError("a weight is a contiguous [out][in] tensor, a bias a contiguous vector")
+    if t.get_device() != device:
+        raise ValueError(f"a tensor is on {t.device}: expected the current device")
+    return t.data_ptr(), _codes.get(t.dtype) if t.dtype in _codes else _code(t.dtype), 1, 1, h, w
 
 
-def _maybe_rows(t):
-    return None if t is None else _rows(t)
+def _on(t):
+    """The current device, which the tensor is on."""
+    if _current_device is None:
+        _bind_torch()
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        raise ValueError(f"a tensor is on {t.device}: expected the current device")
+    return device
 
 
-def _maybe_matrix(t):
-    return None if t is None else _matrix(t)
-
-
-def _room(workspace, need, like, stream):
+def _room(workspace, need, like, stream, device):
     """A call's scratch, its address and size; none where none is needed and none is given."""
-    if workspace is None and not need:
-        return None, None, 0
-    workspace = _scratch(workspace, need, like, stream)
-    return workspace, ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
+    if workspace is None:
+        size = need()
+        if not size:
+            return None, None, 0
+        workspace = _scratch(None, size, like, stream)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    elif workspace.get_device() != device:
+        raise ValueError(f"the workspace is on {workspace.device}: expected the current device")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def sr_layer_linear_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
@@ -583,11 +624,14 @@ def sr_layer_linear_workspace_bytes(rows: int, in_features: int, out_features: i
 def sr_layer_linear(x, weight, bias, act, residual, y, workspace=None, stream=None):
     """y = act(x weight^T + bias) + residual over rows of features (include/sr_layer.h); ``bias`` and ``residual`` may be
     None; scratch is made here unless the caller passes it."""
-    _here(x, weight, bias, residual, y, workspace)
-    dx, dy = _rows(x), _rows(y)
-    need = load().sr_layer_linear_workspace_bytes(dx.n * dx.h * dx.w, dx.c, dy.c, dx.dtype)
-    workspace, room, size = _room(workspace, need, x, stream)
-    _check(_lib.sr_layer_linear(dx, _matrix(weight), _maybe_matrix(bias), act, _maybe_rows(residual), dy, room, size, _stream(stream)))
+    lib, device = _lib or load(), _on(x)
+    dx, dy = _rows(x, device), _rows(y, device)
+    d = _Slots()
+    _fill5(d, 0, *dx, *_matrix(weight, device), *_matrix(bias, device), *(_NONE if residual is None else _rows(residual, device)), *dy)
+    workspace, room, size = _room(workspace, lambda: lib.sr_layer_linear_workspace_bytes(dx[2] * dx[4] * dx[5], dx[3], dy[3], dx[1]), x,
+                                  stream, device)
+    _check(lib.sr_layer_linear(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, None if residual is None else _at(d, _B3),
+                               _at(d, _B4), room, size, _stream(stream)))
     return y
 
 
@@ -595,15 +639,22 @@ def sr_layer_linear_grad_workspace_bytes(rows: int, in_features: int, out_featur
     return int(load().sr_layer_linear_grad_workspace_bytes(rows, in_features, out_features, _code(dtype), act))
 
 
+def _layer_grad(call, need, x, weight, bias, act, dy, dx, dweight, dbias, workspace, stream, device):
+    rx, ry = _rows(x, device), _rows(dy, device)
+    d = _Slots()
+    _fill7(d, 0, *rx, *_matrix(weight, device), *_matrix(bias, device), *ry, *(_NONE if dx is None else _rows(dx, device)),
+           *_matrix(dweight, device), *_matrix(dbias, device))
+    workspace, room, size = _room(workspace, lambda: need(rx[2] * rx[4] * rx[5], rx[3], ry[3], rx[1]), x, stream, device)
+    _check(call(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, _at(d, _B3), None if dx is None else _at(d, _B4),
+                None if dweight is None else _at(d, _B5), None if dbias is None else _at(d, _B6), room, size, _stream(stream)))
+    return dx, dweight, dbias
+
+
 def sr_layer_linear_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace=None, stream=None):
     """Gradient of sr_layer_linear with respect to features, weight and bias, each of which may be None."""
-    _here(x, weight, bias, dy, dx, dweight, dbias, workspace)
-    rx, ry = _rows(x), _rows(dy)
-    need = load().sr_layer_linear_grad_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype, act)
-    workspace, room, size = _room(workspace, need, x, stream)
-    _check(_lib.sr_layer_linear_grad(rx, _matrix(weight), _maybe_matrix(bias), act, ry, _maybe_rows(dx), _maybe_matrix(dweight),
-                                     _maybe_matrix(dbias), room, size, _stream(stream)))
-    return dx, dweight, dbias
+    lib = _lib or load()
+    return _layer_grad(lib.sr_layer_linear_grad, lambda *sizes: lib.sr_layer_linear_grad_workspace_bytes(*sizes, act), x, weight, bias, act, dy,
+                       dx, dweight, dbias, workspace, stream, _on(x))
 
 
 def sr_layer_gated_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
@@ -612,11 +663,13 @@ def sr_layer_gated_workspace_bytes(rows: int, in_features: int, out_features: in
 
 def sr_layer_gated(x, weight, bias, act, y, workspace=None, stream=None):
     """y = act(x Wg^T + bg) (x Wu^T + bu), ``weight`` [2 * out][in] being Wg on top of Wu (include/sr_layer.h)."""
-    _here(x, weight, bias, y, workspace)
-    rx, ry = _rows(x), _rows(y)
-    need = load().sr_layer_gated_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype)
-    workspace, room, size = _room(workspace, need, x, stream)
-    _check(_lib.sr_layer_gated(rx, _matrix(weight), _maybe_matrix(bias), act, ry, room, size, _stream(stream)))
+    lib, device = _lib or load(), _on(x)
+    dx, dy = _rows(x, device), _rows(y, device)
+    d = _Slots()
+    _fill5(d, 0, *dx, *_matrix(weight, device), *_matrix(bias, device), *dy, *_NONE)
+    workspace, room, size = _room(workspace, lambda: lib.sr_layer_gated_workspace_bytes(dx[2] * dx[4] * dx[5], dx[3], dy[3], dx[1]), x,
+                                  stream, device)
+    _check(lib.sr_layer_gated(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, _at(d, _B3), room, size, _stream(stream)))
     return y
 
 
@@ -626,13 +679,9 @@ def sr_layer_gated_grad_workspace_bytes(rows: int, in_features: int, out_feature
 
 def sr_layer_gated_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace=None, stream=None):
     """Gradient of sr_layer_gated with respect to features, weight and bias, each of which may be None."""
-    _here(x, weight, bias, dy, dx, dweight, dbias, workspace)
-    rx, ry = _rows(x), _rows(dy)
-    need = load().sr_layer_gated_grad_workspace_bytes(rx.n * rx.h * rx.w, rx.c, ry.c, rx.dtype)
-    workspace, room, size = _room(workspace, need, x, stream)
-    _check(_lib.sr_layer_gated_grad(rx, _matrix(weight), _maybe_matrix(bias), act, ry, _maybe_rows(dx), _maybe_matrix(dweight),
-                                    _maybe_matrix(dbias), room, size, _stream(stream)))
-    return dx, dweight, dbias
+    lib = _lib or load()
+    return _layer_grad(lib.sr_layer_gated_grad, lib.sr_layer_gated_grad_workspace_bytes, x, weight, bias, act, dy, dx, dweight, dbias,
+                       workspace, stream, _on(x))
 
 
 def _dense(t):

@@ -90,10 +90,9 @@ template <typename F> hipError_t by_type(int d, F f) {
 
 // One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, where
 // sums_out is set, of the sums).
-hipError_t product(GemmArgs g, int dtype, int layout, void* ws, hipStream_t st) {
+hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hipStream_t st) {
     const size_t es = layer_esize(dtype);
     const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
-    Cut c = cut_of(g.m, g.n, g.k, es, layout, gated);
     const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda * es % 16 == 0 && g.ldb * es % 16 == 0;
     g.splits = c.splits;
     g.ksplit = c.ksplit;
@@ -132,20 +131,28 @@ struct Layer {
     bool gated;
 };
 
-size_t forward_scratch(const Layer& l) {
-    const Cut c = cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated);
-    return partial_bytes(c, l.rows, l.wide);
-}
+Cut forward_cut(const Layer& l) { return cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated); }
+size_t forward_scratch(const Layer& l, const Cut& c) { return partial_bytes(c, l.rows, l.wide); }
 // dz, rows on 16-byte pieces
 int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (l.wide + e - 1) / e * e; }
 size_t dz_bytes(const Layer& l, int act) { return l.gated || act != SR_ACT_NONE ? up256((size_t)l.rows * dz_row(l) * layer_esize(l.dtype)) : 0; }
-size_t grad_scratch(const Layer& l, int act) {
-    const size_t es = layer_esize(l.dtype), dz = dz_bytes(l, act);
-    const Cut x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false), w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
-    size_t most = dz ? forward_scratch(l) : 0;
-    if (partial_bytes(x, l.rows, l.in) > most) most = partial_bytes(x, l.rows, l.in);
-    const size_t dw = partial_bytes(w, l.wide, l.in) + (w.splits > 1 ? up256((size_t)w.splits * l.wide * 4) : 0);
-    return dz + (dw > most ? dw : most);
+// A gradient's three products: z, dx, dweight; and the scratch that dz takes and all of it
+struct GradPlan { Cut z, x, w; size_t dz, need; };
+GradPlan grad_plan(const Layer& l, int act) {
+    const size_t es = layer_esize(l.dtype);
+    GradPlan p = {};
+    p.dz = dz_bytes(l, act);
+    p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false);
+    p.w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
+    size_t most = partial_bytes(p.x, l.rows, l.in);
+    if (p.dz) {
+        p.z = forward_cut(l);
+        const size_t z = forward_scratch(l, p.z);
+        if (z > most) most = z;
+    }
+    const size_t dw = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
+    p.need = p.dz + (dw > most ? dw : most);
+    return p;
 }
 
 bool layer_sizes(Layer& l, long long rows, int in, int out, int dtype, bool gated) {
@@ -207,7 +214,8 @@ int forward(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, 
     Layer l;
     int st = layer_args(l, x, weight, bias, act, y, residual, gated);
     if (st != SR_OK) return st;
-    const size_t need = forward_scratch(l);
+    const Cut cut = forward_cut(l);
+    const size_t need = forward_scratch(l, cut);
     st = scratch_args(workspace, workspace_bytes, need);
     if (st != SR_OK) return st;
     const Span out[] = {span(y), {need ? workspace : nullptr, need}}, in[] = {span(x), span(weight), span(bias), span(residual)};
@@ -217,7 +225,7 @@ int forward(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, 
     g.mode = gated ? GEMM_GATED : GEMM_STORE;
     g.extra = residual ? residual->data : nullptr;
     g.out = y->data;
-    return product(g, l.dtype, GEMM_KC_KC, workspace, (hipStream_t)stream) == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
+    return product(g, cut, l.dtype, GEMM_KC_KC, workspace, (hipStream_t)stream) == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }
 
 int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* dy,
@@ -235,7 +243,8 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         if (t && !t->data) return SR_ERR_NULL;
         if (t && (uintptr_t)t->data % es) return SR_ERR_ALIGN;
     }
-    const size_t need = grad_scratch(l, act), dz = dz_bytes(l, act);
+    const GradPlan plan = grad_plan(l, act);
+    const size_t need = plan.need, dz = plan.dz;
     st = scratch_args(workspace, workspace_bytes, need);
     if (st != SR_OK) return st;
     const Span out[] = {span(dx), span(dweight), span(dbias), {need ? workspace : nullptr, need}};
@@ -254,7 +263,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.out = workspace;
         g.ld_out = ldz = dz_row(l);
         z = workspace;
-        if (l.rows) e = product(g, l.dtype, GEMM_KC_KC, rest, s);
+        if (l.rows) e = product(g, plan.z, l.dtype, GEMM_KC_KC, rest, s);
     }
     if (dx && l.rows && e == hipSuccess) {
         GemmArgs g = {};
@@ -268,7 +277,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.mode = GEMM_STORE;
         g.out = dx->data;
         g.ld_out = l.in;
-        e = product(g, l.dtype, GEMM_KC_RC, rest, s);
+        e = product(g, plan.x, l.dtype, GEMM_KC_RC, rest, s);
     }
     if ((dweight || dbias) && e == hipSuccess) {
         GemmArgs g = {};
@@ -283,7 +292,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.out = dweight ? dweight->data : nullptr;
         g.ld_out = l.in;
         g.sums_out = dbias ? dbias->data : nullptr;
-        e = product(g, l.dtype, GEMM_RC_RC, rest, s);
+        e = product(g, plan.w, l.dtype, GEMM_RC_RC, rest, s);
     }
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }
@@ -296,7 +305,7 @@ using namespace srd;
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_linear_workspace_bytes(long long rows, int in, int out, int dtype) {
     Layer l;
-    return layer_sizes(l, rows, in, out, dtype, false) ? forward_scratch(l) : 0;
+    return layer_sizes(l, rows, in, out, dtype, false) ? forward_scratch(l, forward_cut(l)) : 0;
 }
 
 extern "C" __attribute__((visibility("default")))
@@ -308,7 +317,7 @@ int sr_layer_linear(const sr_tensor* x, const sr_tensor* weight, const sr_tensor
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_linear_grad_workspace_bytes(long long rows, int in, int out, int dtype, int act) {
     Layer l;
-    return layer_act(act) && layer_sizes(l, rows, in, out, dtype, false) ? grad_scratch(l, act) : 0;
+    return layer_act(act) && layer_sizes(l, rows, in, out, dtype, false) ? grad_plan(l, act).need : 0;
 }
 
 extern "C" __attribute__((visibility("default")))
@@ -321,7 +330,7 @@ int sr_layer_linear_grad(const sr_tensor* x, const sr_tensor* weight, const sr_t
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_gated_workspace_bytes(long long rows, int in, int out, int dtype) {
     Layer l;
-    return layer_sizes(l, rows, in, out, dtype, true) ? forward_scratch(l) : 0;
+    return layer_sizes(l, rows, in, out, dtype, true) ? forward_scratch(l, forward_cut(l)) : 0;
 }
 
 extern "C" __attribute__((visibility("default")))
@@ -333,7 +342,7 @@ int sr_layer_gated(const sr_tensor* x, const sr_tensor* weight, const sr_tensor*
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_gated_grad_workspace_bytes(long long rows, int in, int out, int dtype) {
     Layer l;
-    return layer_sizes(l, rows, in, out, dtype, true) ? grad_scratch(l, SR_ACT_NONE) : 0;
+    return layer_sizes(l, rows, in, out, dtype, true) ? grad_plan(l, SR_ACT_NONE).need : 0;
 }
 
 extern "C" __attribute__((visibility("default")))

@@ -34,13 +34,16 @@ class Case:
         self.ws, self.bytes = BASE + (8 << 24), 1 << 40
 
     def forward(self, lib):
+        x, weight, bias, y, residual = (t and ctypes.byref(t) for t in (self.x, self.weight, self.bias, self.y, self.residual))
         if self.gated:
-            return lib.sr_layer_gated(self.x, self.weight, self.bias, self.act, self.y, self.ws, self.bytes, None)
-        return lib.sr_layer_linear(self.x, self.weight, self.bias, self.act, self.residual, self.y, self.ws, self.bytes, None)
+            return lib.sr_layer_gated(x, weight, bias, self.act, y, self.ws, self.bytes, None)
+        return lib.sr_layer_linear(x, weight, bias, self.act, residual, y, self.ws, self.bytes, None)
 
     def grad(self, lib):
         call = lib.sr_layer_gated_grad if self.gated else lib.sr_layer_linear_grad
-        return call(self.x, self.weight, self.bias, self.act, self.y, self.dx, self.dweight, self.dbias, self.ws, self.bytes, None)
+        x, weight, bias, y, dx, dweight, dbias = (t and ctypes.byref(t) for t in (self.x, self.weight, self.bias, self.y, self.dx, self.dweight,
+                                                                                   self.dbias))
+        return call(x, weight, bias, self.act, y, dx, dweight, dbias, self.ws, self.bytes, None)
 
 
 def bad(gated, what):
@@ -216,15 +219,27 @@ def test_the_binding_refuses_what_it_cannot_describe(lib):
     with pytest.raises(ValueError, match="one device"):
         sr.sr_grad_clip([x], None, 1.0, torch.zeros(2))
     with pytest.raises(ValueError, match="contiguous"):
-        binding._rows(torch.zeros(8, 4).t())
+        binding._rows(torch.zeros(8, 4).t(), -1)
     with pytest.raises(ValueError, match="contiguous"):
-        binding._matrix(torch.zeros(8, 4).t())
+        binding._rows(torch.zeros(8), -1)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._matrix(torch.zeros(8, 4).t(), -1)
+    with pytest.raises(ValueError, match="contiguous"):
+        binding._matrix(torch.zeros(1, 8, 4), -1)
     with pytest.raises(TypeError):
-        binding._rows(x.double())
-    d = binding._rows(torch.zeros(2, 3, 5, 7))
-    assert (d.n, d.h, d.w, d.c) == (2, 3, 5, 7)
-    d = binding._rows(x)
-    assert (d.n, d.h, d.w, d.c) == (1, 1, 4, 8)
+        binding._rows(x.double(), -1)
+    with pytest.raises(TypeError):
+        binding._matrix(x.long(), -1)
+    assert binding._rows(torch.zeros(2, 3, 5, 7), -1)[1:] == (sr.SR_F32, 2, 7, 3, 5)
+    assert binding._rows(torch.zeros(3, 5, 7).half(), -1)[1:] == (sr.SR_F16, 1, 7, 3, 5)
+    assert binding._rows(x, -1) == (x.data_ptr(), sr.SR_F32, 1, 8, 1, 4)
+    assert binding._matrix(w.bfloat16(), -1)[1:] == (sr.SR_BF16, 1, 1, 3, 8) and binding._matrix(w[0], -1)[1:] == (sr.SR_F32, 1, 1, 1, 8)
+    # what is packed is what the structure holds
+    slots = binding._Slots()
+    binding._fill5(slots, 0, *range(1, 31))
+    for i in range(5):
+        d = slots[i]
+        assert [d.data, d.dtype, d.n, d.c, d.h, d.w] == list(range(6 * i + 1, 6 * i + 7))
 
 
 def test_tensors_without_gaps():
