@@ -67,18 +67,53 @@ template <typename T> hipError_t launch_gemm_finish(const GemmArgs& g, hipStream
 template <typename T> hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st);
 constexpr int SKINNY_ROWS = 64;
 // Many rows, a small weight (layouts KC_KC and KC_RC, every mode but PARTIAL; the output's rows without gaps): what a launch is made of, waves = 0 if
-// the case is none for it.  np: columns of a half in LDS; steps: of 64 bytes of k.
-struct ThinShape { int np, steps, waves; };
+// the case is none for it.  rows: that a wavefront takes at a time; group: tiles of 16 columns (of each half) that are made at a time; np: columns of a
+// half in LDS; steps: of 64 bytes of k.  With fewer than 12 wavefronts on a compute unit the rows' way through memory is not hidden (500 000 rows of
+// 128 to 128, bfloat16, 6 wavefronts: 70 us, the tile kernel 47).
+struct ThinShape { int np, steps, waves, group, rows; };
 inline ThinShape thin_shape(int64_t n, int64_t k, size_t es, bool gated, bool both) {
-    const int64_t group = gated ? 32 : 64, np = (n + group - 1) / group * group, steps = (k * (int64_t)es + 63) / 64;
-    if (steps < 1 || steps > 4 || n > 512) return {0, 0, 0};
-    for (int waves = 4; waves >= 2; waves /= 2) {
-        const int64_t patch = (32 * (both ? 2 * n : n) * (int64_t)es + 15) / 16 * 16;
-        if (np * (gated ? 2 : 1) * (steps * 64 + 20) + waves * patch <= 65536) return {(int)np, (int)steps, waves};
+    const int64_t group = n <= 16 ? 1 : 2, np = (n + 16 * group - 1) / (16 * group) * (16 * group), steps = (k * (int64_t)es + 63) / 64;
+    if (steps < 1 || steps > 4 || n > 512) return {0, 0, 0, 0, 0};
+    for (int rows = 32; rows >= 16; rows /= 2) {
+        const int64_t patch = (rows * (both ? 2 * n : n) * (int64_t)es + 15) / 16 * 16;
+        const int64_t bytes = np * (gated ? 2 : 1) * (steps * 64 + 20) + 4 * patch;
+        if (bytes <= 65536 && 163840 / bytes >= 3) return {(int)np, (int)steps, 4, (int)group, rows};
     }
-    return {0, 0, 0};
+    return {0, 0, 0, 0, 0};
 }
 template <typename T> hipError_t launch_thin(const GemmArgs& g, int layout, hipStream_t st);
+
+// A small layer's whole gradient in one pass over many rows (everything on 16-byte pieces; c and o multiples of a piece).
+struct ThinGradArgs {
+    const void *x, *w, *bias, *dy;
+    void* dx;                  // or null
+    float *partial, *sums;     // [workgroups][wide][c], [workgroups][wide], or null
+    int64_t rows;
+    int c, o, act;
+};
+// Its LDS: strides of the rows of the tiles (an odd number of 16-byte pieces), steps of 64 bytes in a row, where the tiles are; bytes = 0 if the case
+// is none for it.
+struct ThinGradShape { int dz_stride, x_stride, dy_stride, dz_steps, x_steps, wz, dz, x, dy, bias, bytes; };
+__host__ __device__ inline ThinGradShape thin_grad_shape(int c, int o, int es, bool gated, bool z) {
+    ThinGradShape s = {};
+    const int e = 16 / es, wide = gated ? 2 * o : o;
+    if (c > 128 || wide > (c > 64 ? 128 : 256) || c % e || o % e) return s;      // dW's tiles have to fit the registers
+    s.dz_steps = (wide * es + 63) / 64;
+    s.x_steps = (c * es + 63) / 64;
+    s.dz_stride = s.dz_steps * 64 + 16;
+    s.x_stride = s.x_steps * 64 + 16;
+    s.dy_stride = (o * es + 31) / 32 * 32 + 16;
+    const int c16 = (c + 15) / 16 * 16, w16 = (wide + 15) / 16 * 16;
+    s.wz = c16 * s.dz_stride;
+    s.dz = s.wz + (z ? (w16 + (gated ? 16 : 0)) * s.x_stride : 0);
+    s.x = s.dz + 64 * s.dz_stride;
+    s.dy = s.x + 64 * s.x_stride;
+    s.bias = s.dy + (gated ? 64 * s.dy_stride : 0);
+    s.bytes = s.bias + (z ? (w16 + 16) * 4 : 0);
+    if (s.bytes > 65536) s.bytes = 0;
+    return s;
+}
+template <typename T> hipError_t launch_thin_grad(const ThinGradArgs& a, bool gated, int grid, hipStream_t st);
 
 // ---- values ---------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float act_exp(float z) { return __builtin_amdgcn_exp2f(z * LOG2E); }

@@ -3,11 +3,9 @@
 
 #include "sr_gemm_kernel.h"
 #include "sr_skinny.h"
-#include "sr_thin.h"
 
 namespace srd {
 template hipError_t launch_gemm<bf16raw>(const GemmArgs&, int, bool, int, hipStream_t);
-template hipError_t launch_thin<bf16raw>(const GemmArgs&, int, hipStream_t);
 template hipError_t launch_skinny<bf16raw>(const GemmArgs&, bool, hipStream_t);
 template hipError_t launch_gemm_finish<bf16raw>(const GemmArgs&, hipStream_t);
 }  // namespace srd

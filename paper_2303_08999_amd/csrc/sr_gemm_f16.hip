@@ -3,11 +3,9 @@
 
 #include "sr_gemm_kernel.h"
 #include "sr_skinny.h"
-#include "sr_thin.h"
 
 namespace srd {
 template hipError_t launch_gemm<__half>(const GemmArgs&, int, bool, int, hipStream_t);
-template hipError_t launch_thin<__half>(const GemmArgs&, int, hipStream_t);
 template hipError_t launch_skinny<__half>(const GemmArgs&, bool, hipStream_t);
 template hipError_t launch_gemm_finish<__half>(const GemmArgs&, hipStream_t);
 }  // namespace srd

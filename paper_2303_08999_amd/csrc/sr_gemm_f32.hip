@@ -3,11 +3,9 @@
 
 #include "sr_gemm_kernel.h"
 #include "sr_skinny.h"
-#include "sr_thin.h"
 
 namespace srd {
 template hipError_t launch_gemm<float>(const GemmArgs&, int, bool, int, hipStream_t);
-template hipError_t launch_thin<float>(const GemmArgs&, int, hipStream_t);
 template hipError_t launch_skinny<float>(const GemmArgs&, bool, hipStream_t);
 template hipError_t launch_gemm_finish<float>(const GemmArgs&, hipStream_t);
 }  // namespace srd

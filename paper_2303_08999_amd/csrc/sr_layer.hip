@@ -55,13 +55,17 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
     if (rest) us += (rest * full[f][tile] > alone[f][tile] ? rest * full[f][tile] : alone[f][tile]) * (double)steps + round[tile];
     return us;
 }
-// From here on rows with a weight that fits go to the kernel for them.
+// From here on rows with a weight that fits go to the kernel for them; where that takes 16 at a time (500 000 of 128 to 128, bfloat16: 58 us, tiles 47), only
+// if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
 // The cut that should take least.  Split sums cost their way through memory, written and read in fp32 at 4.5 bytes a ps, and a launch.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0};
-    if (layout != GEMM_RC_RC && m >= THIN_FROM && thin_shape(n, k, es, gated, true).waves) return {THIN, 1, 0};
+    if (layout != GEMM_RC_RC && m >= THIN_FROM) {
+        const ThinShape s = thin_shape(n, k, es, gated, gated);
+        if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0};
+    }
     const int64_t nn = gated ? 2 * n : n;
     Cut best = {0, 1, 0};
     double least = 1e300;
@@ -137,10 +141,15 @@ size_t forward_scratch(const Layer& l, const Cut& c) { return partial_bytes(c, l
 int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (l.wide + e - 1) / e * e; }
 size_t dz_bytes(const Layer& l, int act) { return l.gated || act != SR_ACT_NONE ? up256((size_t)l.rows * dz_row(l) * layer_esize(l.dtype)) : 0; }
 // A gradient's three products: z, dx, dweight; and the scratch that dz takes and all of it
-struct GradPlan { Cut z, x, w; size_t dz, need; };
+// (pass: the workgroups of the one pass that makes them all, for a small layer whose tensors allow it, or 0).
+struct GradPlan { Cut z, x, w; int pass; size_t dz, need; };
 GradPlan grad_plan(const Layer& l, int act) {
     const size_t es = layer_esize(l.dtype);
     GradPlan p = {};
+    if (l.rows >= THIN_FROM && thin_grad_shape(l.in, l.out, (int)es, l.gated, l.gated || act != SR_ACT_NONE).bytes) {
+        const int64_t blocks = (l.rows + 63) / 64;
+        p.pass = (int)(blocks < 2 * GPU_CUS ? blocks : 2 * GPU_CUS);
+    }
     p.dz = dz_bytes(l, act);
     p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false);
     p.w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
@@ -152,6 +161,8 @@ GradPlan grad_plan(const Layer& l, int act) {
     }
     const size_t dw = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
     p.need = p.dz + (dw > most ? dw : most);
+    const size_t pass = up256((size_t)p.pass * l.wide * l.in * 4) + up256((size_t)p.pass * l.wide * 4);
+    if (pass > p.need) p.need = pass;
     return p;
 }
 
@@ -252,6 +263,29 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
     if (any_overlap(out, in)) return SR_ERR_ALIAS;
 
     hipStream_t s = (hipStream_t)stream;
+    uintptr_t at = 0;
+    for (const sr_tensor* t : {x, weight, dy, (const sr_tensor*)dx}) at |= t ? (uintptr_t)t->data : 0;
+    if (plan.pass && at % 16 == 0) {
+        ThinGradArgs a = {x->data, weight->data, bias ? bias->data : nullptr, dy->data, dx ? dx->data : nullptr, nullptr, nullptr, l.rows, l.in, l.out, act};
+        if (dweight) a.partial = (float*)workspace;
+        if (dbias) a.sums = (float*)((char*)workspace + up256((size_t)plan.pass * l.wide * l.in * 4));
+        GemmArgs g = {};
+        g.m = l.wide;
+        g.n = l.in;
+        g.splits = plan.pass;
+        g.mode = GEMM_STORE;
+        g.out = dweight ? dweight->data : nullptr;
+        g.ld_out = l.in;
+        g.sums_out = dbias ? dbias->data : nullptr;
+        g.partial = a.partial;
+        g.sums = a.sums;
+        const hipError_t e = by_type(l.dtype, [&](auto t) -> hipError_t {
+            using T = std::remove_pointer_t<decltype(t)>;
+            const hipError_t first = launch_thin_grad<T>(a, gated, plan.pass, s);
+            return first != hipSuccess || !(dweight || dbias) ? first : launch_gemm_finish<T>(g, s);
+        });
+        return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
+    }
     void* const rest = (char*)workspace + dz;
     const void* z = dy->data;
     int64_t ldz = l.out;

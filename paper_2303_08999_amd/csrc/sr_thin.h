@@ -1,8 +1,8 @@
 // Products of many rows with a small weight (sr_gemm.h): a pixel's layer of few features, bound by the rows' way through memory.
 //
-// The weight, turned so that k runs fastest and filled up with zeros, and the bias stay in LDS for the whole launch.  A wavefront takes 32 rows
-// at a time, loaded straight into the matrix instructions' operands while the 32 before are worked on, and leaves what it made of
-// them in LDS as the piece of the output that it is: 32 rows in a row, stored 16 bytes a lane whatever a row's length is.  Wavefronts wait for
+// The weight, turned so that k runs fastest and filled up with zeros, and the bias stay in LDS for the whole launch.  A wavefront takes 32 (or 16)
+// rows at a time, loaded straight into the matrix instructions' operands while those before are worked on, and leaves what it made of
+// them in LDS as the piece of the output that it is: rows without gaps, stored 16 bytes a lane whatever a row's length is.  Wavefronts wait for
 // nobody.  72 outputs of 64 features for the 8.3 million pixels of a 4K frame, fp16: 470 us would be the speed of a copy; the tile kernel takes 654.
 #pragma once
 #include "sr_gemm.h"
@@ -10,11 +10,12 @@
 namespace srd {
 namespace {
 
-constexpr int THIN_ROWS = 32;
+// wavefronts that a SIMD's registers hold
+template <int KS, bool GATED> constexpr int thin_waves = KS <= 2 && !GATED ? 4 : 3;
 
 // Bytes of LDS: weight rows (each half filled up to np of them), bias, and a piece of the output for each wavefront
-template <typename T> size_t thin_lds(int np, int halves, int steps, int width, int waves) {
-    return (size_t)np * halves * (steps * 64 + 16) + (size_t)np * halves * 4 + (size_t)waves * ((THIN_ROWS * width * sizeof(T) + 15) / 16 * 16);
+template <typename T> size_t thin_lds(int np, int halves, int steps, int width, int waves, int rows) {
+    return (size_t)np * halves * (steps * 64 + 16) + (size_t)np * halves * 4 + (size_t)waves * ((rows * width * sizeof(T) + 15) / 16 * 16);
 }
 
 // four values of a row
@@ -63,10 +64,10 @@ template <typename T, bool FOURS> __device__ __forceinline__ void thin_put4(T* p
     }
 }
 
-// KS steps of 64 bytes of k.  NG groups of 16 columns at a time, of each half.
-template <typename T, int KS, bool GATED, bool FOURS>
-__global__ __launch_bounds__(256) void k_thin(const GemmArgs g, const int rc, const int np) {
-    constexpr int E = 16 / sizeof(T), H = GATED ? 2 : 1, NG = GATED ? 2 : 4, SB = KS * 64 + 16;
+// KS steps of 64 bytes of k.  NG tiles of 16 columns at a time, of each half.
+template <typename T, int KS, int NG, int RF, bool GATED, bool FOURS>
+__global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const GemmArgs g, const int rc, const int np) {
+    constexpr int E = 16 / sizeof(T), H = GATED ? 2 : 1, SB = KS * 64 + 16, THIN_ROWS = 16 * RF, U = (NG * RF + 1) / 2;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     float* const bias = (float*)(lds + (size_t)np * H * SB);
@@ -97,10 +98,10 @@ __global__ __launch_bounds__(256) void k_thin(const GemmArgs g, const int rc, co
     const int r = lane % 16, q = lane / 16;
     const int64_t end = (int64_t)g.m * g.lda;              // elements of A
     const int blocks = (g.m + THIN_ROWS - 1) / THIN_ROWS, step = gridDim.x * waves;
-    u32x4g now[2][KS], next[2][KS];
-    auto load = [&](int block, u32x4g (&v)[2][KS]) {
+    u32x4g now[RF][KS], next[RF][KS];
+    auto load = [&](int block, u32x4g (&v)[RF][KS]) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
+        for (int f = 0; f < RF; ++f) {
             const int row = block * THIN_ROWS + f * 16 + r;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
@@ -113,29 +114,62 @@ __global__ __launch_bounds__(256) void k_thin(const GemmArgs g, const int rc, co
             }
         }
     };
-    auto cut = [&](u32x4g (&v)[2][KS]) {
+    auto cut = [&](u32x4g (&v)[RF][KS]) {
         if (g.k == KS * 4 * E) return;
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < RF; ++f)
 #pragma unroll
             for (int s = 0; s < KS; ++s) v[f][s] = gm_cut<T>(v[f][s], g.k - (s * 4 + q) * E);
     };
+    // What is added or multiplied comes as the piece that the output leaves as, and through the same place in LDS, where its rows are as long.
+    const bool linear = g.extra && g.ld_extra == width;
     int block = blockIdx.x * waves + wave;
     if (block < blocks) load(block, next);
     for (; block < blocks; block += step) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int f = 0; f < RF; ++f)
 #pragma unroll
             for (int s = 0; s < KS; ++s) now[f][s] = next[f][s];
         cut(now);
         if (block + step < blocks) load(block + step, next);
-        const int row0 = block * THIN_ROWS;
+        const int row0 = block * THIN_ROWS, rows = g.m - row0 < THIN_ROWS ? g.m - row0 : THIN_ROWS, count = rows * width;
+        if (linear) {
+            const T* const in = (const T*)g.extra + (int64_t)row0 * width;
+            for (int i = lane * E; i < count; i += 4 * 64 * E) {
+                u32x4g v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = gm_piece(in + i + j * 64 * E, count - i - j * 64 * E);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (i + j * 64 * E < count) *(u32x4g*)(patch + i + j * 64 * E) = v[j];
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
         for (int n0 = 0; n0 < g.n; n0 += NG * 16) {
-            f32x4g acc[H][NG][2];
+            // [NG][RF][4 columns] as rows of 8; what is added or multiplied is on its way while the products are made
+            float z[U][8], u[U][8], e[U][8];
+            if constexpr (NG * RF == 1) {
+#pragma unroll
+                for (int i = 4; i < 8; ++i) z[0][i] = u[0][i] = e[0][i] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < NG; ++j)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = 0.0f;
+                    const int n = n0 + j * 16 + q * 4, m = row0 + f * 16 + r;
+                    if (linear) {
+                        if (n < g.n) thin_get4(patch + (f * 16 + r) * width + n, g.n - n, e[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
+                    } else if (g.extra && m < g.m) thin_get4((const T*)g.extra + (int64_t)m * g.ld_extra + n, g.n - n, e[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
+                }
+            f32x4g acc[H][NG][RF];
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int j = 0; j < NG; ++j) acc[h][j][0] = acc[h][j][1] = *(const f32x4g*)(bias + h * np + n0 + j * 16 + q * 4);
+                for (int j = 0; j < NG; ++j)
+#pragma unroll
+                    for (int f = 0; f < RF; ++f) acc[h][j][f] = *(const f32x4g*)(bias + h * np + n0 + j * 16 + q * 4);
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
@@ -143,37 +177,30 @@ __global__ __launch_bounds__(256) void k_thin(const GemmArgs g, const int rc, co
 #pragma unroll
                     for (int j = 0; j < NG; ++j) {
                         const u32x4g b = *(const u32x4g*)(lds + (h * np + n0 + j * 16 + r) * SB + (s * 4 + q) * 16);
-                        gm_mul<T, 16>(acc[h][j][0], b, now[0][s]);
-                        gm_mul<T, 16>(acc[h][j][1], b, now[1][s]);
+#pragma unroll
+                        for (int f = 0; f < RF; ++f) gm_mul<T, 16>(acc[h][j][f], b, now[f][s]);
                     }
-            // [NG][row group][4 columns] as rows of 8
-            float z[NG][8], u[NG][8], e[NG][8];
 #pragma unroll
             for (int j = 0; j < NG; ++j)
 #pragma unroll
-                for (int f = 0; f < 2; ++f) {
+                for (int f = 0; f < RF; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        z[j][f * 4 + i] = acc[0][j][f][i];
-                        if constexpr (GATED) u[j][f * 4 + i] = acc[H - 1][j][f][i];
-                        e[j][f * 4 + i] = 0.0f;
+                        z[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = acc[0][j][f][i];
+                        if constexpr (GATED) u[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = acc[H - 1][j][f][i];
                     }
-                    const int n = n0 + j * 16 + q * 4, m = row0 + f * 16 + r;
-                    if (g.extra && m < g.m) thin_get4((const T*)g.extra + (int64_t)m * g.ld_extra + n, g.n - n, e[j] + f * 4);
-                }
-            gm_finish<GATED, NG>(g, z, u, e);
+            gm_finish<GATED, U>(g, z, u, e);
 #pragma unroll
             for (int j = 0; j < NG; ++j)
 #pragma unroll
-                for (int f = 0; f < 2; ++f) {
+                for (int f = 0; f < RF; ++f) {
                     const int n = n0 + j * 16 + q * 4;
                     T* const p = patch + (f * 16 + r) * width + n;
-                    thin_put4<T, FOURS>(p, g.n - n, z[j] + f * 4);
-                    if (GATED && g.mode == GEMM_GATED_SLOPE) thin_put4<T, FOURS>(p + g.n, g.n - n, u[j] + f * 4);
+                    thin_put4<T, FOURS>(p, g.n - n, z[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
+                    if (GATED && g.mode == GEMM_GATED_SLOPE) thin_put4<T, FOURS>(p + g.n, g.n - n, u[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
                 }
         }
         __builtin_amdgcn_wave_barrier();
-        const int rows = g.m - row0 < THIN_ROWS ? g.m - row0 : THIN_ROWS, count = rows * width;
         T* const out = (T*)g.out + (int64_t)row0 * width;
         for (int i = lane * E; i < count; i += 64 * E) {
             if (i + E <= count) {
@@ -186,16 +213,16 @@ __global__ __launch_bounds__(256) void k_thin(const GemmArgs g, const int rc, co
     }
 }
 
-template <typename T, int KS, bool GATED>
+template <typename T, int KS, int NG, int RF, bool GATED>
 hipError_t start_thin(const GemmArgs& g, bool rc, int np, int waves, size_t lds, hipStream_t st) {
-    const int64_t blocks = ((int64_t)g.m + THIN_ROWS - 1) / THIN_ROWS, groups = (blocks + waves - 1) / waves;
-    // as many workgroups as the compute units hold at once, by LDS or at most 20 wavefronts a unit
+    const int64_t blocks = ((int64_t)g.m + 16 * RF - 1) / (16 * RF), groups = (blocks + waves - 1) / waves;
+    // as many workgroups as the compute units hold at once, by LDS and by registers
     int per = (int)((160 * 1024) / lds);
-    if (per * waves > 20) per = 20 / waves;
+    if (per * waves > 4 * thin_waves<KS, GATED>) per = 4 * thin_waves<KS, GATED> / waves;
     const int64_t most = (int64_t)per * 256;
     const int grid = (int)(groups < most ? groups : most);
-    if (g.n % 4 == 0) k_thin<T, KS, GATED, true><<<grid, waves * 64, lds, st>>>(g, rc, np);
-    else k_thin<T, KS, GATED, false><<<grid, waves * 64, lds, st>>>(g, rc, np);
+    if (g.n % 4 == 0) k_thin<T, KS, NG, RF, GATED, true><<<grid, waves * 64, lds, st>>>(g, rc, np);
+    else k_thin<T, KS, NG, RF, GATED, false><<<grid, waves * 64, lds, st>>>(g, rc, np);
     return hipGetLastError();
 }
 
@@ -206,11 +233,18 @@ hipError_t launch_thin(const GemmArgs& g, int layout, hipStream_t st) {
     const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
     const ThinShape s = thin_shape(g.n, g.k, sizeof(T), gated, g.mode == GEMM_GATED_SLOPE);
     if (!s.waves) return hipErrorInvalidValue;
-    const size_t lds = thin_lds<T>(s.np, gated ? 2 : 1, s.steps, g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n, s.waves);
+    const size_t lds = thin_lds<T>(s.np, gated ? 2 : 1, s.steps, g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n, s.waves, s.rows);
     const bool rc = layout == GEMM_KC_RC;
     auto go = [&](auto ks) {
         constexpr int KS = decltype(ks)::value;
-        return gated ? start_thin<T, KS, true>(g, rc, s.np, s.waves, lds, st) : start_thin<T, KS, false>(g, rc, s.np, s.waves, lds, st);
+        auto start = [&](auto ng, auto rf) {
+            constexpr int NG = decltype(ng)::value, RF = decltype(rf)::value;
+            return gated ? start_thin<T, KS, NG, RF, true>(g, rc, s.np, s.waves, lds, st) : start_thin<T, KS, NG, RF, false>(g, rc, s.np, s.waves, lds, st);
+        };
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 2> two{};
+        if (s.rows == 16) return s.group == 1 ? start(one, one) : start(two, one);
+        return s.group == 1 ? start(one, two) : start(two, two);
     };
     switch (s.steps) {
     case 1: return go(std::integral_constant<int, 1>{});

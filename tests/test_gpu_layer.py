@@ -237,7 +237,7 @@ def test_large_tiles_and_long_sums(gated, shape, t):
 
 # a small weight under many rows: every number of 64-byte steps of a row, rows that are no pieces of 16 bytes, outputs that are no fours
 THIN = [(4096, 1, 1), (4097, 27, 121), (5003, 64, 72), (4100, 31, 33), (9999, 128, 4), (4111, 8, 130), (6000, 33, 64), (4127, 100, 5), (4128, 72, 64), (20001, 16, 31),
-        (4099, 127, 63), (131077, 12, 20), (4100, 24, 300), (4500, 65, 200)]
+        (4099, 127, 63), (131077, 12, 20), (4160, 72, 40), (4097, 128, 128), (4100, 80, 8), (5000, 8, 248), (33333, 64, 64), (4223, 40, 120), (4100, 24, 300), (4500, 65, 200)]
 
 
 @pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
