@@ -128,16 +128,18 @@ def load():
 
 _codes = {}          # torch dtype -> sr_dtype
 _current_device = None   # the current device's ordinal
+_raw = None              # ... and a device's current stream
 _raw_stream = None   # (device ordinal) -> hipStream_t of the device's current stream, without a Stream object
 
 
 def _bind_torch():
     """What a call needs of torch, looked up once: looking it up in every call was a third of the 8.4 us that a call with
     four tensors spent before the library (a small frame takes the GPU about as long)."""
-    global _raw_stream, _current_device
+    global _raw_stream, _current_device, _raw
     import torch
-    _current_device = torch.cuda.current_device
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _raw = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     if raw is not None:
         get_device = torch.cuda.current_device
         _raw_stream = lambda: raw(get_device())
@@ -540,9 +542,10 @@ _at = ctypes.byref
 
 
 def _code(dtype):
-    if not _codes:
-        _bind_torch()
     code = _codes.get(dtype)
+    if code is None and not _codes:
+        _bind_torch()
+        code = _codes.get(dtype)
     if code is None:
         raise TypeError(f"dtype {dtype} is not float32/float16/bfloat16")
     return code
@@ -618,7 +621,7 @@ def _room(workspace, need, like, stream, device):
 
 
 def sr_layer_linear_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
-    return int(load().sr_layer_linear_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+    return (_lib or load()).sr_layer_linear_workspace_bytes(rows, in_features, out_features, _code(dtype))
 
 
 def sr_layer_linear(x, weight, bias, act, residual, y, workspace=None, stream=None):
@@ -631,12 +634,12 @@ def sr_layer_linear(x, weight, bias, act, residual, y, workspace=None, stream=No
     workspace, room, size = _room(workspace, lambda: lib.sr_layer_linear_workspace_bytes(dx[2] * dx[4] * dx[5], dx[3], dy[3], dx[1]), x,
                                   stream, device)
     _check(lib.sr_layer_linear(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, None if residual is None else _at(d, _B3),
-                               _at(d, _B4), room, size, _stream(stream)))
+                               _at(d, _B4), room, size, _raw(device) if stream is None else _stream(stream)))
     return y
 
 
 def sr_layer_linear_grad_workspace_bytes(rows: int, in_features: int, out_features: int, dtype, act: int) -> int:
-    return int(load().sr_layer_linear_grad_workspace_bytes(rows, in_features, out_features, _code(dtype), act))
+    return (_lib or load()).sr_layer_linear_grad_workspace_bytes(rows, in_features, out_features, _code(dtype), act)
 
 
 def _layer_grad(call, need, x, weight, bias, act, dy, dx, dweight, dbias, workspace, stream, device):
@@ -646,7 +649,8 @@ def _layer_grad(call, need, x, weight, bias, act, dy, dx, dweight, dbias, worksp
            *_matrix(dweight, device), *_matrix(dbias, device))
     workspace, room, size = _room(workspace, lambda: need(rx[2] * rx[4] * rx[5], rx[3], ry[3], rx[1]), x, stream, device)
     _check(call(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, _at(d, _B3), None if dx is None else _at(d, _B4),
-                None if dweight is None else _at(d, _B5), None if dbias is None else _at(d, _B6), room, size, _stream(stream)))
+                None if dweight is None else _at(d, _B5), None if dbias is None else _at(d, _B6), room, size,
+                _raw(device) if stream is None else _stream(stream)))
     return dx, dweight, dbias
 
 
@@ -658,7 +662,7 @@ def sr_layer_linear_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace
 
 
 def sr_layer_gated_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
-    return int(load().sr_layer_gated_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+    return (_lib or load()).sr_layer_gated_workspace_bytes(rows, in_features, out_features, _code(dtype))
 
 
 def sr_layer_gated(x, weight, bias, act, y, workspace=None, stream=None):
@@ -669,12 +673,13 @@ def sr_layer_gated(x, weight, bias, act, y, workspace=None, stream=None):
     _fill5(d, 0, *dx, *_matrix(weight, device), *_matrix(bias, device), *dy, *_NONE)
     workspace, room, size = _room(workspace, lambda: lib.sr_layer_gated_workspace_bytes(dx[2] * dx[4] * dx[5], dx[3], dy[3], dx[1]), x,
                                   stream, device)
-    _check(lib.sr_layer_gated(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, _at(d, _B3), room, size, _stream(stream)))
+    _check(lib.sr_layer_gated(_at(d), _at(d, _B1), None if bias is None else _at(d, _B2), act, _at(d, _B3), room, size,
+                              _raw(device) if stream is None else _stream(stream)))
     return y
 
 
 def sr_layer_gated_grad_workspace_bytes(rows: int, in_features: int, out_features: int, dtype) -> int:
-    return int(load().sr_layer_gated_grad_workspace_bytes(rows, in_features, out_features, _code(dtype)))
+    return (_lib or load()).sr_layer_gated_grad_workspace_bytes(rows, in_features, out_features, _code(dtype))
 
 
 def sr_layer_gated_grad(x, weight, bias, act, dy, dx, dweight, dbias, workspace=None, stream=None):

@@ -51,14 +51,12 @@ template <typename T, typename F> __device__ __forceinline__ void edges(const Pa
     if (r.from + pieces >= r.body && (r.from < r.body || r.from == 0) && tail + (int64_t)threadIdx.x < r.count) f(tail + threadIdx.x);
 }
 
+// The last tensor that begins at or before the chunk: a lane looks at two, all at once (a search by halves waits for memory seven times).
 __device__ __forceinline__ int tensor_of(const ClipArgs& a, int chunk) {
-    int lo = 0, hi = a.tensors - 1;
-    while (lo < hi) {                                      // uniform
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.chunk[mid] <= chunk) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
+    static_assert(CLIP_TENSORS == 128, "two a lane");
+    const int lane = threadIdx.x & 63;
+    const bool lo = lane < a.tensors && a.chunk[lane] <= chunk, hi = 64 + lane < a.tensors && a.chunk[64 + lane] <= chunk;
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lo)) + __popcll(__ballot(hi)) - 1);
 }
 
 template <typename T> __device__ __forceinline__ void unpack(u32x4g v, float x[16 / sizeof(T)]) {
@@ -76,64 +74,61 @@ template <typename T> __device__ __forceinline__ void unpack(u32x4g v, float x[1
     }
 }
 
+// A thread's pieces of a chunk from `at` on, BATCH of them, all under way at once; what is behind the chunk's last is 0
+constexpr int BATCH = 8;
+template <typename T> __device__ __forceinline__ void ask(const void* p, const Part& r, int64_t at, u32x4g w[BATCH]) {
+    const u32x4g* const v = (const u32x4g*)((const T*)p + r.head) + at + threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) w[j] = at + threadIdx.x + j * CNT < r.to ? v[j * CNT] : u32x4g{0, 0, 0, 0};
+}
+
 template <typename T> __device__ __forceinline__ double squares(const void* p, int64_t count, int chunk, int pieces) {
     constexpr int E = 16 / sizeof(T);
     const Part r = part_of<T>(p, count, chunk, pieces);
     const T* const q = (const T*)p;
     double s = 0.0;
-    const u32x4g* const v = (const u32x4g*)(q + r.head);
-    int64_t i = r.from + threadIdx.x;
-    for (; i + 3 * CNT < r.to; i += 4 * CNT) {
-        u32x4g w[4];
+    for (int64_t at = r.from; at < r.to; at += BATCH * CNT) {
+        u32x4g w[BATCH];
+        ask<T>(p, r, at, w);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[i + j * CNT];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < BATCH; ++j) {
             float x[E];
             unpack<T>(w[j], x);
 #pragma unroll
             for (int e = 0; e < E; ++e) s = fma((double)x[e], (double)x[e], s);
         }
     }
-    for (; i < r.to; i += CNT) {
-        float x[E];
-        unpack<T>(v[i], x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) s = fma((double)x[e], (double)x[e], s);
-    }
     edges<T>(r, pieces, [&](int64_t e) { const double x = gm_get(q + e); s = fma(x, x, s); });
     return s;
 }
 
-template <typename T> __device__ __forceinline__ void scale(const void* p, void* o, int64_t count, int chunk, int pieces, float f) {
+// first: the first BATCH pieces of each thread are in w already
+template <typename T> __device__ __forceinline__ void scale(const void* p, void* o, int64_t count, int chunk, int pieces, float f, bool first, u32x4g w[BATCH]) {
     constexpr int E = 16 / sizeof(T);
     const Part r = part_of<T>(p, count, chunk, pieces);
     const T* const q = (const T*)p;
     T* const d = (T*)o;
-    const u32x4g* const v = (const u32x4g*)(q + r.head);
-    auto put = [&](int64_t i, u32x4g w) {
-        float x[E];
-        unpack<T>(w, x);
+    for (int64_t at = r.from; at < r.to; at += BATCH * CNT) {
+        if (!first) ask<T>(p, r, at, w);
+        first = false;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] *= f;
-        if constexpr (sizeof(T) == 4) {
-            u32x4u y;
+        for (int j = 0; j < BATCH; ++j) {
+            const int64_t i = at + threadIdx.x + j * CNT;
+            float x[E];
+            unpack<T>(w[j], x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(x[e]);
-            *(u32x4u*)(d + r.head + i * E) = y;
-        } else {
-            gm_put8(d + r.head + i * E, x);
+            for (int e = 0; e < E; ++e) x[e] *= f;
+            if (i >= r.to) continue;
+            if constexpr (sizeof(T) == 4) {
+                u32x4u y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(x[e]);
+                *(u32x4u*)(d + r.head + i * E) = y;
+            } else {
+                gm_put8(d + r.head + i * E, x);
+            }
         }
-    };
-    int64_t i = r.from + threadIdx.x;
-    for (; i + 3 * CNT < r.to; i += 4 * CNT) {
-        u32x4g w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[i + j * CNT];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) put(i + j * CNT, w[j]);
     }
-    for (; i < r.to; i += CNT) put(i, v[i]);
     edges<T>(r, pieces, [&](int64_t e) { gm_put(d + e, gm_get(q + e) * f); });
 }
 
@@ -163,17 +158,30 @@ __global__ __launch_bounds__(CNT) void k_clip_squares(const ClipArgs a) {
 }
 
 __global__ __launch_bounds__(CNT) void k_clip_scale(const ClipArgs a) {
+    // the first chunk's pieces are on their way while the sums are added up
+    u32x4g w[BATCH];
+    const int last = a.chunk[a.tensors] - 1 - (int)blockIdx.x;
+    if (last >= 0) {
+        const int t = tensor_of(a, last), at = last - a.chunk[t];
+        if (a.type[t] == SR_F32) {
+            const Part r = part_of<float>(a.in[t], a.count[t], at, a.pieces);
+            ask<float>(a.in[t], r, r.from, w);
+        } else {
+            const Part r = part_of<__half>(a.in[t], a.count[t], at, a.pieces);
+            ask<__half>(a.in[t], r, r.from, w);
+        }
+    }
     double s = 0.0;
     for (int i = threadIdx.x; i < a.records; i += CNT) s += a.partial[i];
     const double norm = sqrt(block_sum(s));
     const float factor = norm > a.most && norm < INFINITY ? (float)(a.most / norm) : 1.0f;
     if (a.tells && blockIdx.x == 0 && threadIdx.x == 0) a.norm[0] = (float)norm, a.norm[1] = factor;
-    for (int c = a.chunk[a.tensors] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+    for (int c = last; c >= 0; c -= gridDim.x) {
         const int t = tensor_of(a, c), at = c - a.chunk[t];
         if (factor == 1.0f && a.out[t] == a.in[t]) continue;
-        if (a.type[t] == SR_F32) scale<float>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor);
-        else if (a.type[t] == SR_F16) scale<__half>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor);
-        else scale<bf16raw>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor);
+        if (a.type[t] == SR_F32) scale<float>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor, c == last, w);
+        else if (a.type[t] == SR_F16) scale<__half>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor, c == last, w);
+        else scale<bf16raw>(a.in[t], a.out[t], a.count[t], at, a.pieces, factor, c == last, w);
     }
 }
 

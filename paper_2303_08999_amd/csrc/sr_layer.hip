@@ -72,7 +72,9 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
     for (int tile = 0; tile < 4; ++tile) {
         const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
         auto look = [&](int64_t splits) {
-            if (splits < 1 || (splits > 1 && (splits > steps / 4 || splits > 1024))) return;
+            if (splits > steps / 2) splits = steps / 2;
+            if (splits > 1024) splits = 1024;
+            if (splits < 1) splits = 1;
             const int64_t each = steps ? (steps + splits - 1) / splits : 0;
             splits = steps ? (steps + each - 1) / each : 1;
             double us = tile_time(tile, (tiles * splits + GPU_CUS - 1) / GPU_CUS, each, es);

@@ -12,7 +12,7 @@ constexpr int SKW = 8;             // wavefronts of a workgroup
 // eight wavefronts take every eighth step of k and add up in LDS.  Bound by the weights' way from memory and, for small ones, by the launch.
 template <typename T, bool GATED, int RF, bool ALIGNED>
 __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
-    constexpr int E = 16 / sizeof(T), H = GATED ? 2 : 1, AHEAD = RF > 2 ? 2 : 4;
+    constexpr int E = 16 / sizeof(T), H = GATED ? 2 : 1, AHEAD = RF > 2 ? 2 : RF > 1 || GATED ? 4 : 8;
     __shared__ __align__(16) float sh[SKW * H * RF * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = blockIdx.x * 16, r = lane % 16;
@@ -25,6 +25,16 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
         for (int h = 0; h < H; ++h) pb[h] = (const T*)g.b + (int64_t)(n + h * g.half) * g.ldb + kc;
 #pragma unroll
         for (int f = 0; f < RF; ++f) pa[f] = (const T*)g.a + (int64_t)(16 * f + r < g.m ? 16 * f + r : g.m - 1) * g.lda + kc;
+    }
+    // What finishes 8 columns of a row is asked for first, by the lane that will finish them.
+    const int fm = threadIdx.x / 2, fc = threadIdx.x % 2 * 8, col = n0 + fc;
+    const bool finishes = threadIdx.x < 32 * RF && fm < g.m && col < g.n;
+    Raw8<T> bias[H], extra;
+    if (finishes) {
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+            if (g.bias) bias[h].get((const T*)g.bias + h * g.half + col, g.n - col);
+        if (g.extra) extra.get((const T*)g.extra + fm * g.ld_extra + col, g.n - col);
     }
     f32x4g acc[H][RF];
 #pragma unroll
@@ -65,17 +75,23 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
         sh[i] = s;                                         // read by this thread alone
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 32 * RF; i += SKW * 64) {
-        const int m = i / 2, c = i % 2 * 8, col = n0 + c;
-        if (m >= g.m || col >= g.n) continue;
-        float z[1][8], u[1][8];
+    if (!finishes) return;
+    float z[1][8], u[1][8], e[1][8], add[H][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            z[0][e] = sh[m * 16 + c + e];
-            u[0][e] = GATED ? sh[RF * 256 + m * 16 + c + e] : 0.0f;
-        }
-        gm_finish8<T, GATED>(g, m, col, z, u);
+    for (int i = 0; i < 8; ++i) {
+        z[0][i] = sh[fm * 16 + fc + i];
+        u[0][i] = GATED ? sh[RF * 256 + fm * 16 + fc + i] : 0.0f;
+        e[0][i] = 0.0f;
     }
+    if (g.bias) {
+#pragma unroll
+        for (int h = 0; h < H; ++h) bias[h].values(add[h]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[0][i] += add[0][i], u[0][i] += add[H - 1][i];
+    }
+    if (g.extra) extra.values(e[0]);
+    gm_finish<GATED, 1>(g, z, u, e);
+    gm_put_some((T*)g.out + fm * g.ld_out + col, g.n - col, z[0]);
 }
 
 // 8 columns of a row for a group of SL threads, each every SL-th split, in double; what follows is as in the tile kernel.  Behind the rows of C
