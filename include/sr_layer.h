@@ -11,12 +11,12 @@
  *     linear   z = x W^T + b                     y = act(z) + residual
  *     gated    g = x Wg^T + bg, u = x Wu^T + bu  y = act(g) u         (W = Wg on top of Wu, b = bg, bu)
  *
- * All tensors of a call have one type, f32, f16 or bf16.  Products of the stored values are exact and
- * summed in fp32 or better; bias, activation and the rest are fp32; each output is rounded once.  Only
- * the gradient of z is rounded to the tensors' type on its way between two products, where an activation or
- * a gate makes it: it is an operand of 16-bit matrix instructions then, and the next products of a training
- * step round it the same way.  Infinities and NaN stay in the rows and columns to which the formulas take
- * them; in a gradient, z of an infinite size gives NaN.
+ * All tensors of a call have one type, f32, f16 or bf16.  Products are summed in fp32 or better; those of
+ * 16-bit values are exact, those of f32 values are within 2^-24 of themselves.  Bias, activation and the rest are
+ * fp32; each output is rounded once.  Only the gradient of z is rounded to the tensors' type on its way
+ * between two products, where an activation or a gate makes it: it is an operand of 16-bit matrix instructions
+ * then, and the next products of a training step round it the same way.  Infinities and NaN in the inputs stay
+ * in the rows and columns to which the formulas take them; what an infinity makes there may be NaN.
  *
  * All rules of sr_dict.h hold: contiguous device memory of the caller at any address aligned to its elements,
  * every check on the host before anything is launched, its statuses, no allocation, no synchronisation, work

@@ -279,6 +279,32 @@ template <typename T, int MT> __device__ __forceinline__ void gm_mul(typename Ac
         else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8g, a), __builtin_bit_cast(bf8g, b), c, 0, 0, 0);
     }
 }
+// fp32 on the bfloat16 matrix instructions, sixteen times as fast as the fp32 ones: eight values as the sum of three bfloat16 numbers each, x = h + m + l
+// exactly (8 bits are rounded off to the nearest twice, what is left has 8), and of the nine products of two such sums the six that are above 2^-26
+// of x y.  Summed in fp32 like the others.  Two of these a value and three conversions a pair: a third of the matrix instructions' time where
+// a wavefront makes 64 x 64.  4096^3: 145 TFLOP/s by fp32 instructions.
+struct Split8 { u32x4g h, m, l; };
+__device__ __forceinline__ Split8 gm_split(u32x4g a, u32x4g b) {
+    using bf2g = __attribute__((ext_vector_type(2))) __bf16;
+    Split8 s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x = __uint_as_float((unsigned)(i < 2 ? a[2 * i] : b[2 * i - 4])), y = __uint_as_float((unsigned)(i < 2 ? a[2 * i + 1] : b[2 * i - 3]));
+        const unsigned h = __builtin_bit_cast(unsigned, bf2g{(__bf16)x, (__bf16)y});
+        x -= __uint_as_float(h << 16), y -= __uint_as_float(h & 0xffff0000u);
+        const unsigned m = __builtin_bit_cast(unsigned, bf2g{(__bf16)x, (__bf16)y});
+        x -= __uint_as_float(m << 16), y -= __uint_as_float(m & 0xffff0000u);
+        s.h[i] = h;
+        s.m[i] = m;
+        s.l[i] = __builtin_bit_cast(unsigned, bf2g{(__bf16)x, (__bf16)y});
+    }
+    return s;
+}
+// the six products, the small ones first
+template <int MT> __device__ __forceinline__ void gm_mul_part(typename AccOf<MT>::type& c, const Split8& a, const Split8& b, int part) {
+    const u32x4g x = part == 0 ? a.l : part == 2 || part == 3 ? a.m : a.h, y = part == 1 ? b.l : part == 2 || part == 4 ? b.m : b.h;
+    gm_mul<bf16raw, MT>(c, x, y);
+}
 // of the one or two values in 32 bits of a fragment
 template <typename T> __device__ __forceinline__ float gm_sum(unsigned v) {
     if constexpr (sizeof(T) == 4) {

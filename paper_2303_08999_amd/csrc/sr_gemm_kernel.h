@@ -18,7 +18,8 @@ template <int TILE, typename T> struct GemmShape;
 template <typename T> struct GemmShape<0, T> { static constexpr int BM = 64, BN = 64, WM = 32, WN = 32, MT = 16, OCC = 3; static constexpr bool PIPE = false; };
 template <typename T> struct GemmShape<1, T> { static constexpr int BM = 128, BN = 128, WM = 64, WN = 64, MT = 32, OCC = 2; static constexpr bool PIPE = false; };
 template <typename T> struct GemmShape<2, T> { static constexpr int BM = 256, BN = 128, WM = 128, WN = 64, MT = sizeof(T) == 2 ? 16 : 32, OCC = 1; static constexpr bool PIPE = true; };
-// 16-bit types: instructions of 16 rows (8192^3, fp16: 801 us, of 32 rows 876); fp32: of 32 (8192 x 4096 x 4096: 1857 us, of 16 rows 2115)
+// 16-bit types: instructions of 16 rows (8192^3, fp16: 801 us, of 32 rows 876).  fp32 multiplies its three parts in instructions of 32 rows; the smallest tile
+// stays with fp32 instructions, where a wavefront has two parts to make for each product (4096^3: 954 us, by parts 1016).
 template <typename T> struct GemmShape<3, T> { static constexpr int BM = 256, BN = 256, WM = 128, WN = 128, MT = sizeof(T) == 2 ? 16 : 32, OCC = 1; static constexpr bool PIPE = true; };
 
 template <int TILE, typename T>
@@ -224,6 +225,28 @@ void k_gemm(const GemmArgs g) {
     };
 
     auto multiply = [&](const char* s, bool sums) {
+        if constexpr (sizeof(T) == 4 && MT == 32) {
+#pragma unroll
+            for (int step = 0; step < STEPS; step += 2) {
+                Split8 fa[FM], fb[FN];
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    const u32x4g lo = ra(s, i, step), hi = ra(s, i, step + 1);
+                    if constexpr (ARC)
+                        if (sums) add_sum(i, lo), add_sum(i, hi);
+                    fa[i] = gm_split(lo, hi);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[j] = gm_split(rb(s + OpA::BYTES, j, step), rb(s + OpA::BYTES, j, step + 1));
+#pragma unroll
+                for (int part = 0; part < 6; ++part)
+#pragma unroll
+                    for (int i = 0; i < FM; ++i)
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) gm_mul_part<MT>(acc[i][j], fb[j], fa[i], part);
+            }
+            return;
+        }
 #pragma unroll
         for (int step = 0; step < STEPS; ++step) {
             u32x4g fa[FM], fb[FN];
@@ -271,6 +294,74 @@ void k_gemm(const GemmArgs g) {
                 // it, and the next one, started a tile's time before, is there.
                 static_assert(STEPS >= 2 && STEPS % 2 == 0, "fragments of two steps in turn");
                 constexpr int NM = FM * FN, NR = FM + FN, NL = OpA::LOADS + OpB::LOADS;
+                auto fetch = [&](char* s, int q) {
+                    if (q < OpA::LOADS) oa.fetch(s, wave, q);
+                    else ob.fetch(s + OpA::BYTES, wave, q - OpA::LOADS);
+                };
+                auto advance = [&] {
+                    oa.advance(step_a);
+                    ob.advance(step_b);
+                };
+                auto none = [](int) {};
+                if constexpr (sizeof(T) == 4) {
+                    // Two steps at once, as three parts; their values are read while those of the two before are multiplied.
+                    constexpr int DOUBLE = STEPS / 2, ALL = 6 * NM;
+                    u32x4g fa[FM][2], fb[FN][2];
+                    auto read = [&](const char* s, int pair, int q) {
+                        if (q < 2 * FM) fa[q / 2][q % 2] = ra(s, q / 2, 2 * pair + q % 2);
+                        else fb[q / 2 - FM][q % 2] = rb(s + OpA::BYTES, q / 2 - FM, 2 * pair + q % 2);
+                    };
+                    auto step = [&](const char* s, int next, auto load) {
+                        Split8 pa[FM], pb[FN];
+#pragma unroll
+                        for (int i = 0; i < FM; ++i) {
+                            if constexpr (SUMS) add_sum(i, fa[i][0]), add_sum(i, fa[i][1]);
+                            pa[i] = gm_split(fa[i][0], fa[i][1]);
+                        }
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) pb[j] = gm_split(fb[j][0], fb[j][1]);
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int q = 0; q < ALL; ++q) {
+                            gm_mul_part<MT>(acc[q % NM / FN][q % FN], pb[q % FN], pa[q % NM / FN], q / NM);
+                            const int r0 = 4 * q * NR / ALL, r1 = 4 * (q + 1) * NR / ALL, l0 = q * NL / ALL, l1 = (q + 1) * NL / ALL;
+                            if ((r1 > r0 && r0 < 2 * NR) || l1 > l0) {
+                                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                                for (int r = r0; r < r1; ++r)
+                                    if (r < 2 * NR) read(s, next, r);
+#pragma unroll
+                                for (int l = l0; l < l1; ++l) load(l);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                        }
+                    };
+                    auto tile = [&](auto later) {
+                        char *const now = lds + buf * STAGE, *const next = lds + (buf ^ 1) * STAGE;
+#pragma unroll
+                        for (int i = 0; i + 1 < DOUBLE; ++i) step(now, i + 1, none);
+                        landed();
+                        step(next, 0, [&](int q) {
+                            if constexpr (decltype(later)::value) fetch(now, q);
+                        });
+                        advance();
+                        buf ^= 1;
+                    };
+                    landed();
+                    if (full + (tail ? 1 : 0) > 0) {
+#pragma unroll
+                        for (int q = 0; q < 2 * NR; ++q) read(lds, 0, q);
+                        if (left > 0) {
+#pragma unroll
+                            for (int q = 0; q < NL; ++q) fetch(lds + STAGE, q);
+                            advance();
+                            for (; left > 1; --left) tile(std::true_type{});
+                            tile(std::false_type{});
+                        }
+                        tile(std::false_type{});
+                    }
+                    return;
+                }
                 u32x4g fa[2][FM], fb[2][FN];
                 auto read = [&](int into, const char* s, int step, int q) {
                     if (q < FM) fa[into][q] = ra(s, q, step);
@@ -297,15 +388,6 @@ void k_gemm(const GemmArgs g) {
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
-                };
-                auto none = [](int) {};
-                auto fetch = [&](char* s, int q) {
-                    if (q < OpA::LOADS) oa.fetch(s, wave, q);
-                    else ob.fetch(s + OpA::BYTES, wave, q - OpA::LOADS);
-                };
-                auto advance = [&] {
-                    oa.advance(step_a);
-                    ob.advance(step_b);
                 };
                 // `later`: the tile behind the next is still to be fetched
                 auto tile = [&](auto later) {
@@ -499,8 +581,9 @@ hipError_t start_gemm(const GemmArgs& g, hipStream_t st) {
 template <typename T, int LAYOUT, bool GATED>
 hipError_t pick_gemm(const GemmArgs& g, bool aligned, int tile, hipStream_t st) {
     if (!aligned) return tile == 0 ? start_gemm<T, LAYOUT, GATED, false, 0>(g, st) : start_gemm<T, LAYOUT, GATED, false, 1>(g, st);
-    return tile == 0 ? start_gemm<T, LAYOUT, GATED, true, 0>(g, st) : tile == 1 ? start_gemm<T, LAYOUT, GATED, true, 1>(g, st)
-         : tile == 2 ? start_gemm<T, LAYOUT, GATED, true, 2>(g, st) : start_gemm<T, LAYOUT, GATED, true, 3>(g, st);
+    if (tile == 0) return start_gemm<T, LAYOUT, GATED, true, 0>(g, st);
+    if (tile == 1) return start_gemm<T, LAYOUT, GATED, true, 1>(g, st);
+    return tile == 2 ? start_gemm<T, LAYOUT, GATED, true, 2>(g, st) : start_gemm<T, LAYOUT, GATED, true, 3>(g, st);
 }
 
 }  // namespace

@@ -46,7 +46,7 @@ struct Cut { int tile, splits, ksplit; };
 // where `share` of them keep a unit busy, and what a round of them takes beside that.  Measured with 1, 2, 4 and 8 workgroups a unit and k
 // from 64 to 8192.
 double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
-    static const double alone[2][4] = {{0.30, 0.58, 0.79, 1.28}, {0.62, 2.05, 3.70, 7.25}}, full[2][4] = {{0.19, 0.485, 0.79, 1.28}, {0.47, 1.84, 3.70, 7.25}};
+    static const double alone[2][4] = {{0.30, 0.58, 0.79, 1.28}, {0.62, 1.58, 2.67, 4.77}}, full[2][4] = {{0.19, 0.485, 0.79, 1.28}, {0.47, 1.46, 2.67, 4.77}};
     static const double round[4] = {3.0, 5.0, 9.0, 13.0};
     static const int share[4] = {4, 2, 1, 1};
     const int f = es == 4;
