@@ -728,30 +728,33 @@ class sr_tensor_list:
 
 
 def sr_grad_clip_workspace_bytes(tensors: int) -> int:
-    return int(load().sr_grad_clip_workspace_bytes(int(tensors)))
+    return (_lib or load()).sr_grad_clip_workspace_bytes(tensors)
 
 
 def sr_grad_clip(grads, outs, max_norm, norm, workspace=None, stream=None):
     """The norm over all ``grads`` and the factor to at most ``max_norm``, into ``norm`` (float32, 2), and the gradients times that
     factor into ``outs`` (``grads`` itself: in place; None: the norm alone).  Both are lists of tensors, or sr_tensor_list."""
     import torch
-    given = grads
-    if not isinstance(grads, sr_tensor_list):
-        grads = sr_tensor_list(grads)
-    if outs is given:
-        outs = grads
-    elif outs is not None and not isinstance(outs, sr_tensor_list):
-        outs = sr_tensor_list(outs)
-    if outs is not None and outs is not grads:
-        if len(outs) != len(grads):
+    lib = _lib or load()
+    described = grads if isinstance(grads, sr_tensor_list) else sr_tensor_list(grads)
+    count = len(described.tensors)
+    if outs is None:
+        into = None
+    elif outs is grads:
+        into = described.array
+    else:
+        out = outs if isinstance(outs, sr_tensor_list) else sr_tensor_list(outs)
+        if len(out.tensors) != count:
             raise ValueError("as many outputs as gradients")
-        if outs.strides != grads.strides:
+        if out.strides != described.strides:
             raise ValueError("an output is stored in another order than its gradient")
-    for a in (grads, outs):
-        if a is not None and len(a) and a.device != torch.cuda.current_device():
-            raise ValueError("a list is not on the current device")
-    _here(norm, workspace)
-    workspace = _scratch(workspace, sr_grad_clip_workspace_bytes(len(grads)), norm, stream)
-    _check(load().sr_grad_clip(grads.array, None if outs is None else outs.array, len(grads), max_norm, _plain(norm, torch.float32, 2, "norm"),
-                               ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(), _stream(stream)))
+        if count and out.device != described.device:
+            raise ValueError("the outputs are on another device than the gradients")
+        into = out.array
+    device = _on(norm)
+    if count and described.device != device:
+        raise ValueError("the gradients are not on the current device")
+    workspace, room, size = _room(workspace, lambda: lib.sr_grad_clip_workspace_bytes(count), norm, stream, device)
+    _check(lib.sr_grad_clip(described.array, into, count, max_norm, _plain(norm, torch.float32, 2, "norm"), room, size,
+                            _raw(device) if stream is None else _stream(stream)))
     return outs, norm
