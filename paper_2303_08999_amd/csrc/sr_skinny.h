@@ -106,7 +106,7 @@ template <typename T, int SL>
 __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
     const GemmArgs& g = f.g;
     constexpr int PER = 256 / SL;
-    __shared__ double sh[SL > 1 ? 16 * 256 : 1];
+    __shared__ double sh[SL > 1 ? 16 * 256 : 1];           // [16 values][SL][PER]
     const int slot = threadIdx.x % PER, slice = threadIdx.x / PER;
     const int64_t o = (int64_t)blockIdx.x * PER + slot;
     const bool in_sums = o >= f.all;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) zd[i] = ud[i] = 0.0;
     if (any) {
-#pragma unroll 4
+#pragma unroll 8
         for (int s = slice; s < g.splits; s += SL) {
             float v[8];
             gm_get_some(p + s * step, count, v);
@@ -138,10 +138,17 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sh[(i * SL + slice) * PER + slot] = zd[i], sh[((8 + i) * SL + slice) * PER + slot] = ud[i];
         __syncthreads();
+        if (threadIdx.x < 16 * PER) {                      // a value of a slot each, over the slices
+            double* const v = sh + threadIdx.x / PER * 256 + threadIdx.x % PER;
+            double sum = v[0];
+#pragma unroll 8
+            for (int i = 1; i < SL; ++i) sum += v[i * PER];
+            v[0] = sum;
+        }
+        __syncthreads();
         if (slice == 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                for (int s = 1; s < SL; ++s) zd[i] += sh[(i * SL + s) * PER + slot], ud[i] += sh[((8 + i) * SL + s) * PER + slot];
+            for (int i = 0; i < 8; ++i) zd[i] = sh[i * 256 + slot], ud[i] = sh[(8 + i) * 256 + slot];
         }
     }
     if (!any || slice != 0) return;
@@ -179,8 +186,10 @@ hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st) {
     f.octets = (g.n + 7) / 8;
     f.all = (int64_t)(g.partial ? g.m : 0) * f.octets;
     const int64_t all = f.all + (g.sums ? (g.m + 7) / 8 : 0);
-    if (g.splits <= 16) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
-    else k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
+    // so many slices that a thread's loads are all under way at once (512 splits of 72 x 64: 11.4 us in 16 slices)
+    if (g.splits <= 8) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
+    else if (g.splits <= 128) k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
+    else k_gemm_finish<T, 64><<<(int)((all + 3) / 4), 256, 0, st>>>(f);
     return hipGetLastError();
 }
 

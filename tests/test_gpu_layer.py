@@ -362,3 +362,56 @@ def test_other_streams_and_captured_graphs():
         now = [run_forward(d, "bf16", lo.SILU, True)] + run_grad(d, "bf16", lo.SILU, True)
         for a, b in zip(outs, now):
             assert torch.equal(a, b), f"replay {i}"
+
+
+@pytest.mark.parametrize("P,C,O", [((1 << 25) + 77, 128, 8), ((1 << 23) + 33, 520, 24)], ids=["small_weight", "tiles"])
+def test_more_elements_than_32_bits_count(P, C, O):
+    """x has more than 2^32 elements; all rows but a few, some of them the last, are zeros."""
+    assert P * C > 1 << 32
+    g = torch.Generator(device=DEV).manual_seed(3)
+    at = torch.tensor([0, 1, 4095, P // 2, P - 130, P - 2, P - 1], device=DEV)
+    x = torch.zeros((P, C), device=DEV, dtype=torch.bfloat16)
+    x[at] = torch.randn((7, C), generator=g, device=DEV).bfloat16()
+    w, b = (torch.randn((O, C), generator=g, device=DEV) / 16).bfloat16(), torch.randn(O, generator=g, device=DEV).bfloat16()
+    y = torch.empty((P, O), device=DEV, dtype=torch.bfloat16)
+    sr.sr_layer_linear(x, w, b, lo.NONE, None, y)
+    few = {"x": x[at], "w": w, "b": b, "dy": torch.zeros((7, O), device=DEV), "res": None}
+    want, bound = forward_bound("bf16", wide64(few), lo.NONE, False)
+    compare("y", y[at], want, bound)
+    assert torch.equal(y[2:4095], b.expand(4093, O)) and torch.equal(y[P - 129:P - 2], b.expand(127, O))
+    dy = torch.zeros((P, O), device=DEV, dtype=torch.bfloat16)
+    dy[at] = torch.randn((7, O), generator=g, device=DEV).bfloat16()
+    dx, dw, db = torch.full_like(x, 3.0), torch.empty_like(w), torch.empty_like(b)
+    sr.sr_layer_linear_grad(x, w, b, lo.NONE, dy, dx, dw, db)
+    few["dy"] = dy[at]
+    e = wide64(few)
+    for name, got, (want, bound) in zip(("dx", "dweight", "dbias"), (dx[at], dw, db), behind_bound("bf16", e, e["dy"], torch.zeros_like(e["dy"]))):
+        compare(name, got, want, bound)
+    assert not dx[2:4095].any() and not dx[P - 129:P - 2].any() and int((dx != 0).any(1).sum()) == 7
+
+
+def test_the_bounds_tell_mistakes_apart():
+    """Each of these mistakes, made in the oracle, leaves the bound that the kernels keep."""
+    d = inputs(300, 72, 88, "bf16", False, 21, residual=True)
+    y = run_forward(d, "bf16", lo.GELU, False).double()
+    e = wide64(d)
+    want, bound = forward_bound("bf16", e, lo.GELU, False)
+    z = lo.affine(e["x"], e["w"], e["b"])
+    mistakes = {"no bias": lo.act(lo.GELU, z - e["b"]) + e["res"], "residual inside": lo.act(lo.GELU, z + e["res"]), "no residual": lo.act(lo.GELU, z),
+                "silu": lo.act(lo.SILU, z) + e["res"],
+                "a k less": lo.act(lo.GELU, z - e["x"][:, -1:] * e["w"][:, -1]) + e["res"], "rows shifted": want.roll(1, 0), "columns shifted": want.roll(1, 1)}
+    assert ((y - want).abs() <= bound).all()
+    for name, wrong in mistakes.items():
+        assert not ((y - wrong).abs() <= bound).all(), name
+    d = inputs(300, 72, 88, "bf16", True, 22)
+    e = wide64(d)
+    dx, dw, db = (v.double() for v in run_grad(d, "bf16", lo.SILU, True))
+    dz, edz = dz_bound("bf16", e, lo.SILU, True)
+    bounds = [b for _, b in behind_bound("bf16", e, dz, edz)]
+    g, u = lo.affine(e["x"], e["w"], e["b"]).chunk(2, 1)
+    dg, du = dz.chunk(2, 1)
+    mistakes = {"halves exchanged": torch.cat([du, dg], 1), "value for slope": torch.cat([e["dy"] * u * lo.act(lo.SILU, g), du], 1),
+                "no product": torch.cat([e["dy"] * lo.slope(lo.SILU, g), du], 1), "a row less": torch.cat([dz[:-1], torch.zeros_like(dz[:1])])}
+    for name, wrong in mistakes.items():
+        wx, ww, wb = lo.behind_dz(e["x"], e["w"], wrong)
+        assert not (((dx - wx).abs() <= bounds[0]).all() and ((dw - ww).abs() <= bounds[1]).all() and ((db - wb).abs() <= bounds[2]).all()), name
