@@ -210,8 +210,10 @@ hipError_t pick_thin_grad(const ThinGradArgs& a, int grid, hipStream_t st) {
     };
     auto rows = [&](auto nt) {
         if (wide <= 64) return go(nt, std::integral_constant<int, 1>{});
-        if (wide <= 128) return go(nt, std::integral_constant<int, 2>{});
-        return go(nt, std::integral_constant<int, 4>{});
+        if constexpr (decltype(nt)::value < 8) {
+            if (wide > 128) return go(nt, std::integral_constant<int, 4>{});
+        }
+        return go(nt, std::integral_constant<int, 2>{});
     };
     if (a.c <= 32) return rows(std::integral_constant<int, 2>{});
     if (a.c <= 64) return rows(std::integral_constant<int, 4>{});
