@@ -168,6 +168,7 @@ void k_gemm(const GemmArgs g) {
     using OpB = Operand<T, BN, NW, BRC, MT, GATED>;
     constexpr int BK = OpA::BK, STEPS = 8 * MT / 64;
     constexpr int PR = S::PIPE ? 64 : 32, STRIDE = WN + 4, PATCH = PR * STRIDE * 4;      // a wavefront's part of the way out: rows, bytes
+    static_assert(BM / WM == 2, "rows of the output's sums");
     constexpr int STAGE = OpA::BYTES + OpB::BYTES, LDS = 2 * STAGE > NW * PATCH ? 2 * STAGE : NW * PATCH;
     __shared__ __align__(1024) char lds[LDS];
     using Acc = typename AccOf<MT>::type;
@@ -220,7 +221,7 @@ void k_gemm(const GemmArgs g) {
             gm_mul<T, MT>(sum[i], u32x4g{one, one, one, one}, f);
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[i] += gm_sum<T>(f[j]);
+            for (int j = 0; j < 4; ++j) sum[i] = gm_sum<T>(f[j], sum[i]);
         }
     };
 
@@ -375,7 +376,7 @@ void k_gemm(const GemmArgs g) {
                         gm_mul<T, MT>(acc[q / FN][q % FN], fb[now][q % FN], fa[now][q / FN]);
                         if constexpr (SUMS) {
 #pragma unroll
-                            for (int d = q * 4 * FM / NM; d < (q + 1) * 4 * FM / NM; ++d) sum[d / 4] += gm_sum<T>(fa[now][d / 4][d % 4]);
+                            for (int d = q * 4 * FM / NM; d < (q + 1) * 4 * FM / NM; ++d) sum[d / 4] = gm_sum<T>(fa[now][d / 4][d % 4], sum[d / 4]);
                         }
                         const int r0 = 2 * q * NR / NM, r1 = 2 * (q + 1) * NR / NM, l0 = q * NL / NM, l1 = (q + 1) * NL / NM;
                         if ((r1 > r0 && r0 < NR) || l1 > l0) {
@@ -501,6 +502,12 @@ void k_gemm(const GemmArgs g) {
         }
     };
     if (extra) ask(0);
+    // sums of dz over the rows (db), on the way: beside dW's matrix instructions they cost the workgroups that take them a sixth (8192 rows of 2048 to
+    // 4096: 14 us of 146)
+    constexpr bool SLOPES = LAYOUT == GEMM_KC_KC;
+    float sz[8], su[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sz[i] = su[i] = 0.0f;
     float bz[8], bu[8];
     if (g.mode != GEMM_PARTIAL) gm_bias8<T>(g, col, GATED, bz, bu);
 #pragma unroll
@@ -561,6 +568,13 @@ void k_gemm(const GemmArgs g) {
             for (int r = 0; r < U; ++r) {
                 const int m = first + r * RI;
                 if (m < g.m && count > 0) {
+                    if (SLOPES && g.sums) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            sz[i] += z[r][i];
+                            if constexpr (GATED) su[i] += u[r][i];
+                        }
+                    }
                     T* const out = (T*)g.out + (int64_t)m * g.ld_out + col;
                     gm_put_some(out, count, z[r]);
                     if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[r]);
@@ -568,6 +582,20 @@ void k_gemm(const GemmArgs g) {
             }
         }
         __builtin_amdgcn_wave_barrier();
+    }
+    if (SLOPES && g.sums && g.mode != GEMM_PARTIAL) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int d = LR; d < 64; d <<= 1) {
+                sz[i] += __shfl_xor(sz[i], d);
+                if constexpr (GATED) su[i] += __shfl_xor(su[i], d);
+            }
+        if (lr == 0 && count > 0) {
+            float* const s = g.sums + (int64_t)(2 * tm + wm / WM) * (GATED ? 2 * (int64_t)g.half : g.n) + col;
+            gm_put_some(s, count, sz);
+            if (GATED) gm_put_some(s + g.half, count, su);
+        }
     }
 }
 

@@ -58,7 +58,8 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 // From here on rows with a weight that fits go to the kernel for them; where that takes 16 at a time (500 000 of 128 to 128, bfloat16: 58 us, tiles 47), only
 // if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
-// The cut that should take least.  Split sums cost their way through memory, written and read in fp32 at 4.5 bytes a ps, and a launch.
+// The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
+// caches, at 4.5 past them.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0};
@@ -78,7 +79,8 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
             const int64_t each = steps ? (steps + splits - 1) / splits : 0;
             splits = steps ? (steps + each - 1) / each : 1;
             double us = tile_time(tile, (tiles * splits + GPU_CUS - 1) / GPU_CUS, each, es);
-            if (splits > 1) us += 3.0 + 8.0 * (double)splits * (double)m * (double)nn / 4.5e6;
+            const double mb = 8e-6 * (double)splits * (double)m * (double)nn;
+            if (splits > 1) us += 3.0 + mb / (mb < 128.0 ? 8.0 : 4.5);
             if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk)};
         };
         for (int s = 1; s <= 8; ++s) look(s);
@@ -92,6 +94,15 @@ size_t partial_bytes(const Cut& c, int64_t m, int64_t width) { return c.splits >
 
 template <typename F> hipError_t by_type(int d, F f) {
     return d == SR_F32 ? f((float*)nullptr) : d == SR_F16 ? f((__half*)nullptr) : f((bf16raw*)nullptr);
+}
+
+// Whether the product that makes z sums dz over the rows too, and the scratch that takes (tiles of 128 rows where the operands are off 16-byte pieces): a
+// launch more, 4 us (gradient of 4096 rows of 64 to 128, gated, fp32: 22.8 us, so 27.6), which the large tiles' sums beside dW cost more than (8192 rows
+// of 2048 to 4096: 429 us, so 386).
+bool sums_slopes(const Cut& z, const Cut& w) { return z.tile >= 0 && z.splits == 1 && w.tile >= 2; }
+size_t slope_sum_bytes(const Cut& c, int64_t m, int64_t width) {
+    const int64_t rows = gemm_tile_rows(c.tile > 1 ? 1 : c.tile);
+    return up256((size_t)(2 * ((m + rows - 1) / rows)) * width * 4);
 }
 
 // One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, where
@@ -113,7 +124,17 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         if (g.splits == 1) {
             g.tiles_n = g.out ? (int)(((int64_t)(gated ? 2 : 1) * g.n + cols - 1) / cols) : 1;      // without: the sums of dz alone
             if (g.ksplit == 0) g.ksplit = g.k;
-            return launch_gemm<T>(g, layout, aligned, tile, st);
+            const bool slopes = layout == GEMM_KC_KC && g.sums_out;      // db from the products' epilogue
+            if (slopes) g.sums = (float*)ws;
+            const hipError_t e = launch_gemm<T>(g, layout, aligned, tile, st);
+            if (e != hipSuccess || !slopes) return e;
+            GemmArgs f = {};
+            f.m = gated ? 2 * g.half : g.n;
+            f.n = 1;
+            f.splits = 2 * g.tiles_m;
+            f.sums = g.sums;
+            f.sums_out = g.sums_out;
+            return launch_gemm_finish<T>(f, st);
         }
         GemmArgs p = g;
         p.mode = GEMM_PARTIAL;
@@ -158,7 +179,7 @@ GradPlan grad_plan(const Layer& l, int act) {
     size_t most = partial_bytes(p.x, l.rows, l.in);
     if (p.dz) {
         p.z = forward_cut(l);
-        const size_t z = forward_scratch(l, p.z);
+        const size_t z = sums_slopes(p.z, p.w) ? slope_sum_bytes(p.z, l.rows, l.wide) : forward_scratch(l, p.z);
         if (z > most) most = z;
     }
     const size_t dw = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
@@ -299,6 +320,10 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.out = workspace;
         g.ld_out = ldz = dz_row(l);
         z = workspace;
+        if (dbias && l.rows && sums_slopes(plan.z, plan.w)) {
+            g.sums_out = dbias->data;
+            dbias = nullptr;                     // that was it
+        }
         if (l.rows) e = product(g, plan.z, l.dtype, GEMM_KC_KC, rest, s);
     }
     if (dx && l.rows && e == hipSuccess) {

@@ -315,6 +315,15 @@ def test_large_and_small_values(t):
     check_grad(90, 64, 40, t, lo.SILU, True, spoil=faint)
 
 
+@pytest.mark.parametrize("shape", [(8200, 264, 1032), (16400, 2048, 4096)], ids=str)
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_faint_gradients_of_large_layers(t, shape):
+    """fp16 gradients that are subnormal numbers, in the products and in the sums beside them."""
+    def faint(d):
+        d["dy"] *= 2.0 ** -16 if t == "f16" else 2.0 ** -100
+    check_grad(*shape, t, lo.NONE, False, spoil=faint)
+
+
 def test_runs_give_the_same_bits():
     for shape in ((3000, 72, 64), (40, 520, 33), (9000, 256, 256)):
         for gated in (False, True):
