@@ -54,6 +54,9 @@ struct GemmArgs {
     float* partial;            // [splits][m][n]
     float* sums;               // RC_RC: [splits][m] sums of A over k, or null; SLOPE, GATED_SLOPE: [2 tiles_m][outputs] sums of the output over m, or null
     void* sums_out;            // RC_RC of one split: sums of A, [m] in the operands' type; and where launch_gemm_finish puts them
+    int sum_rows;              // of sums, for launch_gemm_finish (0: splits)
+    int64_t out_lo;            // SLOPE, GATED_SLOPE: 0, or elements from `out` to where goes what its rounding leaves off (tiles 0 and 1)
+    int64_t a_lo;              // KC_RC, RC_RC: 0, or elements from A to a second matrix that is added to it (tiles 0 and 1)
 };
 
 // Tiles: 0: 64 x 64, 1: 128 x 128, 2: 256 x 128, 3: 256 x 256 (2 and 3: operands on 16-byte pieces only).
@@ -93,7 +96,7 @@ struct ThinGradArgs {
 };
 // Its LDS: strides of the rows of the tiles (an odd number of 16-byte pieces), steps of 64 bytes in a row, where the tiles are; bytes = 0 if the case
 // is none for it.
-struct ThinGradShape { int dz_stride, x_stride, dy_stride, dz_steps, x_steps, wz, dz, x, dy, bias, bytes; };
+struct ThinGradShape { int dz_stride, x_stride, dy_stride, dz_steps, x_steps, wz, dz, lo, x, dy, bias, bytes; };
 __host__ __device__ inline ThinGradShape thin_grad_shape(int c, int o, int es, bool gated, bool z) {
     ThinGradShape s = {};
     const int e = 16 / es, wide = gated ? 2 * o : o;
@@ -106,7 +109,8 @@ __host__ __device__ inline ThinGradShape thin_grad_shape(int c, int o, int es, b
     const int c16 = (c + 15) / 16 * 16, w16 = (wide + 15) / 16 * 16;
     s.wz = c16 * s.dz_stride;
     s.dz = s.wz + (z ? (w16 + (gated ? 16 : 0)) * s.x_stride : 0);
-    s.x = s.dz + 64 * s.dz_stride;
+    s.lo = s.dz + 64 * s.dz_stride;
+    s.x = s.lo + (z && es == 2 ? 64 * s.dz_stride : 0);
     s.dy = s.x + 64 * s.x_stride;
     s.bias = s.dy + (gated ? 64 * s.dy_stride : 0);
     s.bytes = s.bias + (z ? (w16 + 16) * 4 : 0);
@@ -352,6 +356,21 @@ template <typename T> struct Raw8 {
     }
 };
 
+// 8 values of an output that comes in two parts, the second what the first's rounding left off
+template <typename T> __device__ __forceinline__ void gm_put_parts(T* p, int64_t lo, int count, const float v[8]) {
+    gm_put_some(p, count, v);
+    if (sizeof(T) == 2 && lo) {
+        float rest[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            T t;
+            gm_put(&t, v[i]);
+            rest[i] = v[i] - gm_get(&t);
+        }
+        gm_put_some(p + lo, count, rest);
+    }
+}
+
 // What a layer does to 8 U values of z, outputs in its place; e: of `extra`.  For the gated forms u is the same columns of the second half, and
 // becomes the second output.
 template <bool GATED, int U>
@@ -397,7 +416,7 @@ __device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int c
     }
     gm_finish<GATED, 1>(g, z, u, e);
     T* const out = (T*)g.out + row * g.ld_out + col;
-    gm_put_some(out, count, z[0]);
-    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[0]);
+    gm_put_parts(out, g.out_lo, count, z[0]);
+    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_parts(out + g.half, g.out_lo, count, u[0]);
 }
 }  // namespace srd

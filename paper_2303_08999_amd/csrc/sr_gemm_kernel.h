@@ -452,13 +452,20 @@ void k_gemm(const GemmArgs g) {
             }
         }
     };
-    if constexpr (ARC) {
-        if (sums) loop(std::true_type{});
-        else loop(std::false_type{});
-    } else {
-        loop(std::false_type{});
+    const char* const a0 = oa.base;
+    const char* const b0 = ob.base;
+    for (int part = 0;; ++part) {
+        if constexpr (ARC) {
+            if (sums) loop(std::true_type{});
+            else loop(std::false_type{});
+        } else {
+            loop(std::false_type{});
+        }
+        __syncthreads();
+        if (S::PIPE || sizeof(T) == 4 || LAYOUT == GEMM_KC_KC || part || !g.a_lo) break;
+        oa.base = a0 + g.a_lo * (int)sizeof(T);            // A's second part
+        ob.base = b0;
     }
-    __syncthreads();
 
     if constexpr (ARC) {
         if (sums) {
@@ -576,8 +583,9 @@ void k_gemm(const GemmArgs g) {
                         }
                     }
                     T* const out = (T*)g.out + (int64_t)m * g.ld_out + col;
-                    gm_put_some(out, count, z[r]);
-                    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_some(out + g.half, count, u[r]);
+                    const int64_t lo = S::PIPE ? 0 : g.out_lo;
+                    gm_put_parts(out, lo, count, z[r]);
+                    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_parts(out + g.half, lo, count, u[r]);
                 }
             }
         }

@@ -60,10 +60,10 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 constexpr int64_t THIN_FROM = 4096;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
 // caches, at 4.5 past them.
-Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated) {
+Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0};
-    if (layout != GEMM_RC_RC && m >= THIN_FROM) {
+    if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
         const ThinShape s = thin_shape(n, k, es, gated, gated);
         if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0};
     }
@@ -96,57 +96,47 @@ template <typename F> hipError_t by_type(int d, F f) {
     return d == SR_F32 ? f((float*)nullptr) : d == SR_F16 ? f((__half*)nullptr) : f((bf16raw*)nullptr);
 }
 
-// Whether the product that makes z sums dz over the rows too, and the scratch that takes (tiles of 128 rows where the operands are off 16-byte pieces): a
-// launch more, 4 us (gradient of 4096 rows of 64 to 128, gated, fp32: 22.8 us, so 27.6), which the large tiles' sums beside dW cost more than (8192 rows
-// of 2048 to 4096: 429 us, so 386).
-bool sums_slopes(const Cut& z, const Cut& w) { return z.tile >= 0 && z.splits == 1 && w.tile >= 2; }
+// Scratch for the sums of dz over the rows that the product which makes it leaves (two of them for each row of tiles, of 128 rows where the operands are
+// off 16-byte pieces)
 size_t slope_sum_bytes(const Cut& c, int64_t m, int64_t width) {
-    const int64_t rows = gemm_tile_rows(c.tile > 1 ? 1 : c.tile);
+    const int64_t rows = gemm_tile_rows(c.tile < 0 ? 0 : c.tile > 1 ? 1 : c.tile);
     return up256((size_t)(2 * ((m + rows - 1) / rows)) * width * 4);
 }
 
-// One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, where
-// sums_out is set, of the sums).
-hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hipStream_t st) {
+// One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, for RC_RC with sums_out but
+// no sums, of those).  A forward product of one split with g.sums says in *sum_rows how many rows of them it leaves.
+hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hipStream_t st, int* sum_rows = nullptr) {
     const size_t es = layer_esize(dtype);
     const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
     const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda * es % 16 == 0 && g.ldb * es % 16 == 0;
     g.splits = c.splits;
-    g.ksplit = c.ksplit;
+    g.ksplit = c.ksplit ? c.ksplit : g.k;
     return by_type(dtype, [&](auto t) -> hipError_t {
         using T = std::remove_pointer_t<decltype(t)>;
         if (c.tile == SKINNY && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
-        if (c.tile == THIN && g.ld_out == (g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n)) return launch_thin<T>(g, layout, st);
-        int tile = c.tile >= 0 ? c.tile : c.tile == THIN ? 1 : 0;
-        if (!aligned && tile > 1) tile = 1;
+        if (c.tile == THIN) return launch_thin<T>(g, layout, st);
+        int tile = c.tile < 0 ? 0 : c.tile;
+        if ((!aligned || g.a_lo || g.out_lo) && tile > 1) tile = 1;
         const int rows = gemm_tile_rows(tile), cols = gemm_tile_cols(tile);
+        const int64_t width = gated ? 2 * (int64_t)g.n : g.n;
         g.tiles_m = (g.m + rows - 1) / rows;
-        if (g.splits == 1) {
-            g.tiles_n = g.out ? (int)(((int64_t)(gated ? 2 : 1) * g.n + cols - 1) / cols) : 1;      // without: the sums of dz alone
-            if (g.ksplit == 0) g.ksplit = g.k;
-            const bool slopes = layout == GEMM_KC_KC && g.sums_out;      // db from the products' epilogue
-            if (slopes) g.sums = (float*)ws;
-            const hipError_t e = launch_gemm<T>(g, layout, aligned, tile, st);
-            if (e != hipSuccess || !slopes) return e;
-            GemmArgs f = {};
-            f.m = gated ? 2 * g.half : g.n;
-            f.n = 1;
-            f.splits = 2 * g.tiles_m;
-            f.sums = g.sums;
-            f.sums_out = g.sums_out;
-            return launch_gemm_finish<T>(f, st);
-        }
+        g.tiles_n = g.out ? (int)((width + cols - 1) / cols) : 1;      // without: the sums of dz alone
+        if (sum_rows) *sum_rows = 2 * g.tiles_m;
         GemmArgs p = g;
-        p.mode = GEMM_PARTIAL;
-        p.n = gated ? 2 * g.half : g.n;
-        p.tiles_n = g.out ? (p.n + cols - 1) / cols : 1;
-        p.partial = g.partial = g.out ? (float*)ws : nullptr;
-        if (g.sums_out) {
-            p.sums = g.sums = (float*)((char*)ws + partial_bytes(c, g.m, p.n));
-            p.sums_out = nullptr;
+        if (g.splits > 1) {
+            p.mode = GEMM_PARTIAL;
+            p.n = (int)width;
+            p.partial = g.partial = g.out ? (float*)ws : nullptr;
         }
-        const hipError_t e = launch_gemm<T>(p, layout, aligned, tile, st);
-        return e != hipSuccess ? e : launch_gemm_finish<T>(g, st);
+        if (layout == GEMM_RC_RC) {
+            if (g.sums) p.sums = nullptr, p.sums_out = nullptr;        // there already: only to be added up
+            else if (g.sums_out && g.splits > 1) p.sums = g.sums = (float*)((char*)ws + partial_bytes(c, g.m, width));
+        }
+        if (layout != GEMM_RC_RC || g.out || !g.sum_rows) {
+            const hipError_t e = launch_gemm<T>(p, layout, aligned, tile, st);
+            if (e != hipSuccess) return e;
+        }
+        return g.partial || (layout == GEMM_RC_RC && g.sums) ? launch_gemm_finish<T>(g, st) : hipSuccess;
     });
 }
 
@@ -162,28 +152,41 @@ Cut forward_cut(const Layer& l) { return cut_of(l.rows, l.out, l.in, layer_esize
 size_t forward_scratch(const Layer& l, const Cut& c) { return partial_bytes(c, l.rows, l.wide); }
 // dz, rows on 16-byte pieces
 int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (l.wide + e - 1) / e * e; }
-size_t dz_bytes(const Layer& l, int act) { return l.gated || act != SR_ACT_NONE ? up256((size_t)l.rows * dz_row(l) * layer_esize(l.dtype)) : 0; }
-// A gradient's three products: z, dx, dweight; and the scratch that dz takes and all of it
-// (pass: the workgroups of the one pass that makes them all, for a small layer whose tensors allow it, or 0).
-struct GradPlan { Cut z, x, w; int pass; size_t dz, need; };
+
+// 16-bit types: up to so many operations a product, dz goes on as two numbers, which hold it to 2^-17 or better: twice the matrix instructions in two products that
+// are launches' time.  Beyond, it is rounded once, which adds 2^-9 (fp16: 2^-12) of each value in random directions to sums over many: a gradient's error in norm
+// is 1.4 times that of its own rounding.  db is summed before that rounding.
+constexpr double TWO_PARTS_UP_TO = 2e9;
+
+// How a gradient is made.  pass: the workgroups of the one pass that makes all of it, for a small layer whose tensors allow it, or 0.  Else three products, z, dx and
+// dweight; parts: numbers that dz is stored as (0: dy is dz); slopes: db comes from sums that z's product leaves.  Scratch: dz, those sums, and what the products take.
+struct GradPlan { Cut z, x, w; int pass, parts; bool slopes; size_t dz, sums, need; };
 GradPlan grad_plan(const Layer& l, int act) {
     const size_t es = layer_esize(l.dtype);
+    const bool again = l.gated || act != SR_ACT_NONE;
     GradPlan p = {};
-    if (l.rows >= THIN_FROM && thin_grad_shape(l.in, l.out, (int)es, l.gated, l.gated || act != SR_ACT_NONE).bytes) {
+    if (l.rows >= THIN_FROM && thin_grad_shape(l.in, l.out, (int)es, l.gated, again).bytes) {
         const int64_t blocks = (l.rows + 63) / 64;
         p.pass = (int)(blocks < 2 * GPU_CUS ? blocks : 2 * GPU_CUS);
     }
-    p.dz = dz_bytes(l, act);
     p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false);
     p.w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
-    size_t most = partial_bytes(p.x, l.rows, l.in);
-    if (p.dz) {
-        p.z = forward_cut(l);
-        const size_t z = sums_slopes(p.z, p.w) ? slope_sum_bytes(p.z, l.rows, l.wide) : forward_scratch(l, p.z);
-        if (z > most) most = z;
+    size_t most = 0;
+    if (again) {
+        p.parts = es == 2 && 2.0 * (double)l.rows * l.in * l.wide <= TWO_PARTS_UP_TO ? 2 : 1;
+        if (p.parts == 2 && p.x.tile == THIN) p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, false);
+        p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false);
+        // fp32 loses nothing on the way; there it is only that the large tiles' sums beside dW cost their workgroups a sixth
+        p.slopes = p.parts == 1 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
+        p.dz = up256((size_t)p.parts * l.rows * dz_row(l) * es);
+        p.sums = p.slopes ? slope_sum_bytes(p.z, l.rows, l.wide) : 0;
+        most = partial_bytes(p.z, l.rows, l.wide);
     }
-    const size_t dw = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
-    p.need = p.dz + (dw > most ? dw : most);
+    const size_t x = partial_bytes(p.x, l.rows, l.in);
+    const size_t w = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
+    if (x > most) most = x;
+    if (w > most) most = w;
+    p.need = p.dz + p.sums + most;
     const size_t pass = up256((size_t)p.pass * l.wide * l.in * 4) + up256((size_t)p.pass * l.wide * 4);
     if (pass > p.need) p.need = pass;
     return p;
@@ -278,7 +281,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         if (t && (uintptr_t)t->data % es) return SR_ERR_ALIGN;
     }
     const GradPlan plan = grad_plan(l, act);
-    const size_t need = plan.need, dz = plan.dz;
+    const size_t need = plan.need;
     st = scratch_args(workspace, workspace_bytes, need);
     if (st != SR_OK) return st;
     const Span out[] = {span(dx), span(dweight), span(dbias), {need ? workspace : nullptr, need}};
@@ -309,27 +312,28 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         });
         return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
     }
-    void* const rest = (char*)workspace + dz;
+    float* const slopes = plan.slopes ? (float*)((char*)workspace + plan.dz) : nullptr;
+    void* const rest = (char*)workspace + plan.dz + plan.sums;
     const void* z = dy->data;
-    int64_t ldz = l.out;
+    int64_t ldz = l.out, lo = 0;
+    int slope_rows = 0;
     hipError_t e = hipSuccess;
-    if (dz) {
+    if (plan.parts) {
         GemmArgs g = forward_args(l, x, weight, bias, act);
         g.mode = gated ? GEMM_GATED_SLOPE : GEMM_SLOPE;
         g.extra = dy->data;
         g.out = workspace;
         g.ld_out = ldz = dz_row(l);
+        g.out_lo = lo = plan.parts == 2 ? l.rows * ldz : 0;
+        if (dbias) g.sums = slopes;
         z = workspace;
-        if (dbias && l.rows && sums_slopes(plan.z, plan.w)) {
-            g.sums_out = dbias->data;
-            dbias = nullptr;                     // that was it
-        }
-        if (l.rows) e = product(g, plan.z, l.dtype, GEMM_KC_KC, rest, s);
+        if (l.rows) e = product(g, plan.z, l.dtype, GEMM_KC_KC, rest, s, g.sums ? &slope_rows : nullptr);
     }
     if (dx && l.rows && e == hipSuccess) {
         GemmArgs g = {};
         g.a = z;
         g.lda = ldz;
+        g.a_lo = lo;
         g.b = weight->data;
         g.ldb = l.in;
         g.m = (int)l.rows;
@@ -344,6 +348,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         GemmArgs g = {};
         g.a = z;
         g.lda = ldz;
+        g.a_lo = lo;
         g.b = x->data;
         g.ldb = l.in;
         g.m = l.wide;
@@ -353,6 +358,7 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.out = dweight ? dweight->data : nullptr;
         g.ld_out = l.in;
         g.sums_out = dbias ? dbias->data : nullptr;
+        if (slope_rows) g.sums = slopes, g.sum_rows = slope_rows;
         e = product(g, plan.w, l.dtype, GEMM_RC_RC, rest, s);
     }
     return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;

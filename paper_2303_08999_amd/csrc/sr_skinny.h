@@ -95,12 +95,13 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
 }
 
 // 8 columns of a row for a group of SL threads, each every SL-th split, in double; what follows is as in the tile kernel.  Behind the rows of C
-// come the octets of `sums` (its splits' rows of g.m values), stored as they are.
+// come the octets of `sums` (rows of g.m values), stored as they are.
 struct FinishArgs {
     GemmArgs g;
     int width;                 // of a row of partial: n, or 2 half
     int octets;                // of a row of C
     int64_t all;               // octets of C
+    int sum_rows;
 };
 template <typename T, int SL>
 __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
     for (int i = 0; i < 8; ++i) zd[i] = ud[i] = 0.0;
     if (any) {
 #pragma unroll 8
-        for (int s = slice; s < g.splits; s += SL) {
+        for (int s = slice; s < (in_sums ? f.sum_rows : g.splits); s += SL) {
             float v[8];
             gm_get_some(p + s * step, count, v);
 #pragma unroll
@@ -186,9 +187,21 @@ hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st) {
     f.octets = (g.n + 7) / 8;
     f.all = (int64_t)(g.partial ? g.m : 0) * f.octets;
     const int64_t all = f.all + (g.sums ? (g.m + 7) / 8 : 0);
+    f.sum_rows = g.sum_rows ? g.sum_rows : g.splits;
+    // The rows of C share the launch with the sums, whose few threads may take as long as a launch for their rows; more of those have one of their own.
+    if (g.partial && g.sums && f.sum_rows > g.splits && f.sum_rows > 64) {
+        GemmArgs c = g;
+        c.sums = nullptr;
+        const hipError_t e = launch_gemm_finish<T>(c, st);
+        if (e != hipSuccess) return e;
+        c = g;
+        c.partial = nullptr;
+        return launch_gemm_finish<T>(c, st);
+    }
+    const int splits = g.partial ? g.splits : f.sum_rows;
     // so many slices that a thread's loads are all under way at once (512 splits of 72 x 64: 11.4 us in 16 slices)
-    if (g.splits <= 8) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
-    else if (g.splits <= 128) k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
+    if (splits <= 8) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
+    else if (splits <= 128) k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
     else k_gemm_finish<T, 64><<<(int)((all + 3) / 4), 256, 0, st>>>(f);
     return hipGetLastError();
 }

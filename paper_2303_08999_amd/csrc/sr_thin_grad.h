@@ -44,6 +44,9 @@ __global__ __launch_bounds__(256, 2) void k_thin_grad(const ThinGradArgs a) {
     char* const wt = lds;                                  // [c][wide]
     char* const wz = lds + s.wz;                           // [wide][c]
     char* const dz = lds + s.dz;                           // [row][wide]; dy first where there is no gate
+    // 16-bit types: what dz's rounding left off, for all three sums (2^-17 and better instead of 2^-9, fp16 2^-12)
+    constexpr bool LO = Z && sizeof(T) == 2;
+    char* const dl = lds + s.lo;
     char* const xs = lds + s.x;                            // [row][c]
     char* const dys = lds + (GATED ? s.dy : s.dz);         // [row][o]
     float* const bias = (float*)(lds + s.bias);
@@ -134,7 +137,11 @@ __global__ __launch_bounds__(256, 2) void k_thin_grad(const ThinGradArgs a) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         gm_put(p + i, z[0][i]);
-                        if constexpr (GATED) gm_put(p + a.o + i, u[0][i]);
+                        if constexpr (LO) gm_put((T*)(dl + ((char*)(p + i) - dz)), z[0][i] - gm_get(p + i));
+                        if constexpr (GATED) {
+                            gm_put(p + a.o + i, u[0][i]);
+                            if constexpr (LO) gm_put((T*)(dl + ((char*)(p + a.o + i) - dz)), u[0][i] - gm_get(p + a.o + i));
+                        }
                     }
                 }
             }
@@ -146,9 +153,15 @@ __global__ __launch_bounds__(256, 2) void k_thin_grad(const ThinGradArgs a) {
             for (int j = 0; j < NT; ++j) d[j] = f32x4g{0.0f, 0.0f, 0.0f, 0.0f};
             for (int k = 0; k < s.dz_steps; ++k) {
                 const u32x4g f = *(const u32x4g*)(dz + mine * s.dz_stride + (k * 4 + q) * 16);
+                u32x4g fl;
+                if constexpr (LO) fl = *(const u32x4g*)(dl + mine * s.dz_stride + (k * 4 + q) * 16);
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
-                    if (j * 16 < a.c) gm_mul<T, 16>(d[j], *(const u32x4g*)(wt + (j * 16 + r) * s.dz_stride + (k * 4 + q) * 16), f);
+                    if (j * 16 < a.c) {
+                        const u32x4g w = *(const u32x4g*)(wt + (j * 16 + r) * s.dz_stride + (k * 4 + q) * 16);
+                        gm_mul<T, 16>(d[j], w, f);
+                        if constexpr (LO) gm_mul<T, 16>(d[j], w, fl);
+                    }
             }
             const int64_t row = block * TG_ROWS + mine;
             if (row < a.rows) {
@@ -179,6 +192,13 @@ __global__ __launch_bounds__(256, 2) void k_thin_grad(const ThinGradArgs a) {
                             if (j * 16 < a.c) gm_mul<T, 16>(acc[i][j], fx[j], f);
                         constexpr unsigned one = sizeof(T) == 4 ? 0x3f800000u : __is_same(T, __half) ? 0x3c003c00u : 0x3f803f80u;
                         gm_mul<T, 16>(sum[i], u32x4g{one, one, one, one}, f);
+                        if constexpr (LO) {
+                            const u32x4g fl = turned_frag<T>(dl, s.dz_stride, k, m, lane);
+#pragma unroll
+                            for (int j = 0; j < NT; ++j)
+                                if (j * 16 < a.c) gm_mul<T, 16>(acc[i][j], fx[j], fl);
+                            gm_mul<T, 16>(sum[i], u32x4g{one, one, one, one}, fl);
+                        }
                     }
                 }
             }

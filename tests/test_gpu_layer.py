@@ -324,6 +324,24 @@ def test_faint_gradients_of_large_layers(t, shape):
     check_grad(*shape, t, lo.NONE, False, spoil=faint)
 
 
+@pytest.mark.parametrize("shape,parts", [((500, 64, 72), 2), ((33, 520, 40), 2), ((5000, 64, 72), 2), ((4100, 24, 16), 2), ((900, 1000, 1030), 2), ((3000, 1032, 776), 1),
+                                         ((9000, 256, 512), 1)], ids=str)
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_errors_of_gradients_in_norm(gated, t, shape, parts):
+    """In norm: the error of an exact result's rounding, and, where z's gradient goes through the type, as much again in random directions (1.41 in all; the
+    bias's gradient is summed before).  Where it goes in two parts, nothing is added.  A fifth of each is left for what a few hundred
+    values scatter."""
+    d = inputs(*shape, t, gated, 31)
+    e = wide64(d)
+    dz = (lo.gated_dz if gated else lo.linear_dz)(e["x"], e["w"], e["b"], lo.GELU, e["dy"])
+    if 2 * shape[0] * shape[1] * d["w"].shape[0] > 2e9:
+        parts = 1
+    for name, got, want in zip(("dx", "dweight", "dbias"), run_grad(d, t, lo.GELU, gated), lo.behind_dz(e["x"], e["w"], dz)):
+        rounding = (want.to(DT[t]).double() - want).norm()
+        assert (got.double() - want).norm() <= (1.2 if parts == 2 or name == "dbias" else 1.7) * rounding, name
+
+
 def test_runs_give_the_same_bits():
     for shape in ((3000, 72, 64), (40, 520, 33), (9000, 256, 256)):
         for gated in (False, True):
