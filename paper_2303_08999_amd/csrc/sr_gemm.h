@@ -66,7 +66,9 @@ inline int gemm_tile_cols(int tile) { return tile < 1 ? 64 : tile < 3 ? 128 : 25
 
 // z of the split sums, and what the epilogue would have done: elements [m][n], sums over the splits in double
 template <typename T> hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st);
-// Few rows: one pass over the weights (layout KC_KC; modes STORE and GATED)
+// Rows of `cols` elements at any address to rows of whole 16-byte pieces, zeros behind the last element
+template <typename T> hipError_t launch_pack(const void* from, int64_t rows, int cols, void* to, hipStream_t st);
+// Few rows: one pass over the weights (layout KC_KC, every mode but PARTIAL)
 template <typename T> hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st);
 constexpr int SKINNY_ROWS = 64;
 // Many rows, a small weight (layouts KC_KC and KC_RC, every mode but PARTIAL; the output's rows without gaps): what a launch is made of, waves = 0 if

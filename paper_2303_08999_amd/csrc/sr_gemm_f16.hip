@@ -6,6 +6,7 @@
 
 namespace srd {
 template hipError_t launch_gemm<__half>(const GemmArgs&, int, bool, int, hipStream_t);
+template hipError_t launch_pack<__half>(const void*, int64_t, int, void*, hipStream_t);
 template hipError_t launch_skinny<__half>(const GemmArgs&, bool, hipStream_t);
 template hipError_t launch_gemm_finish<__half>(const GemmArgs&, hipStream_t);
 }  // namespace srd

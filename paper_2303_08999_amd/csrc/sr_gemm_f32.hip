@@ -6,6 +6,7 @@
 
 namespace srd {
 template hipError_t launch_gemm<float>(const GemmArgs&, int, bool, int, hipStream_t);
+template hipError_t launch_pack<float>(const void*, int64_t, int, void*, hipStream_t);
 template hipError_t launch_skinny<float>(const GemmArgs&, bool, hipStream_t);
 template hipError_t launch_gemm_finish<float>(const GemmArgs&, hipStream_t);
 }  // namespace srd

@@ -38,9 +38,9 @@ bool any_overlap(const Span (&out)[NO], const Span (&in)[NI]) {
     return false;
 }
 
-// How one product is cut: tile (or the kernel for few rows, or for a small weight), splits of k.
+// How one product is cut: tile (or the kernel for few rows, or for a small weight), splits of k, and what the tiles should take.
 constexpr int SKINNY = -1, THIN = -2;
-struct Cut { int tile, splits, ksplit; };
+struct Cut { int tile, splits, ksplit; double us; };
 
 // Microseconds of c workgroups of a tile on each compute unit, each with `steps` of 128 bytes of k: what one alone takes a step, what each takes
 // where `share` of them keep a unit busy, and what a round of them takes beside that.  Measured with 1, 2, 4 and 8 workgroups a unit and k
@@ -62,13 +62,13 @@ constexpr int64_t THIN_FROM = 4096;
 // caches, at 4.5 past them.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
-    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0};
+    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0};
     if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
         const ThinShape s = thin_shape(n, k, es, gated, gated);
-        if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0};
+        if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0, 0.0};
     }
     const int64_t nn = gated ? 2 * n : n;
-    Cut best = {0, 1, 0};
+    Cut best = {0, 1, 0, 0.0};
     double least = 1e300;
     for (int tile = 0; tile < 4; ++tile) {
         const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
@@ -81,7 +81,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
             double us = tile_time(tile, (tiles * splits + GPU_CUS - 1) / GPU_CUS, each, es);
             const double mb = 8e-6 * (double)splits * (double)m * (double)nn;
             if (splits > 1) us += 3.0 + mb / (mb < 128.0 ? 8.0 : 4.5);
-            if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk)};
+            if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk), us};
         };
         for (int s = 1; s <= 8; ++s) look(s);
         for (int c = 1; c <= 8 && tiles; ++c) look(c * GPU_CUS / tiles);
@@ -99,7 +99,7 @@ template <typename F> hipError_t by_type(int d, F f) {
 // Scratch for the sums of dz over the rows that the product which makes it leaves (two of them for each row of tiles, of 128 rows where the operands are
 // off 16-byte pieces)
 size_t slope_sum_bytes(const Cut& c, int64_t m, int64_t width) {
-    const int64_t rows = gemm_tile_rows(c.tile < 0 ? 0 : c.tile > 1 ? 1 : c.tile);
+    const int64_t rows = gemm_tile_rows(c.tile > 1 ? 1 : c.tile);
     return up256((size_t)(2 * ((m + rows - 1) / rows)) * width * 4);
 }
 
@@ -113,9 +113,9 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
     g.ksplit = c.ksplit ? c.ksplit : g.k;
     return by_type(dtype, [&](auto t) -> hipError_t {
         using T = std::remove_pointer_t<decltype(t)>;
-        if (c.tile == SKINNY && (g.mode == GEMM_STORE || g.mode == GEMM_GATED)) return launch_skinny<T>(g, aligned, st);
+        if (c.tile == SKINNY) return launch_skinny<T>(g, aligned, st);
         if (c.tile == THIN) return launch_thin<T>(g, layout, st);
-        int tile = c.tile < 0 ? 0 : c.tile;
+        int tile = c.tile;
         if ((!aligned || g.a_lo || g.out_lo) && tile > 1) tile = 1;
         const int rows = gemm_tile_rows(tile), cols = gemm_tile_cols(tile);
         const int64_t width = gated ? 2 * (int64_t)g.n : g.n;
@@ -148,10 +148,28 @@ struct Layer {
     bool gated;
 };
 
-Cut forward_cut(const Layer& l) { return cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated); }
-size_t forward_scratch(const Layer& l, const Cut& c) { return partial_bytes(c, l.rows, l.wide); }
-// dz, rows on 16-byte pieces
-int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (l.wide + e - 1) / e * e; }
+// Rows on 16-byte pieces: dz, and copies of tensors that are not, for products by tiles that take longer than the copies: the tile kernels read other rows by way of
+// registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1106 us).
+int64_t whole_row(const Layer& l, int64_t cols) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (cols + e - 1) / e * e; }
+bool whole(const Layer& l, int64_t cols) { return whole_row(l, cols) == cols; }
+size_t copy_bytes(const Layer& l, int64_t rows, int64_t cols) { return up256((size_t)rows * whole_row(l, cols) * layer_esize(l.dtype)); }
+bool copies_pay(double us, size_t bytes, int copies) { return 1.2 * us > 4.0 * copies + 2.0 * (double)bytes / 4.5e6; }
+hipError_t copy_rows(const Layer& l, const void* from, int64_t rows, int cols, void* to, hipStream_t st) {
+    return by_type(l.dtype, [&](auto t) { return launch_pack<std::remove_pointer_t<decltype(t)>>(from, rows, cols, to, st); });
+}
+
+// A forward call: its product, and whether x and the weight are copied first; its scratch.
+struct ForwardPlan { Cut z; size_t x, w, need; };
+ForwardPlan forward_plan(const Layer& l) {
+    ForwardPlan p = {};
+    p.z = cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated);
+    if (p.z.tile >= 0 && !whole(l, l.in)) {
+        const size_t x = copy_bytes(l, l.rows, l.in), w = copy_bytes(l, l.wide, l.in);
+        if (copies_pay(p.z.us, x + w, 2)) p.x = x, p.w = w;
+    }
+    p.need = p.x + p.w + partial_bytes(p.z, l.rows, l.wide);
+    return p;
+}
 
 // 16-bit types: up to so many operations a product, dz goes on as two numbers, which hold it to 2^-17 or better: twice the matrix instructions in two products that
 // are launches' time.  Beyond, it is rounded once, which adds 2^-9 (fp16: 2^-12) of each value in random directions to sums over many: a gradient's error in norm
@@ -159,8 +177,9 @@ int64_t dz_row(const Layer& l) { const int64_t e = 16 / (int64_t)layer_esize(l.d
 constexpr double TWO_PARTS_UP_TO = 2e9;
 
 // How a gradient is made.  pass: the workgroups of the one pass that makes all of it, for a small layer whose tensors allow it, or 0.  Else three products, z, dx and
-// dweight; parts: numbers that dz is stored as (0: dy is dz); slopes: db comes from sums that z's product leaves.  Scratch: dz, those sums, and what the products take.
-struct GradPlan { Cut z, x, w; int pass, parts; bool slopes; size_t dz, sums, need; };
+// dweight; parts: numbers that dz is stored as (0: dy is dz); slopes: db comes from sums that z's product leaves.  Scratch: copies of x, the
+// weight and dy on 16-byte pieces where they pay, dz, those sums, and what the products take.
+struct GradPlan { Cut z, x, w; int pass, parts; bool slopes; size_t copy_x, copy_w, copy_dy, dz, sums, need; };
 GradPlan grad_plan(const Layer& l, int act) {
     const size_t es = layer_esize(l.dtype);
     const bool again = l.gated || act != SR_ACT_NONE;
@@ -177,16 +196,19 @@ GradPlan grad_plan(const Layer& l, int act) {
         if (p.parts == 2 && p.x.tile == THIN) p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, false);
         p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false);
         // fp32 loses nothing on the way; there it is only that the large tiles' sums beside dW cost their workgroups a sixth
-        p.slopes = p.parts == 1 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
-        p.dz = up256((size_t)p.parts * l.rows * dz_row(l) * es);
+        p.slopes = p.parts == 1 && p.z.tile >= 0 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
+        p.dz = up256((size_t)p.parts * l.rows * whole_row(l, l.wide) * es);
         p.sums = p.slopes ? slope_sum_bytes(p.z, l.rows, l.wide) : 0;
         most = partial_bytes(p.z, l.rows, l.wide);
     }
+    size_t copies[3] = {whole(l, l.in) ? 0 : copy_bytes(l, l.rows, l.in), whole(l, l.in) ? 0 : copy_bytes(l, l.wide, l.in),
+                        again || whole(l, l.out) ? 0 : copy_bytes(l, l.rows, l.out)};
+    if (l.rows && copies_pay(p.z.us + p.x.us + p.w.us, copies[0] + copies[1] + copies[2], 3)) p.copy_x = copies[0], p.copy_w = copies[1], p.copy_dy = copies[2];
     const size_t x = partial_bytes(p.x, l.rows, l.in);
     const size_t w = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
     if (x > most) most = x;
     if (w > most) most = w;
-    p.need = p.dz + p.sums + most;
+    p.need = p.copy_x + p.copy_w + p.copy_dy + p.dz + p.sums + most;
     const size_t pass = up256((size_t)p.pass * l.wide * l.in * 4) + up256((size_t)p.pass * l.wide * 4);
     if (pass > p.need) p.need = pass;
     return p;
@@ -251,8 +273,8 @@ int forward(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, 
     Layer l;
     int st = layer_args(l, x, weight, bias, act, y, residual, gated);
     if (st != SR_OK) return st;
-    const Cut cut = forward_cut(l);
-    const size_t need = forward_scratch(l, cut);
+    const ForwardPlan plan = forward_plan(l);
+    const size_t need = plan.need;
     st = scratch_args(workspace, workspace_bytes, need);
     if (st != SR_OK) return st;
     const Span out[] = {span(y), {need ? workspace : nullptr, need}}, in[] = {span(x), span(weight), span(bias), span(residual)};
@@ -262,7 +284,18 @@ int forward(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, 
     g.mode = gated ? GEMM_GATED : GEMM_STORE;
     g.extra = residual ? residual->data : nullptr;
     g.out = y->data;
-    return product(g, cut, l.dtype, GEMM_KC_KC, workspace, (hipStream_t)stream) == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e = hipSuccess;
+    if (plan.x) {
+        char* const copy = (char*)workspace;
+        e = copy_rows(l, x->data, l.rows, l.in, copy, s);
+        if (e == hipSuccess) e = copy_rows(l, weight->data, l.wide, l.in, copy + plan.x, s);
+        g.a = copy;
+        g.b = copy + plan.x;
+        g.lda = g.ldb = whole_row(l, l.in);
+    }
+    if (e == hipSuccess) e = product(g, plan.z, l.dtype, GEMM_KC_KC, (char*)workspace + plan.x + plan.w, s);
+    return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
 }
 
 int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias, int act, const sr_tensor* dy,
@@ -312,21 +345,41 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         });
         return e == hipSuccess ? SR_OK : SR_ERR_LAUNCH;
     }
-    float* const slopes = plan.slopes ? (float*)((char*)workspace + plan.dz) : nullptr;
-    void* const rest = (char*)workspace + plan.dz + plan.sums;
-    const void* z = dy->data;
-    int64_t ldz = l.out, lo = 0;
-    int slope_rows = 0;
+    char* at_ws = (char*)workspace;
+    auto take = [&](size_t bytes) { char* const p = at_ws; at_ws += bytes; return p; };
+    const void *xa = x->data, *wa = weight->data, *z = dy->data;
+    int64_t ldx = l.in, ldz = l.out, lo = 0;
     hipError_t e = hipSuccess;
-    if (plan.parts) {
+    if (plan.copy_x) {
+        char *const cx = take(plan.copy_x), *const cw = take(plan.copy_w);
+        e = copy_rows(l, xa, l.rows, l.in, cx, s);
+        if (e == hipSuccess) e = copy_rows(l, wa, l.wide, l.in, cw, s);
+        xa = cx;
+        wa = cw;
+        ldx = whole_row(l, l.in);
+    }
+    if (plan.copy_dy) {
+        char* const cd = take(plan.copy_dy);
+        if (e == hipSuccess) e = copy_rows(l, z, l.rows, l.out, cd, s);
+        z = cd;
+        ldz = whole_row(l, l.out);
+    }
+    char* const dz = take(plan.dz);
+    float* const slopes = plan.slopes ? (float*)take(plan.sums) : nullptr;
+    void* const rest = at_ws;
+    int slope_rows = 0;
+    if (plan.parts && e == hipSuccess) {
         GemmArgs g = forward_args(l, x, weight, bias, act);
+        g.a = xa;
+        g.b = wa;
+        g.lda = g.ldb = ldx;
         g.mode = gated ? GEMM_GATED_SLOPE : GEMM_SLOPE;
         g.extra = dy->data;
-        g.out = workspace;
-        g.ld_out = ldz = dz_row(l);
+        g.out = dz;
+        g.ld_out = ldz = whole_row(l, l.wide);
         g.out_lo = lo = plan.parts == 2 ? l.rows * ldz : 0;
         if (dbias) g.sums = slopes;
-        z = workspace;
+        z = dz;
         if (l.rows) e = product(g, plan.z, l.dtype, GEMM_KC_KC, rest, s, g.sums ? &slope_rows : nullptr);
     }
     if (dx && l.rows && e == hipSuccess) {
@@ -334,8 +387,8 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.a = z;
         g.lda = ldz;
         g.a_lo = lo;
-        g.b = weight->data;
-        g.ldb = l.in;
+        g.b = wa;
+        g.ldb = ldx;
         g.m = (int)l.rows;
         g.n = l.in;
         g.k = l.wide;
@@ -349,8 +402,8 @@ int gradient(const sr_tensor* x, const sr_tensor* weight, const sr_tensor* bias,
         g.a = z;
         g.lda = ldz;
         g.a_lo = lo;
-        g.b = x->data;
-        g.ldb = l.in;
+        g.b = xa;
+        g.ldb = ldx;
         g.m = l.wide;
         g.n = l.in;
         g.k = (int)l.rows;
@@ -372,7 +425,7 @@ using namespace srd;
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_linear_workspace_bytes(long long rows, int in, int out, int dtype) {
     Layer l;
-    return layer_sizes(l, rows, in, out, dtype, false) ? forward_scratch(l, forward_cut(l)) : 0;
+    return layer_sizes(l, rows, in, out, dtype, false) ? forward_plan(l).need : 0;
 }
 
 extern "C" __attribute__((visibility("default")))
@@ -397,7 +450,7 @@ int sr_layer_linear_grad(const sr_tensor* x, const sr_tensor* weight, const sr_t
 extern "C" __attribute__((visibility("default")))
 size_t sr_layer_gated_workspace_bytes(long long rows, int in, int out, int dtype) {
     Layer l;
-    return layer_sizes(l, rows, in, out, dtype, true) ? forward_scratch(l, forward_cut(l)) : 0;
+    return layer_sizes(l, rows, in, out, dtype, true) ? forward_plan(l).need : 0;
 }
 
 extern "C" __attribute__((visibility("default")))

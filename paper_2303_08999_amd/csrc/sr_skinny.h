@@ -91,7 +91,9 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
     }
     if (g.extra) extra.values(e[0]);
     gm_finish<GATED, 1>(g, z, u, e);
-    gm_put_some((T*)g.out + fm * g.ld_out + col, g.n - col, z[0]);
+    T* const out = (T*)g.out + fm * g.ld_out + col;
+    gm_put_parts(out, g.out_lo, g.n - col, z[0]);
+    if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_parts(out + g.half, g.out_lo, g.n - col, u[0]);
 }
 
 // 8 columns of a row for a group of SL threads, each every SL-th split, in double; what follows is as in the tile kernel.  Behind the rows of C
@@ -161,6 +163,18 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
     else gm_finish8<T, false>(g, row, col, z, u);
 }
 
+// A workgroup takes `per` rows of `pieces` each, a thread a piece at a time: bound by memory, read and written once.
+template <typename T>
+__global__ __launch_bounds__(256) void k_pack(const T* from, int64_t rows, int cols, u32x4g* to, int pieces, int per) {
+    constexpr int E = 16 / sizeof(T);
+    const int64_t row0 = (int64_t)blockIdx.x * per;
+    const int all = (int)(rows - row0 < per ? rows - row0 : per) * pieces;
+    for (int i = threadIdx.x; i < all; i += 256) {
+        const int row = i / pieces, p = i - row * pieces;
+        to[row0 * pieces + i] = gm_piece(from + (row0 + row) * cols + p * E, cols - p * E);
+    }
+}
+
 template <typename T, bool GATED, int RF>
 hipError_t start_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
     const int blocks = (g.n + 15) / 16;
@@ -172,8 +186,16 @@ hipError_t start_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
 }  // namespace
 
 template <typename T>
+hipError_t launch_pack(const void* from, int64_t rows, int cols, void* to, hipStream_t st) {
+    constexpr int E = 16 / sizeof(T);
+    const int pieces = (cols + E - 1) / E, per = pieces < 1024 ? 1024 / pieces : 1;
+    k_pack<T><<<(int)((rows + per - 1) / per), 256, 0, st>>>((const T*)from, rows, cols, (u32x4g*)to, pieces, per);
+    return hipGetLastError();
+}
+
+template <typename T>
 hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
-    if (g.mode == GEMM_GATED)
+    if (g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE)
         return g.m <= 16 ? start_skinny<T, true, 1>(g, aligned, st) : g.m <= 32 ? start_skinny<T, true, 2>(g, aligned, st) : start_skinny<T, true, 4>(g, aligned, st);
     return g.m <= 16 ? start_skinny<T, false, 1>(g, aligned, st) : g.m <= 32 ? start_skinny<T, false, 2>(g, aligned, st) : start_skinny<T, false, 4>(g, aligned, st);
 }
