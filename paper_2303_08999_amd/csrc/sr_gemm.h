@@ -358,17 +358,20 @@ template <typename T> struct Raw8 {
     }
 };
 
-// 8 values of an output that comes in two parts, the second what the first's rounding left off
+// What the rounding of v to T left off; of a value beyond T nothing, so that its infinity stays one.
+template <typename T> __device__ __forceinline__ float gm_rest(float v) {
+    T t;
+    gm_put(&t, v);
+    const float f = gm_get(&t);
+    return fabsf(f) == INFINITY ? 0.0f : v - f;
+}
+// 8 values of an output that comes in two parts
 template <typename T> __device__ __forceinline__ void gm_put_parts(T* p, int64_t lo, int count, const float v[8]) {
     gm_put_some(p, count, v);
     if (sizeof(T) == 2 && lo) {
         float rest[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            T t;
-            gm_put(&t, v[i]);
-            rest[i] = v[i] - gm_get(&t);
-        }
+        for (int i = 0; i < 8; ++i) rest[i] = gm_rest<T>(v[i]);
         gm_put_some(p + lo, count, rest);
     }
 }

@@ -58,6 +58,8 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 // From here on rows with a weight that fits go to the kernel for them; where that takes 16 at a time (500 000 of 128 to 128, bfloat16: 58 us, tiles 47), only
 // if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
+// A launch has less than 2^32 threads, 256 a tile: 2^31 rows of few columns need larger tiles than the smallest.
+constexpr int64_t LAUNCH_TILES = 1 << 24;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
 // caches, at 4.5 past them.
 Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true) {
@@ -72,6 +74,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     double least = 1e300;
     for (int tile = 0; tile < 4; ++tile) {
         const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
+        if (tiles >= LAUNCH_TILES && tile < 3) continue;
         auto look = [&](int64_t splits) {
             if (splits > steps / 2) splits = steps / 2;
             if (splits > 1024) splits = 1024;

@@ -104,6 +104,7 @@ struct FinishArgs {
     int octets;                // of a row of C
     int64_t all;               // octets of C
     int sum_rows;
+    int64_t sum_step;          // values from one row of sums to the next
 };
 template <typename T, int SL>
 __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
     const int count = (in_sums ? g.m : g.n) - col;
     const bool any = count > 0 && (!in_sums || g.sums);
     const float* const p = in_sums ? g.sums + col : g.partial + row * f.width + col;
-    const int64_t step = in_sums ? g.m : (int64_t)g.m * f.width;
+    const int64_t step = in_sums ? f.sum_step : (int64_t)g.m * f.width;
     double zd[8], ud[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) zd[i] = ud[i] = 0.0;
@@ -163,6 +164,21 @@ __global__ __launch_bounds__(256) void k_gemm_finish(const FinishArgs f) {
     else gm_finish8<T, false>(g, row, col, z, u);
 }
 
+// Sums of many rows: each workgroup adds up `chunk` of them, 64 columns of each, into the first of these, for k_gemm_finish to add those.  Its
+// threads for few columns would take the rows one behind another (gradient of 8294400 rows of 27 to 121, bfloat16: 3755 us, so 3205).
+__global__ __launch_bounds__(256) void k_fold(float* sums, int rows, int width, int chunk) {
+    __shared__ double sh[256];
+    const int col = blockIdx.x * 64 + (threadIdx.x & 63), first = blockIdx.y * chunk, end = rows - first < chunk ? rows : first + chunk;
+    double s = 0.0;
+    if (col < width) {
+#pragma unroll 8
+        for (int r = first + (threadIdx.x >> 6); r < end; r += 4) s += (double)sums[(int64_t)r * width + col];
+    }
+    sh[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 64 && col < width) sums[(int64_t)first * width + col] = (float)(sh[threadIdx.x] + sh[64 + threadIdx.x] + sh[128 + threadIdx.x] + sh[192 + threadIdx.x]);
+}
+
 // A workgroup takes `per` rows of `pieces` each, a thread a piece at a time: bound by memory, read and written once.
 template <typename T>
 __global__ __launch_bounds__(256) void k_pack(const T* from, int64_t rows, int cols, u32x4g* to, int pieces, int per) {
@@ -181,6 +197,15 @@ hipError_t start_skinny(const GemmArgs& g, bool aligned, hipStream_t st) {
     if (aligned) k_skinny<T, GATED, RF, true><<<blocks, SKW * 64, 0, st>>>(g);
     else k_skinny<T, GATED, RF, false><<<blocks, SKW * 64, 0, st>>>(g);
     return hipGetLastError();
+}
+
+constexpr int FOLD_FROM = 512;
+template <typename T>
+void start_finish(const FinishArgs& f, int64_t octets, int splits, hipStream_t st) {
+    // so many slices that a thread's loads are all under way at once (512 splits of 72 x 64: 11.4 us in 16 slices)
+    if (splits <= 8) k_gemm_finish<T, 1><<<(int)((octets + 255) / 256), 256, 0, st>>>(f);
+    else if (splits <= 128) k_gemm_finish<T, 16><<<(int)((octets + 15) / 16), 256, 0, st>>>(f);
+    else k_gemm_finish<T, 64><<<(int)((octets + 3) / 4), 256, 0, st>>>(f);
 }
 
 }  // namespace
@@ -208,23 +233,25 @@ hipError_t launch_gemm_finish(const GemmArgs& g, hipStream_t st) {
     f.width = gated ? 2 * g.half : g.n;
     f.octets = (g.n + 7) / 8;
     f.all = (int64_t)(g.partial ? g.m : 0) * f.octets;
-    const int64_t all = f.all + (g.sums ? (g.m + 7) / 8 : 0);
     f.sum_rows = g.sum_rows ? g.sum_rows : g.splits;
+    f.sum_step = g.m;
+    if (g.sums && g.sum_rows > FOLD_FROM) {
+        const int most = g.sum_rows > 16384 ? 256 : 64, chunk = (g.sum_rows + most - 1) / most;
+        f.sum_rows = (g.sum_rows + chunk - 1) / chunk;
+        f.sum_step = (int64_t)g.m * chunk;
+        k_fold<<<dim3((g.m + 63) / 64, f.sum_rows), 256, 0, st>>>(g.sums, g.sum_rows, g.m, chunk);
+    }
     // The rows of C share the launch with the sums, whose few threads may take as long as a launch for their rows; more of those have one of their own.
     if (g.partial && g.sums && f.sum_rows > g.splits && f.sum_rows > 64) {
-        GemmArgs c = g;
-        c.sums = nullptr;
-        const hipError_t e = launch_gemm_finish<T>(c, st);
-        if (e != hipSuccess) return e;
-        c = g;
-        c.partial = nullptr;
-        return launch_gemm_finish<T>(c, st);
+        FinishArgs c = f;
+        c.g.sums = nullptr;
+        start_finish<T>(c, f.all, g.splits, st);
+        f.all = 0;
+        f.g.partial = nullptr;
+        start_finish<T>(f, (g.m + 7) / 8, f.sum_rows, st);
+    } else {
+        start_finish<T>(f, f.all + (g.sums ? (g.m + 7) / 8 : 0), g.partial ? g.splits : f.sum_rows, st);
     }
-    const int splits = g.partial ? g.splits : f.sum_rows;
-    // so many slices that a thread's loads are all under way at once (512 splits of 72 x 64: 11.4 us in 16 slices)
-    if (splits <= 8) k_gemm_finish<T, 1><<<(int)((all + 255) / 256), 256, 0, st>>>(f);
-    else if (splits <= 128) k_gemm_finish<T, 16><<<(int)((all + 15) / 16), 256, 0, st>>>(f);
-    else k_gemm_finish<T, 64><<<(int)((all + 3) / 4), 256, 0, st>>>(f);
     return hipGetLastError();
 }
 

@@ -137,10 +137,10 @@ __global__ __launch_bounds__(256, 2) void k_thin_grad(const ThinGradArgs a) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         gm_put(p + i, z[0][i]);
-                        if constexpr (LO) gm_put((T*)(dl + ((char*)(p + i) - dz)), z[0][i] - gm_get(p + i));
+                        if constexpr (LO) gm_put((T*)(dl + ((char*)(p + i) - dz)), gm_rest<T>(z[0][i]));
                         if constexpr (GATED) {
                             gm_put(p + a.o + i, u[0][i]);
-                            if constexpr (LO) gm_put((T*)(dl + ((char*)(p + a.o + i) - dz)), u[0][i] - gm_get(p + a.o + i));
+                            if constexpr (LO) gm_put((T*)(dl + ((char*)(p + a.o + i) - dz)), gm_rest<T>(u[0][i]));
                         }
                     }
                 }

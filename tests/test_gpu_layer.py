@@ -417,6 +417,156 @@ def test_more_elements_than_32_bits_count(P, C, O):
     assert not dx[2:4095].any() and not dx[P - 129:P - 2].any() and int((dx != 0).any(1).sum()) == 7
 
 
+# features that are no 16-byte pieces, in products long enough for copies that are
+@pytest.mark.parametrize("shape,t", [((2500, 1021, 2053), "bf16"), ((3000, 1754, 1183), "f16"), ((1500, 777, 1030), "f32"), ((9000, 1032, 777), "bf16")], ids=str)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_copies_on_whole_pieces(gated, shape, t):
+    P, C, O = shape
+    if C % 8:
+        need = sr.sr_layer_gated_workspace_bytes if gated else sr.sr_layer_linear_workspace_bytes
+        assert need(P, C, O, DT[t]) >= P * C * DT[t].itemsize
+    for kind, shift in ((lo.NONE, 0), (lo.SILU, 1)):
+        check_forward(*shape, t, kind, gated, residual=not gated, shift=shift)
+        check_grad(*shape, t, kind, gated, shift=shift)
+
+
+@pytest.mark.parametrize("shape,t", [((66000, 136, 200), "bf16"), ((140000, 27, 121), "f16"), ((1200001, 17, 9), "bf16"), ((90000, 520, 264), "f32")], ids=str)
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_bias_gradients_of_very_many_rows(gated, shape, t):
+    """The sums that every row of tiles leaves are so many that they are added up in two steps."""
+    check_grad(*shape, t, lo.GELU, gated)
+
+
+# one of each way that a call is made: few rows, tiles, split sums, small weights, one pass, dz in two parts or one, copies
+WAYS = [(7, 2048, 33), (64, 129, 31), (300, 64, 72), (1000, 1000, 264), (5000, 64, 72), (5000, 31, 33), (2500, 1021, 1030), (90, 4100, 65), (9000, 256, 512), (70000, 136, 40)]
+
+
+@pytest.mark.parametrize("shape", WAYS, ids=lambda s: "P%dC%dO%d" % s)
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_a_workspace_of_the_size_asked_for_and_no_more(gated, t, shape):
+    """What is in it before does not matter, and what is around it stays."""
+    P, C, O = shape
+    d = inputs(*shape, t, gated, 12)
+    y, grads = run_forward(d, t, lo.SILU, gated), run_grad(d, t, lo.SILU, gated)
+    out = [torch.empty_like(v) for v in (y, *grads)]
+    if gated:
+        sizes = sr.sr_layer_gated_workspace_bytes(P, C, O, DT[t]), sr.sr_layer_gated_grad_workspace_bytes(P, C, O, DT[t])
+    else:
+        sizes = sr.sr_layer_linear_workspace_bytes(P, C, O, DT[t]), sr.sr_layer_linear_grad_workspace_bytes(P, C, O, DT[t], lo.SILU)
+    room = [torch.full((n + 8192,), 255, device=DEV, dtype=torch.uint8) for n in sizes]
+    ws = [r[4096:4096 + n] if n else None for r, n in zip(room, sizes)]
+    if gated:
+        sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.SILU, out[0], workspace=ws[0])
+        sr.sr_layer_gated_grad(d["x"], d["w"], d["b"], lo.SILU, d["dy"], *out[1:], workspace=ws[1])
+    else:
+        sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.SILU, None, out[0], workspace=ws[0])
+        sr.sr_layer_linear_grad(d["x"], d["w"], d["b"], lo.SILU, d["dy"], *out[1:], workspace=ws[1])
+    torch.cuda.synchronize()
+    for a, b in zip(out, (y, *grads)):
+        assert torch.equal(a, b)
+    for r, n in zip(room, sizes):
+        assert (r[:4096] == 255).all() and (r[4096 + n:] == 255).all()
+
+
+@pytest.mark.parametrize("shape", WAYS, ids=lambda s: "P%dC%dO%d" % s)
+def test_every_way_at_once_on_two_streams_and_replayed(shape):
+    """Two streams with a workspace each, at the same time; the same calls from a graph, with eager ones between its replays."""
+    P, C, O = shape
+    sets = [inputs(*shape, "bf16", gated, 40 + gated) for gated in (False, True)]
+    want = [[run_forward(d, "bf16", lo.GELU, gated), *run_grad(d, "bf16", lo.GELU, gated)] for gated, d in enumerate(sets)]
+    outs = [[torch.empty_like(v) for v in w] for w in want]
+    streams = [torch.cuda.Stream() for _ in sets]
+    grad_bytes = (sr.sr_layer_linear_grad_workspace_bytes(P, C, O, torch.bfloat16, lo.GELU), sr.sr_layer_gated_grad_workspace_bytes(P, C, O, torch.bfloat16))
+    forward_bytes = (sr.sr_layer_linear_workspace_bytes(P, C, O, torch.bfloat16), sr.sr_layer_gated_workspace_bytes(P, C, O, torch.bfloat16))
+    ws = [torch.empty(max(a, b, 16), device=DEV, dtype=torch.uint8) for a, b in zip(grad_bytes, forward_bytes)]
+
+    def both(streams):
+        for gated, d in enumerate(sets):
+            o = outs[gated]
+            if gated:
+                sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.GELU, o[0], workspace=ws[1], stream=streams[1])
+                sr.sr_layer_gated_grad(d["x"], d["w"], d["b"], lo.GELU, d["dy"], *o[1:], workspace=ws[1], stream=streams[1])
+            else:
+                sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.GELU, None, o[0], workspace=ws[0], stream=streams[0])
+                sr.sr_layer_linear_grad(d["x"], d["w"], d["b"], lo.GELU, d["dy"], *o[1:], workspace=ws[0], stream=streams[0])
+
+    def same(what):
+        torch.cuda.synchronize()
+        for w, o in zip(want, outs):
+            for name, a, b in zip(("y", "dx", "dweight", "dbias"), w, o):
+                assert torch.equal(a, b), (what, name)
+                b.zero_()
+        torch.cuda.synchronize()
+
+    torch.cuda.synchronize()
+    for i in range(3):
+        both(streams)
+    same("two streams")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both((None, None))
+    for i in range(3):
+        for w in ws:
+            w.fill_(255)
+        graph.replay()
+        same(f"replay {i}")
+        both(streams)
+        same("between replays")
+
+
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("P", [7, 300, 5000, 40000])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_gradients_beyond_the_type_are_infinite(gated, P, t):
+    """z's gradient may leave the type between two products: an infinity then, whose row and column it stays in, and no NaN where its
+    product with a weight or a feature is none."""
+    C, O, row, n = 64, 72, P - 2, 5
+    d = inputs(P, C, O, t, gated, 17)
+    d["b"].zero_()
+    d["w"][:, 0] = 0
+    d["w"][n::O, 0] = 1
+    d["x"][row] = 2.0 ** -9
+    d["x"][row, 0] = 1.5
+    big = torch.finfo(DT[t]).max
+    d["dy"][row, n] = big                                        # times gelu'(1.5) = 1.128, and for the gate another 1.5
+    dx, dw, db = run_grad(d, t, lo.GELU, gated)
+    other = torch.arange(P, device=DEV) != row
+    assert dx[other].isfinite().all()
+    if gated:                                                    # du = dy gelu(1.5) is infinite as well: where the signs of the two weights differ, NaN
+        a, b = d["w"][n].float(), d["w"][O + n].float()
+        sure = a * b > 0
+        assert (dx[row][sure].float() == ((a + b) * math.inf)[sure]).all()
+    else:
+        a = d["w"][n].float()
+        assert (dx[row][a != 0].float() == (a * math.inf)[a != 0]).all()
+    rows = torch.zeros(dw.shape[0], dtype=torch.bool, device=DEV)
+    rows[n::O] = True
+    assert dw[~rows].isfinite().all() and (dw[rows].float() == math.inf).all()
+    assert db[~rows].isfinite().all() and (db[rows].float() == math.inf).all()
+
+
+def test_more_rows_than_a_launch_of_small_tiles_has():
+    P = (1 << 30) + 77
+    at = torch.tensor([0, 1, 4095, P // 2, P - 130, P - 2, P - 1], device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.zeros((P, 1), device=DEV, dtype=torch.bfloat16)
+    x[at] = torch.randn((7, 1), generator=g, device=DEV).bfloat16()
+    w, b = torch.full((1, 1), 0.75, device=DEV).bfloat16(), torch.full((1,), 0.5, device=DEV).bfloat16()
+    dy = torch.zeros((P, 1), device=DEV, dtype=torch.bfloat16)
+    dy[at] = torch.randn((7, 1), generator=g, device=DEV).bfloat16()
+    e = wide64({"x": x[at], "w": w, "b": b, "dy": dy[at], "res": None})
+    y = torch.empty_like(x)
+    sr.sr_layer_linear(x, w, b, lo.SILU, None, y)
+    want, bound = forward_bound("bf16", e, lo.SILU, False)
+    compare("y", y[at], want, bound)
+    dx, dw, db = torch.full_like(x, 3.0), torch.empty_like(w), torch.empty_like(b)
+    sr.sr_layer_linear_grad(x, w, b, lo.SILU, dy, dx, dw, db)
+    for name, got, (want, bound) in zip(("dx", "dweight", "dbias"), (dx[at], dw, db), behind_bound("bf16", e, *dz_bound("bf16", e, lo.SILU, False))):
+        compare(name, got, want, bound)
+    assert int((dx != 0).sum()) == 7
+
+
 def test_the_bounds_tell_mistakes_apart():
     """Each of these mistakes, made in the oracle, leaves the bound that the kernels keep."""
     d = inputs(300, 72, 88, "bf16", False, 21, residual=True)
