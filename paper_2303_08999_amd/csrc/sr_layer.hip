@@ -38,9 +38,17 @@ bool any_overlap(const Span (&out)[NO], const Span (&in)[NI]) {
     return false;
 }
 
+int64_t rows_of(const sr_tensor* t) { return (int64_t)t->n * t->h * t->w; }
+
+struct Layer {
+    int64_t rows;
+    int in, out, wide, dtype;
+    bool gated;
+};
+
 // How one product is cut: tile (or the kernel for few rows, or for a small weight), splits of k, and what the tiles should take.
 constexpr int SKINNY = -1, THIN = -2;
-struct Cut { int tile, splits, ksplit; double us; };
+struct Cut { int tile, splits, ksplit; double us; bool rows; };       // rows: by launch_rows where A is on 16-byte pieces
 
 // Microseconds of c workgroups of a tile on each compute unit, each with `steps` of 128 bytes of k: what one alone takes a step, what each takes
 // where `share` of them keep a unit busy, and what a round of them takes beside that.  Measured with 1, 2, 4 and 8 workgroups a unit and k
@@ -58,19 +66,24 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 // From here on rows with a weight that fits go to the kernel for them; where that takes 16 at a time (500 000 of 128 to 128, bfloat16: 58 us, tiles 47), only
 // if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
+// From so many outputs on (of a launch; more where there is more to read, or several) the kernel that holds the weight is worth its start (bfloat16, 65536 rows
+// of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  It reads the
+// rows once for each launch; beside dz's sums it holds half as many columns (131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427).
+constexpr double ROWS_FROM = 26e6;
+constexpr int ROWS_LAUNCHES = 4;
 // A launch has less than 2^32 threads, 256 a tile: 2^31 rows of few columns need larger tiles than the smallest.
 constexpr int64_t LAUNCH_TILES = 1 << 24;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
 // caches, at 4.5 past them.
-Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true) {
+Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true, bool rows = true, bool slope = false) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
-    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0};
+    if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0, false};
     if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
         const ThinShape s = thin_shape(n, k, es, gated, gated);
-        if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0, 0.0};
+        if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0, 0.0, false};
     }
     const int64_t nn = gated ? 2 * n : n;
-    Cut best = {0, 1, 0, 0.0};
+    Cut best = {0, 1, 0, 0.0, false};
     double least = 1e300;
     for (int tile = 0; tile < 4; ++tile) {
         const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
@@ -84,10 +97,15 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
             double us = tile_time(tile, (tiles * splits + GPU_CUS - 1) / GPU_CUS, each, es);
             const double mb = 8e-6 * (double)splits * (double)m * (double)nn;
             if (splits > 1) us += 3.0 + mb / (mb < 128.0 ? 8.0 : 4.5);
-            if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk), us};
+            if (us < least) least = us, best = Cut{tile, (int)splits, (int)(each * bk), us, false};
         };
         for (int s = 1; s <= 8; ++s) look(s);
         for (int c = 1; c <= 8 && tiles; ++c) look(c * GPU_CUS / tiles);
+    }
+    if (rows && layout != GEMM_RC_RC && best.splits == 1) {
+        const RowsShape s = rows_shape(m, n, k, es, gated, slope);
+        const double cols = gated ? 2.0 * s.cols : s.cols;
+        best.rows = s.grid && s.launches <= (slope ? 2 : ROWS_LAUNCHES) && (double)m * cols >= ROWS_FROM * (k > cols ? (double)k / cols : 1.0) * (s.launches > 1 ? 2.0 : 1.0);
     }
     return best;
 }
@@ -99,11 +117,16 @@ template <typename F> hipError_t by_type(int d, F f) {
     return d == SR_F32 ? f((float*)nullptr) : d == SR_F16 ? f((__half*)nullptr) : f((bf16raw*)nullptr);
 }
 
-// Scratch for the sums of dz over the rows that the product which makes it leaves (two of them for each row of tiles, of 128 rows where the operands are
-// off 16-byte pieces)
-size_t slope_sum_bytes(const Cut& c, int64_t m, int64_t width) {
+// Scratch for the sums of dz over the rows that the product which makes it leaves: two of them for each row of tiles, of 128 rows where the operands are
+// off 16-byte pieces; one for each group of rows of a workgroup that holds the weight
+size_t slope_sum_bytes(const Cut& c, const Layer& l) {
     const int64_t rows = gemm_tile_rows(c.tile > 1 ? 1 : c.tile);
-    return up256((size_t)(2 * ((m + rows - 1) / rows)) * width * 4);
+    int64_t all = 2 * ((l.rows + rows - 1) / rows);
+    if (c.rows) {
+        const RowsShape s = rows_shape(l.rows, l.out, l.in, layer_esize(l.dtype), l.gated, true);
+        if (all < (int64_t)s.grid * s.wr) all = (int64_t)s.grid * s.wr;
+    }
+    return up256((size_t)all * l.wide * 4);
 }
 
 // One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, for RC_RC with sums_out but
@@ -118,6 +141,13 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         using T = std::remove_pointer_t<decltype(t)>;
         if (c.tile == SKINNY) return launch_skinny<T>(g, aligned, st);
         if (c.tile == THIN) return launch_thin<T>(g, layout, st);
+        if constexpr (sizeof(T) == 2) {
+            if (c.rows && (uintptr_t)g.a % 16 == 0 && g.lda * es % 16 == 0) {
+                const RowsShape r = rows_shape(g.m, g.n, g.k, es, gated, g.mode == GEMM_SLOPE || g.mode == GEMM_GATED_SLOPE);
+                if (sum_rows) *sum_rows = r.grid * r.wr;
+                return launch_rows<T>(g, layout, st);
+            }
+        }
         int tile = c.tile;
         if ((!aligned || g.a_lo || g.out_lo) && tile > 1) tile = 1;
         const int rows = gemm_tile_rows(tile), cols = gemm_tile_cols(tile);
@@ -142,14 +172,6 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         return g.partial || (layout == GEMM_RC_RC && g.sums) ? launch_gemm_finish<T>(g, st) : hipSuccess;
     });
 }
-
-int64_t rows_of(const sr_tensor* t) { return (int64_t)t->n * t->h * t->w; }
-
-struct Layer {
-    int64_t rows;
-    int in, out, wide, dtype;
-    bool gated;
-};
 
 // Rows on 16-byte pieces: dz, and copies of tensors that are not, for products by tiles that take longer than the copies: the tile kernels read other rows by way of
 // registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1106 us).
@@ -196,12 +218,12 @@ GradPlan grad_plan(const Layer& l, int act) {
     size_t most = 0;
     if (again) {
         p.parts = es == 2 && 2.0 * (double)l.rows * l.in * l.wide <= TWO_PARTS_UP_TO ? 2 : 1;
-        if (p.parts == 2 && p.x.tile == THIN) p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, false);
-        p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false);
+        if (p.parts == 2) p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, false, false);
+        p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false, p.parts == 1, true);
         // fp32 loses nothing on the way; there it is only that the large tiles' sums beside dW cost their workgroups a sixth
         p.slopes = p.parts == 1 && p.z.tile >= 0 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
         p.dz = up256((size_t)p.parts * l.rows * whole_row(l, l.wide) * es);
-        p.sums = p.slopes ? slope_sum_bytes(p.z, l.rows, l.wide) : 0;
+        p.sums = p.slopes ? slope_sum_bytes(p.z, l) : 0;
         most = partial_bytes(p.z, l.rows, l.wide);
     }
     size_t copies[3] = {whole(l, l.in) ? 0 : copy_bytes(l, l.rows, l.in), whole(l, l.in) ? 0 : copy_bytes(l, l.wide, l.in),

@@ -437,8 +437,43 @@ def test_bias_gradients_of_very_many_rows(gated, shape, t):
     check_grad(*shape, t, lo.GELU, gated)
 
 
+# so many outputs that the kernel which holds the weight takes them: k that ends inside a step, widths that are no pieces, several launches
+HELD = [(65600, 64, 410), (131100, 40, 200), (131075, 136, 201), (70001, 250, 400), (262200, 264, 120), (140000, 8, 264), (110000, 72, 1030), (300000, 512, 100), (56000, 512, 500), (70000, 130, 391),
+        (211111, 100, 255), (430001, 120, 62), (900000, 24, 40)]
+
+
+@pytest.mark.parametrize("shape", HELD, ids=lambda s: "P%dC%dO%d" % s)
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_very_many_rows(gated, shape, t):
+    kind = shape[0] % 4 + 1
+    check_forward(*shape, t, kind, gated)
+    check_forward(*shape, t, lo.NONE, gated, bias=False, residual=not gated, shift=shape[0] % 2 * 8)
+    check_grad(*shape, t, kind, gated, shift=shape[0] % 2 * 3)
+    check_grad(*shape, t, lo.NONE, gated)
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+@pytest.mark.parametrize("C", [40, 72, 132, 264])
+def test_rows_of_nan_among_very_many(gated, C):
+    P, O = 131080, 256 if gated else 264
+    d = inputs(P, C, O, "bf16", gated, 5)
+    clean = run_forward(d, "bf16", lo.SILU, gated).clone()
+    at = torch.tensor([0, 63, 777, 65536, P - 2], device=DEV)
+    d["x"][at] = float("nan")
+    y = run_forward(d, "bf16", lo.SILU, gated)
+    rows = torch.ones(P, dtype=torch.bool, device=DEV)
+    rows[at] = False
+    assert torch.equal(y[rows], clean[rows]) and y[~rows].isnan().all()
+    d["x"].zero_()
+    clean = run_grad(d, "bf16", lo.NONE, gated, want=(True, False, False))[0].clone()
+    d["dy"][at] = float("nan")
+    dx = run_grad(d, "bf16", lo.NONE, gated, want=(True, False, False))[0]
+    assert torch.equal(dx[rows], clean[rows]) and dx[~rows].isnan().all()
+
+
 # one of each way that a call is made: few rows, tiles, split sums, small weights, one pass, dz in two parts or one, copies
-WAYS = [(7, 2048, 33), (64, 129, 31), (300, 64, 72), (1000, 1000, 264), (5000, 64, 72), (5000, 31, 33), (2500, 1021, 1030), (90, 4100, 65), (9000, 256, 512), (70000, 136, 40)]
+WAYS = [(7, 2048, 33), (64, 129, 31), (300, 64, 72), (1000, 1000, 264), (5000, 64, 72), (5000, 31, 33), (2500, 1021, 1030), (90, 4100, 65), (9000, 256, 512), (70000, 136, 40), (66000, 72, 520)]
 
 
 @pytest.mark.parametrize("shape", WAYS, ids=lambda s: "P%dC%dO%d" % s)
