@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsrdict.so")
 SOURCES = ["sr_api.hip", "sr_generic.hip", "sr_list.hip", "sr_mfma.hip", "sr_mfma_k3.hip", "sr_mfma_k5.hip", "sr_mfma_k5_big.hip", "sr_mfma_k5_ps.hip", "sr_mfma_k5_pm.hip", "sr_mfma_k5_lg.hip", "sr_mfma_k5_blk.hip", "sr_mfma_list.hip", "sr_mfma_k5_f32.hip", "sr_mfma_k5_f8.hip", "sr_mfma_k7.hip", "sr_mfma_k7_f8.hip", "sr_mfma_bf16.hip", "sr_slots.hip", "sr_slots_k3c1.hip", "sr_slots_k3c3.hip", "sr_slots_k5c1.hip", "sr_slots_k5c3.hip", "sr_slots_k7c1.hip", "sr_slots_k7c3.hip", "sr_probe.hip", "sr_select.hip", "sr_route.hip", "sr_route_f32.hip", "sr_route_f16.hip", "sr_route_bf16.hip", "sr_list_grad.hip", "sr_list_grad_f16.hip", "sr_list_grad_f32.hip",
-           "sr_layer.hip", "sr_gemm_f32.hip", "sr_gemm_f16.hip", "sr_gemm_bf16.hip", "sr_thin_f32.hip", "sr_thin_f16.hip", "sr_thin_bf16.hip", "sr_rows_f16.hip", "sr_rows_bf16.hip", "sr_grad_clip.hip"]
+           "sr_layer.hip", "sr_gemm_f32.hip", "sr_gemm_f16.hip", "sr_gemm_bf16.hip", "sr_thin_f32.hip", "sr_thin_f16.hip", "sr_thin_bf16.hip", "sr_rows_f32.hip", "sr_rows_f16.hip", "sr_rows_bf16.hip", "sr_grad_clip.hip"]
 HEADERS = ["sr_device.h", "sr_launch.h", "sr_mfma_kernel.h", "sr_slots.h", "sr_route.h", "sr_route_lanes.h", "sr_list_grad.h", "sr_list_grad_mfma.h", "sr_gemm.h", "sr_gemm_kernel.h", "sr_skinny.h", "sr_thin.h", "sr_thin_grad.h", "sr_rows.h", os.path.join("..", "..", "include", "sr_dict.h"),
            os.path.join("..", "..", "include", "sr_probe.h"),
            os.path.join("..", "..", "include", "sr_select.h"),

@@ -93,15 +93,22 @@ template <typename T> hipError_t launch_thin(const GemmArgs& g, int layout, hipS
 // wr of rows, are the wavefronts; steps: of 32 k that the kernel has registers for; subs: of 32 wr rows, in a block of rows.
 constexpr int ROWS_STAGE = 65536;                    // bytes of a block of rows
 struct RowsShape { int grid, launches, cols, wn, wr, tiles, steps, subs; };
-inline RowsShape rows_shape(int64_t m, int64_t n, int64_t k, size_t es, bool gated, bool slope) {
-    if (es != 2 || n < 1 || k < 1) return {};
+inline RowsShape rows_shape(int64_t m, int64_t n, int64_t k, size_t es, bool gated, bool extra) {
+    if (n < 1 || k < 1) return {};
     RowsShape s = {};
     const int64_t steps = (k + 31) / 32;
-    // tiles x steps x halves: 32 fill half of the registers; beside the sums of dz and what it is multiplied with there is room for half of that
-    if (!gated && steps <= (slope ? 4 : 8)) s.tiles = 4;
-    else if (steps <= (gated ? slope ? 4 : 8 : slope ? 8 : 16)) s.tiles = 2;
-    else return {};
-    s.steps = steps <= 4 ? 4 : steps <= 8 ? 8 : 16;
+    // tiles x steps x halves: 32 (fp32: 8, of three parts) fill half of the registers; beside what is added or multiplied there is room for half of that
+    if (es == 4) {
+        if (!gated && !extra && steps <= 2) s.tiles = 4;
+        else if (steps <= (gated ? 2 : 4)) s.tiles = 2;
+        else return {};
+        s.steps = steps <= 2 ? 2 : 4;
+    } else {
+        if (!gated && steps <= (extra ? 4 : 8)) s.tiles = 4;
+        else if (steps <= (gated ? extra ? 4 : 8 : extra ? 8 : 16)) s.tiles = 2;
+        else return {};
+        s.steps = steps <= 4 ? 4 : steps <= 8 ? 8 : 16;
+    }
     const int64_t most_cols = s.tiles * 128, group = s.tiles * 16;
     s.launches = (int)((n + most_cols - 1) / most_cols);
     s.cols = (int)(((n + s.launches - 1) / s.launches + group - 1) / group * group);
@@ -110,7 +117,7 @@ inline RowsShape rows_shape(int64_t m, int64_t n, int64_t k, size_t es, bool gat
     s.wr = s.wn <= 1 ? 8 : s.wn <= 2 ? 4 : s.wn <= 4 ? 2 : 1;
     const int64_t sub = 32 * s.wr;
     // as few rows a workgroup as there can be, in blocks as large as there can be, but four of them
-    int64_t least = 0, most = ROWS_STAGE / (sub * steps * 64);
+    int64_t least = 0, most = ROWS_STAGE / (sub * steps * 32 * (int64_t)es);
     if (most > 1 && most > m / (4 * 256 * sub)) most = m / (4 * 256 * sub) > 1 ? m / (4 * 256 * sub) : 1;
     for (int64_t c = most; c >= 1; --c) {
         const int64_t blocks = (m + sub * c - 1) / (sub * c), each = (blocks + 255) / 256 * c;

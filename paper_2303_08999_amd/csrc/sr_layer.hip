@@ -48,7 +48,7 @@ struct Layer {
 
 // How one product is cut: tile (or the kernel for few rows, or for a small weight), splits of k, and what the tiles should take.
 constexpr int SKINNY = -1, THIN = -2;
-struct Cut { int tile, splits, ksplit; double us; bool rows; };       // rows: by launch_rows where A is on 16-byte pieces
+struct Cut { int tile, splits, ksplit; double us; bool rows; };       // rows: by launch_rows where A's rows are at multiples of four bytes
 
 // Microseconds of c workgroups of a tile on each compute unit, each with `steps` of 128 bytes of k: what one alone takes a step, what each takes
 // where `share` of them keep a unit busy, and what a round of them takes beside that.  Measured with 1, 2, 4 and 8 workgroups a unit and k
@@ -67,10 +67,10 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 // if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
 // From so many outputs on (of a launch; more where there is more to read, or several) the kernel that holds the weight is worth its start (bfloat16, 65536 rows
-// of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  It reads the
-// rows once for each launch; beside dz's sums it holds half as many columns (131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427).
+// of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  Each launch reads the
+// rows again (bfloat16, 131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427; fp32, 351576 rows of 64 to 1024 in two: 564 and 505).
+// fp32 of more than 64 features splits more values than it multiplies (351576 rows of 128 to 256: 200 us, tiles 196; 1048576: 530 and 581).
 constexpr double ROWS_FROM = 26e6;
-constexpr int ROWS_LAUNCHES = 4;
 // A launch has less than 2^32 threads, 256 a tile: 2^31 rows of few columns need larger tiles than the smallest.
 constexpr int64_t LAUNCH_TILES = 1 << 24;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
@@ -105,7 +105,9 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     if (rows && layout != GEMM_RC_RC && best.splits == 1) {
         const RowsShape s = rows_shape(m, n, k, es, gated, slope);
         const double cols = gated ? 2.0 * s.cols : s.cols;
-        best.rows = s.grid && s.launches <= (slope ? 2 : ROWS_LAUNCHES) && (double)m * cols >= ROWS_FROM * (k > cols ? (double)k / cols : 1.0) * (s.launches > 1 ? 2.0 : 1.0);
+        const int most = es == 2 ? slope ? 2 : 4 : gated && !slope ? 4 : 1;
+        const double from = ROWS_FROM * (k > cols ? (double)k / cols : 1.0) * (s.launches > 1 ? 2.0 : 1.0) * (es == 4 && k > 64 ? 4.0 : 1.0);
+        best.rows = s.grid && s.launches <= most && (double)m * cols >= from;
     }
     return best;
 }
@@ -141,12 +143,10 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         using T = std::remove_pointer_t<decltype(t)>;
         if (c.tile == SKINNY) return launch_skinny<T>(g, aligned, st);
         if (c.tile == THIN) return launch_thin<T>(g, layout, st);
-        if constexpr (sizeof(T) == 2) {
-            if (c.rows && (uintptr_t)g.a % 16 == 0 && g.lda * es % 16 == 0) {
-                const RowsShape r = rows_shape(g.m, g.n, g.k, es, gated, g.mode == GEMM_SLOPE || g.mode == GEMM_GATED_SLOPE);
-                if (sum_rows) *sum_rows = r.grid * r.wr;
-                return launch_rows<T>(g, layout, st);
-            }
+        if (c.rows && (uintptr_t)g.a % 4 == 0 && g.lda * es % 4 == 0) {
+            const RowsShape r = rows_shape(g.m, g.n, g.k, es, gated, g.extra);
+            if (sum_rows) *sum_rows = r.grid * r.wr;
+            if (r.grid) return launch_rows<T>(g, layout, st);
         }
         int tile = c.tile;
         if ((!aligned || g.a_lo || g.out_lo) && tile > 1) tile = 1;
@@ -188,7 +188,7 @@ struct ForwardPlan { Cut z; size_t x, w, need; };
 ForwardPlan forward_plan(const Layer& l) {
     ForwardPlan p = {};
     p.z = cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated);
-    if (p.z.tile >= 0 && !whole(l, l.in)) {
+    if (p.z.tile >= 0 && !whole(l, l.in) && !(p.z.rows && l.dtype == SR_F32)) {
         const size_t x = copy_bytes(l, l.rows, l.in), w = copy_bytes(l, l.wide, l.in);
         if (copies_pay(p.z.us, x + w, 2)) p.x = x, p.w = w;
     }

@@ -439,36 +439,36 @@ def test_bias_gradients_of_very_many_rows(gated, shape, t):
 
 # so many outputs that the kernel which holds the weight takes them: k that ends inside a step, widths that are no pieces, several launches
 HELD = [(65600, 64, 410), (131100, 40, 200), (131075, 136, 201), (70001, 250, 400), (262200, 264, 120), (140000, 8, 264), (110000, 72, 1030), (300000, 512, 100), (56000, 512, 500), (70000, 130, 391),
-        (211111, 100, 255), (430001, 120, 62), (900000, 24, 40)]
+        (211111, 100, 255), (430001, 120, 62), (900000, 24, 40), (351576, 27, 121), (131080, 59, 300)]
 
 
 @pytest.mark.parametrize("shape", HELD, ids=lambda s: "P%dC%dO%d" % s)
-@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
 def test_very_many_rows(gated, shape, t):
     kind = shape[0] % 4 + 1
     check_forward(*shape, t, kind, gated)
-    check_forward(*shape, t, lo.NONE, gated, bias=False, residual=not gated, shift=shape[0] % 2 * 8)
-    check_grad(*shape, t, kind, gated, shift=shape[0] % 2 * 3)
+    check_forward(*shape, t, lo.NONE, gated, bias=False, residual=not gated, shift=(2, 8, 1)[shape[1] % 3])
+    check_grad(*shape, t, kind, gated, shift=(0, 3, 2)[shape[1] % 3])
     check_grad(*shape, t, lo.NONE, gated)
 
 
 @pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
-@pytest.mark.parametrize("C", [40, 72, 132, 264])
-def test_rows_of_nan_among_very_many(gated, C):
+@pytest.mark.parametrize("t,C", [("bf16", 40), ("bf16", 72), ("bf16", 132), ("bf16", 264), ("f32", 40), ("f32", 59), ("f32", 101)])
+def test_rows_of_nan_among_very_many(gated, t, C):
     P, O = 131080, 256 if gated else 264
-    d = inputs(P, C, O, "bf16", gated, 5)
-    clean = run_forward(d, "bf16", lo.SILU, gated).clone()
+    d = inputs(P, C, O, t, gated, 5)
+    clean = run_forward(d, t, lo.SILU, gated).clone()
     at = torch.tensor([0, 63, 777, 65536, P - 2], device=DEV)
     d["x"][at] = float("nan")
-    y = run_forward(d, "bf16", lo.SILU, gated)
+    y = run_forward(d, t, lo.SILU, gated)
     rows = torch.ones(P, dtype=torch.bool, device=DEV)
     rows[at] = False
     assert torch.equal(y[rows], clean[rows]) and y[~rows].isnan().all()
     d["x"].zero_()
-    clean = run_grad(d, "bf16", lo.NONE, gated, want=(True, False, False))[0].clone()
+    clean = run_grad(d, t, lo.NONE, gated, want=(True, False, False))[0].clone()
     d["dy"][at] = float("nan")
-    dx = run_grad(d, "bf16", lo.NONE, gated, want=(True, False, False))[0]
+    dx = run_grad(d, t, lo.NONE, gated, want=(True, False, False))[0]
     assert torch.equal(dx[rows], clean[rows]) and dx[~rows].isnan().all()
 
 
