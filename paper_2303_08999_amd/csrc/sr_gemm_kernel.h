@@ -79,14 +79,39 @@ struct Operand {
     static __device__ __forceinline__ bool other(int i, int wave) { return GATED && ((i * NW + wave) * 8 / MT & 1); }
     __device__ __forceinline__ const char* from(int i, int wave) const { return GATED && other(i, wave) ? base + second : base; }
     // Straight to LDS; the whole of it is there.  Written out, because the compiler lets every turning LDS read wait for all loads to LDS that it
-    // knows of, whatever they write: landed() is what waits for these.  The instruction takes the place from m0, a wait state behind its writing.
+    // knows of, whatever they write: landed() is what waits for these.  The instruction takes the place from m0, a wait state behind
+    // its writing, and the base from scalar registers, five behind a vector instruction that wrote them (the compiler counts neither for instructions it did not place).
     __device__ __forceinline__ void fetch(char* lds, int wave, int i) const {
-        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+        asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1"
                      :: "v"(off[i]), "s"(from(i, wave)), "{m0}"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024)) : "memory");
     }
     __device__ __forceinline__ void fetch(char* lds, int wave) const {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) fetch(lds, wave, i);
+    }
+    // fp32 off 16-byte pieces: by 4 bytes, their places worked out anew each time (four times as many registers would not be there).  row_of: as for init;
+    // last: of the rows, from the tile's first (RC).
+    template <typename RowOf>
+    __device__ __forceinline__ void fetch_fours(char* lds, int wave, int lane, int64_t ld, int last, RowOf row_of) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint64_t p = (uint64_t)from(i, wave);
+            const uint64_t uniform = (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)p);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int pos = (i * NW + wave) * 1024 + j * 256 + lane * 4;
+                unsigned at;
+                if constexpr (!RC) {
+                    const int r = pos / 128;
+                    at = (unsigned)row_of(r) * (unsigned)(ld * 4) + (((pos % 128 / 16) ^ (r & 7)) << 4) + pos % 16;
+                } else {
+                    const int k = pos / RB, slot = pos % RB, r = ((slot / CB) ^ turn(k)) * 16 + slot % CB / 4;
+                    at = ((unsigned)k * (unsigned)ld + (unsigned)(r < last ? r : last)) * 4;
+                }
+                asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1"
+                             :: "v"(at), "s"(uniform), "{m0}"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024 + j * 256)) : "memory");
+            }
+        }
     }
     // By way of registers: `k` values of k are left, rows behind the last are zeros where pieces may be cut
     __device__ __forceinline__ void load(u32x4g v[LOADS], int wave, int k, int row0, int rows, bool aligned) const {
@@ -157,7 +182,9 @@ struct Reader {
     }
 };
 
-template <typename T, int LAYOUT, bool GATED, bool ALIGNED, int TILE>
+// ALIGN: how operands come to LDS
+enum { BY_REGISTERS = 0, BY_PIECES = 1, BY_FOURS = 2 };
+template <typename T, int LAYOUT, bool GATED, int ALIGN, int TILE>
 __global__ __launch_bounds__((gemm_threads<TILE, T>), (GemmShape<TILE, T>::OCC))
 void k_gemm(const GemmArgs g) {
     using S = GemmShape<TILE, T>;
@@ -192,12 +219,23 @@ void k_gemm(const GemmArgs g) {
 
     OpA oa;
     OpB ob;
-    oa.init(g.a, g.lda, m0, g.m, wave, lane, k0, ALIGNED, 0, [&](int r) { return m0 + r < g.m ? r : g.m - 1 - m0; });
+    const auto row_a = [&](int r) { return m0 + r < g.m ? r : g.m - 1 - m0; };
     // gated: every MT rows of the first half are followed by the same MT of the second
-    ob.init(g.b, g.ldb, n0, g.n, wave, lane, k0, ALIGNED, g.half, [&](int r) {
+    const auto row_b = [&](int r) {
         const int c = GATED ? r / (2 * MT) * MT + r % MT : r;
         return n0 + c < g.n ? c : g.n - 1 - n0;
-    });
+    };
+    oa.init(g.a, g.lda, m0, g.m, wave, lane, k0, ALIGN == BY_PIECES, 0, row_a);
+    ob.init(g.b, g.ldb, n0, g.n, wave, lane, k0, ALIGN == BY_PIECES, g.half, row_b);
+    const auto fetch_both = [&](char* to) {
+        if constexpr (ALIGN == BY_FOURS) {
+            oa.fetch_fours(to, wave, lane, g.lda, g.m - 1 - m0, row_a);
+            ob.fetch_fours(to + OpA::BYTES, wave, lane, g.ldb, g.n - 1 - n0, row_b);
+        } else {
+            oa.fetch(to, wave);
+            ob.fetch(to + OpA::BYTES, wave);
+        }
+    };
     const int64_t step_a = (ARC ? g.lda * BK : (int64_t)BK) * (int)sizeof(T), step_b = (BRC ? g.ldb * BK : (int64_t)BK) * (int)sizeof(T);
 
     const int wm = wave / NWN * WM, wn = wave % NWN * WN;
@@ -270,22 +308,21 @@ void k_gemm(const GemmArgs g) {
     const int full = kn / BK, tail = kn - full * BK;
     auto loop = [&](auto with) {
         constexpr bool SUMS = decltype(with)::value;
-        if constexpr (ALIGNED) {
+        if constexpr (ALIGN != BY_REGISTERS) {
             // the cut tile first, by way of registers; then the others, each fetched while the one before is multiplied
             int buf = 0, left = full;
             if (tail) {
                 u32x4g va[OpA::LOADS], vb[OpB::LOADS];
                 oa.advance(step_a * full);
                 ob.advance(step_b * full);
-                oa.load(va, wave, tail, m0, g.m, true);
-                ob.load(vb, wave, tail, n0, g.n, true);
+                oa.load(va, wave, tail, m0, g.m, ALIGN == BY_PIECES);
+                ob.load(vb, wave, tail, n0, g.n, ALIGN == BY_PIECES);
                 oa.park(lds, wave, lane, va);
                 ob.park(lds + OpA::BYTES, wave, lane, vb);
                 oa.advance(-step_a * full);
                 ob.advance(-step_b * full);
             } else if (left) {
-                oa.fetch(lds, wave);
-                ob.fetch(lds + OpA::BYTES, wave);
+                fetch_both(lds);
                 oa.advance(step_a);
                 ob.advance(step_b);
                 --left;
@@ -420,8 +457,7 @@ void k_gemm(const GemmArgs g) {
                 landed();                                // everyone's part of the tile is in LDS, and nobody reads the other buffer any more
                 char* const other = lds + (buf ^ 1) * STAGE;
                 if (left > 0) {
-                    oa.fetch(other, wave);
-                    ob.fetch(other + OpA::BYTES, wave);
+                    fetch_both(other);
                     oa.advance(step_a);
                     ob.advance(step_b);
                     --left;
@@ -607,19 +643,21 @@ void k_gemm(const GemmArgs g) {
     }
 }
 
-template <typename T, int LAYOUT, bool GATED, bool ALIGNED, int TILE>
+template <typename T, int LAYOUT, bool GATED, int ALIGN, int TILE>
 hipError_t start_gemm(const GemmArgs& g, hipStream_t st) {
     const int64_t blocks = (int64_t)g.tiles_m * g.tiles_n * g.splits;
     if (blocks < 1 || blocks > 0x7fffffff) return hipErrorInvalidValue;
-    k_gemm<T, LAYOUT, GATED, ALIGNED, TILE><<<(int)blocks, gemm_threads<TILE, T>, 0, st>>>(g);
+    k_gemm<T, LAYOUT, GATED, ALIGN, TILE><<<(int)blocks, gemm_threads<TILE, T>, 0, st>>>(g);
     return hipGetLastError();
 }
 template <typename T, int LAYOUT, bool GATED>
 hipError_t pick_gemm(const GemmArgs& g, bool aligned, int tile, hipStream_t st) {
-    if (!aligned) return tile == 0 ? start_gemm<T, LAYOUT, GATED, false, 0>(g, st) : start_gemm<T, LAYOUT, GATED, false, 1>(g, st);
-    if (tile == 0) return start_gemm<T, LAYOUT, GATED, true, 0>(g, st);
-    if (tile == 1) return start_gemm<T, LAYOUT, GATED, true, 1>(g, st);
-    return tile == 2 ? start_gemm<T, LAYOUT, GATED, true, 2>(g, st) : start_gemm<T, LAYOUT, GATED, true, 3>(g, st);
+    // fp32 is on 4 bytes wherever it is
+    constexpr int OFF = sizeof(T) == 4 ? BY_FOURS : BY_REGISTERS;
+    if (!aligned) return tile == 0 ? start_gemm<T, LAYOUT, GATED, OFF, 0>(g, st) : start_gemm<T, LAYOUT, GATED, OFF, 1>(g, st);
+    if (tile == 0) return start_gemm<T, LAYOUT, GATED, BY_PIECES, 0>(g, st);
+    if (tile == 1) return start_gemm<T, LAYOUT, GATED, BY_PIECES, 1>(g, st);
+    return tile == 2 ? start_gemm<T, LAYOUT, GATED, BY_PIECES, 2>(g, st) : start_gemm<T, LAYOUT, GATED, BY_PIECES, 3>(g, st);
 }
 
 }  // namespace

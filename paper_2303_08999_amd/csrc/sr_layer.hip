@@ -75,7 +75,7 @@ constexpr double ROWS_FROM = 26e6;
 constexpr int64_t LAUNCH_TILES = 1 << 24;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
 // caches, at 4.5 past them.
-Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true, bool rows = true, bool slope = false) {
+Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, bool thin = true, bool rows = true, bool slope = false, int tiles_up_to = 4) {
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0, false};
     if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
@@ -85,7 +85,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     const int64_t nn = gated ? 2 * n : n;
     Cut best = {0, 1, 0, 0.0, false};
     double least = 1e300;
-    for (int tile = 0; tile < 4; ++tile) {
+    for (int tile = 0; tile < tiles_up_to; ++tile) {
         const int64_t tiles = ((m + gemm_tile_rows(tile) - 1) / gemm_tile_rows(tile)) * ((nn + gemm_tile_cols(tile) - 1) / gemm_tile_cols(tile));
         if (tiles >= LAUNCH_TILES && tile < 3) continue;
         auto look = [&](int64_t splits) {
@@ -173,12 +173,15 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
     });
 }
 
-// Rows on 16-byte pieces: dz, and copies of tensors that are not, for products by tiles that take longer than the copies: the tile kernels read other rows by way of
-// registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1106 us).
+// Rows on 16-byte pieces: dz, and copies of tensors that are not, where the products gain more than the copies take.  16-bit types: the tile kernels read other rows by way
+// of registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1106 us, so 527).  fp32 goes to LDS by 4 bytes (500 rows of 333 to 555: 16
+// us, by registers 21); copies have the larger tiles to gain.
 int64_t whole_row(const Layer& l, int64_t cols) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (cols + e - 1) / e * e; }
 bool whole(const Layer& l, int64_t cols) { return whole_row(l, cols) == cols; }
 size_t copy_bytes(const Layer& l, int64_t rows, int64_t cols) { return up256((size_t)rows * whole_row(l, cols) * layer_esize(l.dtype)); }
-bool copies_pay(double us, size_t bytes, int copies) { return 1.2 * us > 4.0 * copies + 2.0 * (double)bytes / 4.5e6; }
+constexpr int TILES_OFF_PIECES = 2;
+constexpr double OFF_PIECES = 1.1;          // what these take there, of what tile_time says (8192 rows of 4095 to 4097, fp32: 1828 us, with copies 1722)
+bool copies_pay(double gain, size_t bytes, int copies) { return gain > 4.0 * copies + 2.0 * (double)bytes / 4.5e6; }
 hipError_t copy_rows(const Layer& l, const void* from, int64_t rows, int cols, void* to, hipStream_t st) {
     return by_type(l.dtype, [&](auto t) { return launch_pack<std::remove_pointer_t<decltype(t)>>(from, rows, cols, to, st); });
 }
@@ -187,10 +190,13 @@ hipError_t copy_rows(const Layer& l, const void* from, int64_t rows, int cols, v
 struct ForwardPlan { Cut z; size_t x, w, need; };
 ForwardPlan forward_plan(const Layer& l) {
     ForwardPlan p = {};
-    p.z = cut_of(l.rows, l.out, l.in, layer_esize(l.dtype), GEMM_KC_KC, l.gated);
-    if (p.z.tile >= 0 && !whole(l, l.in) && !(p.z.rows && l.dtype == SR_F32)) {
+    const size_t es = layer_esize(l.dtype);
+    p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated);
+    if (p.z.tile >= 0 && !whole(l, l.in) && !(p.z.rows && es == 4)) {
         const size_t x = copy_bytes(l, l.rows, l.in), w = copy_bytes(l, l.wide, l.in);
-        if (copies_pay(p.z.us, x + w, 2)) p.x = x, p.w = w;
+        const Cut off = es == 4 ? cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, true, false, false, TILES_OFF_PIECES) : p.z;
+        if (copies_pay(es == 4 ? OFF_PIECES * off.us - p.z.us : 1.2 * p.z.us, x + w, 2)) p.x = x, p.w = w;
+        else p.z = off;
     }
     p.need = p.x + p.w + partial_bytes(p.z, l.rows, l.wide);
     return p;
@@ -213,22 +219,33 @@ GradPlan grad_plan(const Layer& l, int act) {
         const int64_t blocks = (l.rows + 63) / 64;
         p.pass = (int)(blocks < 2 * GPU_CUS ? blocks : 2 * GPU_CUS);
     }
-    p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false);
-    p.w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false);
+    if (again) p.parts = es == 2 && 2.0 * (double)l.rows * l.in * l.wide <= TWO_PARTS_UP_TO ? 2 : 1;
+    const bool free = p.parts < 2;                         // of second parts: any kernel
+    auto cut = [&](int tiles) {
+        p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, free, free, false, tiles);
+        p.w = cut_of(l.wide, l.in, l.rows, es, GEMM_RC_RC, false, false, false, false, tiles);
+        if (again) p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false, free, true, tiles);
+        return p.z.us + p.x.us + p.w.us;
+    };
+    size_t copies[3] = {whole(l, l.in) ? 0 : copy_bytes(l, l.rows, l.in), whole(l, l.in) ? 0 : copy_bytes(l, l.wide, l.in),
+                        again || whole(l, l.out) ? 0 : copy_bytes(l, l.rows, l.out)};
+    const size_t copied = copies[0] + copies[1] + copies[2];
+    double us = cut(4);
+    if (l.rows && copied) {
+        const double off = es == 4 ? cut(TILES_OFF_PIECES) : 0.0;
+        if (copies_pay(es == 4 ? OFF_PIECES * off - us : 1.2 * us, copied, 3)) {
+            p.copy_x = copies[0], p.copy_w = copies[1], p.copy_dy = copies[2];
+            if (es == 4) us = cut(4);
+        }
+    }
     size_t most = 0;
     if (again) {
-        p.parts = es == 2 && 2.0 * (double)l.rows * l.in * l.wide <= TWO_PARTS_UP_TO ? 2 : 1;
-        if (p.parts == 2) p.x = cut_of(l.rows, l.in, l.wide, es, GEMM_KC_RC, false, false, false);
-        p.z = cut_of(l.rows, l.out, l.in, es, GEMM_KC_KC, l.gated, false, p.parts == 1, true);
         // fp32 loses nothing on the way; there it is only that the large tiles' sums beside dW cost their workgroups a sixth
         p.slopes = p.parts == 1 && p.z.tile >= 0 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
         p.dz = up256((size_t)p.parts * l.rows * whole_row(l, l.wide) * es);
         p.sums = p.slopes ? slope_sum_bytes(p.z, l) : 0;
         most = partial_bytes(p.z, l.rows, l.wide);
     }
-    size_t copies[3] = {whole(l, l.in) ? 0 : copy_bytes(l, l.rows, l.in), whole(l, l.in) ? 0 : copy_bytes(l, l.wide, l.in),
-                        again || whole(l, l.out) ? 0 : copy_bytes(l, l.rows, l.out)};
-    if (l.rows && copies_pay(p.z.us + p.x.us + p.w.us, copies[0] + copies[1] + copies[2], 3)) p.copy_x = copies[0], p.copy_w = copies[1], p.copy_dy = copies[2];
     const size_t x = partial_bytes(p.x, l.rows, l.in);
     const size_t w = partial_bytes(p.w, l.wide, l.in) + (p.w.splits > 1 ? up256((size_t)p.w.splits * l.wide * 4) : 0);
     if (x > most) most = x;

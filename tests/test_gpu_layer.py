@@ -418,11 +418,11 @@ def test_more_elements_than_32_bits_count(P, C, O):
 
 
 # features that are no 16-byte pieces, in products long enough for copies that are
-@pytest.mark.parametrize("shape,t", [((2500, 1021, 2053), "bf16"), ((3000, 1754, 1183), "f16"), ((1500, 777, 1030), "f32"), ((9000, 1032, 777), "bf16")], ids=str)
+@pytest.mark.parametrize("shape,t", [((2500, 1021, 2053), "bf16"), ((3000, 1754, 1183), "f16"), ((1500, 777, 1030), "f32"), ((9000, 1032, 777), "bf16"), ((8200, 2047, 2049), "f32")], ids=str)
 @pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
 def test_copies_on_whole_pieces(gated, shape, t):
     P, C, O = shape
-    if C % 8:
+    if C % 8 and t != "f32":                                      # which the tile kernels read as it is
         need = sr.sr_layer_gated_workspace_bytes if gated else sr.sr_layer_linear_workspace_bytes
         assert need(P, C, O, DT[t]) >= P * C * DT[t].itemsize
     for kind, shift in ((lo.NONE, 0), (lo.SILU, 1)):
