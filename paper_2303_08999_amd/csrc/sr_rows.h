@@ -74,14 +74,15 @@ __global__ __launch_bounds__(512, 2) void k_rows(const GemmArgs g, const int wn,
     const auto fetch = [&](int block, char* to) {
         const int row0 = block * block_rows, last = g.m - 1 - row0;
         const char* const from = (const char*)g.a + (int64_t)row0 * g.lda * (int)sizeof(T);
-        // (s_nop: a base that a vector instruction wrote is there five wait states later)  What is behind a row or the last row is read in their place, and taken out when it is used or not stored
+        // what is behind a row or the last row is read in their place, and taken out when it is used or not stored (the moves: see the tile kernel's loads)
         if (whole) {
             for (int i = wave; i < loads; i += waves) {
                 const int x = i * 64 + lane, row = (int)(x * per_row >> 20);
                 int p = (x - row * PS * steps) ^ turn(row);
                 if (p >= pieces) p = pieces - 1;
                 const unsigned off = (unsigned)(row < last ? row : last) * (unsigned)(g.lda * (int)sizeof(T)) + p * 16;
-                asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 1024)) : "memory");
+                uint64_t at;
+                asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(at) : "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 1024)) : "memory");
             }
         } else {
             const int fours = (g.k * (int)sizeof(T) + 3) / 4;
@@ -90,7 +91,8 @@ __global__ __launch_bounds__(512, 2) void k_rows(const GemmArgs g, const int wn,
                 int p = ((x - row * PS * steps) ^ turn(row)) * 4 + lane % 4;
                 if (p >= fours) p = fours - 1;
                 const unsigned off = (unsigned)(row < last ? row : last) * (unsigned)(g.lda * (int)sizeof(T)) + p * 4;
-                asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" :: "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 256)) : "memory");
+                uint64_t at;
+                asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0" : "=&s"(at) : "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 256)) : "memory");
             }
         }
     };
