@@ -13,10 +13,12 @@
  *
  * All tensors of a call have one type, f32, f16 or bf16.  Products are summed in fp32 or better; those of
  * 16-bit values are exact, those of f32 values are within 2^-24 of themselves.  Bias, activation and the rest are
- * fp32; each output is rounded once.  Only the gradient of z is rounded to the tensors' type on its way
- * between two products, where an activation or a gate makes it: it is an operand of 16-bit matrix instructions
- * then, and the next products of a training step round it the same way.  Infinities and NaN in the inputs stay
- * in the rows and columns to which the formulas take them; what an infinity makes there may be NaN.
+ * fp32; each output is rounded once.  z's gradient, where an activation or a gate makes it, is an operand of two more
+ * products: f16 and bf16 calls of up to 2e9 operations a product (2 rows x in x rows of the weight) hold it in two numbers of
+ * their type, to 2^-17 of itself or better (f16: or 2^-25), larger ones round it once, as the next layer of a training step does
+ * with what it is given; the bias's gradient is summed before that where it is rounded once.  An f16 gradient of z beyond 65504 is an infinity on that
+ * way.  Infinities and NaN in the inputs stay in the rows and columns to which the formulas take them; what an infinity makes
+ * there may be NaN.
  *
  * All rules of sr_dict.h hold: contiguous device memory of the caller at any address aligned to its elements,
  * every check on the host before anything is launched, its statuses, no allocation, no synchronisation, work

@@ -4,7 +4,7 @@
 // Operands of one type, fp32, fp16 or bfloat16; sums in fp32.  An operand is stored with k running fastest (KC: a layer's rows and
 // its weight in the forward product) or with the other index running fastest (RC: the weight in dx = dz W, both in dW = dz^T x).
 // A workgroup makes a BM x BN tile of C.  128 bytes of k (64 values, 32 of fp32) of both operands go to LDS at a time, two buffers in
-// turn: while one is multiplied the next is under way, straight from memory to LDS.  RC operands are turned by the LDS
+// turn: while one is multiplied the next is under way, straight from memory to LDS (16-bit rows that are no pieces of 16 bytes: by way of registers).  RC operands are turned by the LDS
 // reads (16-bit types) or read value by value (fp32, whose matrix instructions are slow enough for that).
 //
 // LDS: KC as [row][8 pieces of 16 bytes], piece p of row r in place p ^ (r & 7), so that the 16 or 32 rows a read takes at one k lie in

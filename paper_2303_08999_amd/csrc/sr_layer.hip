@@ -1,7 +1,7 @@
 // Layers and their gradients (include/sr_layer.h): checks, which kernels a call is made of, and their workspace.
 //
-// A gradient is three products: z made anew, with dz = dy act'(z) as its epilogue, stored in the workspace; dx = dz W; dW = dz^T x, whose
-// workgroups of the first column of tiles sum dz over the rows on the way (db).  Without an activation dy is dz.
+// A gradient is three products: z made anew, with dz = dy act'(z) as its epilogue, stored in the workspace; dx = dz W; dW = dz^T x.  db comes from sums that the
+// first leaves on its way out, or from the workgroups of dW's first column of tiles, which sum dz beside it.  Without an activation dy is dz.
 #include <stdint.h>
 #include <type_traits>
 

@@ -1,4 +1,4 @@
-// Products of few rows with a weight (sr_gemm.h), and the sums of split products.
+// Products of few rows with a weight (sr_gemm.h), the sums of split products and of dz, and copies on 16-byte pieces.
 #pragma once
 #include "sr_gemm.h"
 
