@@ -68,7 +68,7 @@ __global__ __launch_bounds__(512, 2) void k_rows(const GemmArgs g, const int wn,
 
     // Rows in LDS: pieces of 16 bytes, those of a row exchanged so that 8 rows at one k lie in different banks.
     const auto turn = [&](int row) { return stride & 64 ? row >> 1 & 3 : row & 7; };
-    const int block_rows = 32 * wr * subs, blocks = (g.m + block_rows - 1) / block_rows, loads = block_rows * stride / 1024;
+    const int block_rows = 32 * wr * subs, blocks = g.m / block_rows + (g.m % block_rows != 0), loads = block_rows * stride / 1024;
     const unsigned per_row = (1 << 20) / (PS * steps) + 1;                 // x * per_row >> 20 = x / (PS steps) for x < 4096
     const bool whole = (uintptr_t)g.a % 16 == 0 && g.lda % E == 0;         // else rows come by 4 bytes
     const auto fetch = [&](int block, char* to) {

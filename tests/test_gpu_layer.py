@@ -581,8 +581,8 @@ def test_gradients_beyond_the_type_are_infinite(gated, P, t):
     assert db[~rows].isfinite().all() and (db[rows].float() == math.inf).all()
 
 
-def test_more_rows_than_a_launch_of_small_tiles_has():
-    P = (1 << 30) + 77
+@pytest.mark.parametrize("P", [(1 << 30) + 77, (1 << 31) - 300])
+def test_more_rows_than_a_launch_of_small_tiles_has(P):
     at = torch.tensor([0, 1, 4095, P // 2, P - 130, P - 2, P - 1], device=DEV)
     g = torch.Generator(device=DEV).manual_seed(3)
     x = torch.zeros((P, 1), device=DEV, dtype=torch.bfloat16)
