@@ -8,6 +8,7 @@ if the library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
 
@@ -701,27 +702,45 @@ def _dense(t):
     return True
 
 
+_PIECE = 1 << 30
+_one = struct.Struct("@Qiiiii4x").pack
+
+
+def _elements(t):
+    """What describes a tensor that is gone through element by element, packed: its axes in the four fields, which are 32-bit integers; where
+    one is beyond that, pieces of 2^30 elements, and behind them what is left.  (Packing refuses what a structure's own fields would cut to 32 bits.)"""
+    shape, code, count = t.shape, _codes.get(t.dtype) or _code(t.dtype), t.numel()
+    address, axes = t.data_ptr() if count else 0, len(shape)
+    try:
+        if axes == 1:
+            return _one(address, code, 1, 1, 1, *shape)
+        if axes <= 4:
+            return _one(address, code, *(1,) * (4 - axes), *shape)
+        return _one(address, code, math.prod(shape[:-3]), *shape[-3:])
+    except struct.error:
+        pieces, rest = divmod(count, _PIECE)
+        described = _one(address, code, 1, 1, pieces, _PIECE)
+        return described + _one(address + pieces * _PIECE * t.element_size(), code, 1, 1, 1, rest) if rest else described
+
+
 class sr_tensor_list:
     """Descriptions of a list of tensors, made once and used for as long as they are where they are (the tensors are kept
-    alive).  All on one device, of any number of axes, stored without gaps in any order of them: a list is gone through
-    element by element."""
+    alive).  All on one device, of any number of axes and any sizes, stored without gaps in any order of them: a list is gone through
+    element by element.  ``count`` descriptions: one a tensor, two where an axis has 2^31 elements or more and they are no multiple of 2^30."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        self.array = (sr_tensor * max(1, len(self.tensors)))()
         self.strides = [t.stride() for t in self.tensors]
         self.device = self.tensors[0].get_device() if self.tensors else -1
-        for d, t in zip(self.array, self.tensors):
+        described = b""
+        for t in self.tensors:
             if not t.is_cuda or t.get_device() != self.device:
                 raise ValueError(f"a tensor is on {t.device}: expected all of them on one device")
             if not _dense(t):
                 raise ValueError("expected tensors without gaps")
-            shape = tuple(t.shape)
-            lead = 1
-            for n in shape[:-3]:
-                lead *= n
-            d.data, d.dtype = (t.data_ptr() if t.numel() else 0) or None, _code(t.dtype)
-            d.n, d.c, d.h, d.w = (lead,) + (1,) * (3 - len(shape)) + shape[-3:]
+            described += _elements(t)
+        self.count = len(described) // ctypes.sizeof(sr_tensor)
+        self.array = (sr_tensor * max(1, self.count)).from_buffer_copy(described or bytes(ctypes.sizeof(sr_tensor)))
 
     def __len__(self):
         return len(self.tensors)
@@ -733,21 +752,24 @@ def sr_grad_clip_workspace_bytes(tensors: int) -> int:
 
 def sr_grad_clip(grads, outs, max_norm, norm, workspace=None, stream=None):
     """The norm over all ``grads`` and the factor to at most ``max_norm``, into ``norm`` (float32, 2), and the gradients times that
-    factor into ``outs`` (``grads`` itself: in place; None: the norm alone).  Both are lists of tensors, or sr_tensor_list."""
+    factor into ``outs`` (``grads`` itself: in place; None: the norm alone).  Both are lists of tensors, or sr_tensor_list, whose ``count`` is what
+    sr_grad_clip_workspace_bytes takes for the caller's own scratch."""
     import torch
     lib = _lib or load()
     described = grads if isinstance(grads, sr_tensor_list) else sr_tensor_list(grads)
-    count = len(described.tensors)
+    count = described.count
     if outs is None:
         into = None
     elif outs is grads:
         into = described.array
     else:
         out = outs if isinstance(outs, sr_tensor_list) else sr_tensor_list(outs)
-        if len(out.tensors) != count:
+        if len(out.tensors) != len(described.tensors):
             raise ValueError("as many outputs as gradients")
         if out.strides != described.strides:
             raise ValueError("an output is stored in another order than its gradient")
+        if out.count != count:
+            raise ValueError("an output has another size than its gradient")
         if count and out.device != described.device:
             raise ValueError("the outputs are on another device than the gradients")
         into = out.array

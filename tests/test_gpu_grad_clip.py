@@ -183,3 +183,28 @@ def test_lists_kept_streams_and_graphs():
         g[0].add_(1.0)
         sr.sr_grad_clip(g, out, 1.0, stats)
         first = [o.clone() for o in out]
+
+
+@pytest.mark.parametrize("shape,t", [(((1 << 32) + 5,), "bf16"), (((1 << 31) + 3,), "f16"), ((1 << 32,), "bf16"), ((3, 1 << 31), "f16"), ((1 << 16, (1 << 16) + 1, 1, 1, 1), "bf16")],
+                         ids=lambda v: "x".join(map(str, v)) if isinstance(v, tuple) else v)
+def test_a_tensor_of_more_elements_than_32_bits_count(shape, t):
+    """A bucket beyond 2^31 and 2^32 elements beside a small tensor; all values but a few, some of them the last, are zeros."""
+    big, small = torch.zeros(shape, device=DEV, dtype=DT[t]), torch.tensor([2.0, -4.0], device=DEV)
+    flat, n = big.view(-1), big.numel()
+    at = torch.tensor(sorted({0, 7, (1 << 30) - 1, 1 << 30, (1 << 31) - 1, min(1 << 31, n - 3), n // 2 + 1, n - 2, n - 1}), device=DEV)
+    flat[at] = torch.arange(1, len(at) + 1, device=DEV).to(DT[t])
+    values = flat[at].double()
+    norm = math.sqrt(float((values ** 2).sum()) + 20.0)
+    stats = torch.empty(2, device=DEV)
+    grads = sr.sr_tensor_list([big, small])
+    ws = torch.empty(sr.sr_grad_clip_workspace_bytes(grads.count), device=DEV, dtype=torch.uint8)
+    sr.sr_grad_clip(grads, grads, norm / 4, stats, workspace=ws)
+    torch.cuda.synchronize()
+    assert abs(float(stats[0]) - norm) <= 2 * U * norm and abs(float(stats[1]) - 0.25) <= 2 * U
+    # the quarter of a small whole number is one of the type's, but for the factor's own rounding
+    assert ((flat[at].double() - values / 4).abs() <= (torch.finfo(DT[t]).eps / 2 + 4 * U) * values).all()
+    assert ((small.double() - torch.tensor([0.5, -1.0], device=DEV)).abs() <= 4 * U).all()
+    assert int(torch.count_nonzero(flat)) == len(at)
+    if len(shape) == 1 and n % (1 << 30):
+        with pytest.raises(ValueError, match="another size"):
+            sr.sr_grad_clip(grads, [flat[:1 << 30], small], 1.0, stats)

@@ -247,3 +247,26 @@ def test_tensors_without_gaps():
     assert binding._dense(t) and binding._dense(t.permute(2, 0, 1)) and binding._dense(t[:, :1][:2].permute(1, 0, 2)[:, :1])
     assert binding._dense(torch.zeros(2, 3, 4, 5).to(memory_format=torch.channels_last))
     assert not binding._dense(t[:, ::2]) and not binding._dense(t[..., :7]) and not binding._dense(torch.zeros(4, 1).expand(4, 3))
+
+
+def test_lists_of_tensors_beyond_32_bits_are_described_whole():
+    """No field of a description is cut to 32 bits: what is described has the tensor's elements, one piece behind the other."""
+    def fields(t):
+        packed = binding._elements(t)
+        array = (sr.sr_tensor * (len(packed) // ctypes.sizeof(sr.sr_tensor))).from_buffer_copy(packed)
+        return [(d.data, d.dtype, d.n, d.c, d.h, d.w) for d in array]
+
+    for shape in ((1 << 31,), ((1 << 32) + 5,), (3 * 10 ** 9,), (1 << 32,), ((1 << 31) + 1, 1), (1 << 16, (1 << 16) + 1, 1, 1, 1), (1 << 11, 1 << 20, 1, 2, 1)):
+        t = torch.empty(shape, dtype=torch.bfloat16)                     # memory that nothing touches
+        at = t.data_ptr()
+        for data, dtype, n, c, h, w in fields(t):
+            assert data == at and dtype == sr.SR_BF16 and min(n, c, h, w) > 0
+            at += 2 * n * c * h * w
+        assert at == t.data_ptr() + 2 * t.numel(), shape
+    t = torch.empty((1 << 16, (1 << 15) - 1, 1, 1, 1), dtype=torch.bfloat16)
+    assert fields(t) == [(t.data_ptr(), sr.SR_BF16, (1 << 31) - (1 << 16), 1, 1, 1)]
+    assert fields(torch.empty(2, 3, 4, 5, 6))[0][2:] == (6, 4, 5, 6)
+    assert fields(torch.empty(7).half())[0][1:] == (sr.SR_F16, 1, 1, 1, 7) and fields(torch.tensor(1.0))[0][1:] == (sr.SR_F32, 1, 1, 1, 1)
+    assert fields(torch.empty(3, 0)) == [(None, sr.SR_F32, 1, 1, 3, 0)]
+    for data, dtype, n, c, h, w in fields(torch.empty((0, 1 << 32))):
+        assert data is None and n * c * h * w == 0
