@@ -12,8 +12,8 @@
  *     gated    g = x Wg^T + bg, u = x Wu^T + bu  y = act(g) u         (W = Wg on top of Wu, b = bg, bu)
  *
  * All tensors of a call have one type, f32, f16 or bf16.  Products are summed in fp32 or better; those of
- * 16-bit values are exact, those of f32 values are within 2^-24 of themselves.  Bias, activation and the rest are
- * fp32; each output is rounded once.  z's gradient, where an activation or a gate makes it, is an operand of two more
+ * 16-bit values are exact, those of f32 values are within 2^-24 of themselves (large calls hold an f32 value below 2^-110 to 2^-134, as
+ * three bfloat16 numbers).  Bias, activation and the rest are fp32; each output is rounded once.  z's gradient, where an activation or a gate makes it, is an operand of two more
  * products: f16 and bf16 calls of up to 2e9 operations a product (2 rows x in x rows of the weight) hold it in two numbers of
  * their type, to 2^-17 of itself or better (f16: or 2^-25), larger ones round it once, as the next layer of a training step does
  * with what it is given; the bias's gradient is summed before that where it is rounded once.  An f16 gradient of z beyond 65504 is an infinity on that

@@ -325,9 +325,12 @@ template <typename T, int MT> __device__ __forceinline__ void gm_mul(typename Ac
     }
 }
 // fp32 on the bfloat16 matrix instructions, sixteen times as fast as the fp32 ones: eight values as the sum of three bfloat16 numbers each, x = h + m + l
-// exactly (8 bits are rounded off to the nearest twice, what is left has 8), and of the nine products of two such sums the six that are above 2^-26
-// of x y.  Summed in fp32 like the others.  Two of these a value and three conversions a pair: a third of the matrix instructions' time where
-// a wavefront makes 64 x 64.  4096^3: 145 TFLOP/s by fp32 instructions.
+// exactly (8 bits are rounded off to the nearest twice, what is left has 8), and of the nine products of two such sums the six large ones; the other
+// three come to 2^-24 of x y at most.  Summed in fp32 like the others.  What rounds beyond bfloat16's largest number has that as its h (an infinity there would make NaN of numbers from
+// 0x1.ffp127 on; 4096^3: 655 us without, 677 with it).  Below 2^-110 the parts end at bfloat16's smallest number, 2^-133: a value is held to
+// 2^-134.  Two of these a value and three conversions a pair: a third of the matrix instructions' time where a wavefront makes 64 x 64.  4096^3: 145
+// TFLOP/s by fp32 instructions, 203 so.
+constexpr float BF16_MOST = 0x1.fep127f;
 struct Split8 { u32x4g h, m, l; };
 __device__ __forceinline__ Split8 gm_split(u32x4g a, u32x4g b) {
     using bf2g = __attribute__((ext_vector_type(2))) __bf16;
@@ -335,7 +338,8 @@ __device__ __forceinline__ Split8 gm_split(u32x4g a, u32x4g b) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float x = __uint_as_float((unsigned)(i < 2 ? a[2 * i] : b[2 * i - 4])), y = __uint_as_float((unsigned)(i < 2 ? a[2 * i + 1] : b[2 * i - 3]));
-        const unsigned h = __builtin_bit_cast(unsigned, bf2g{(__bf16)x, (__bf16)y});
+        const float hx = __builtin_amdgcn_fmed3f(x, -BF16_MOST, BF16_MOST), hy = __builtin_amdgcn_fmed3f(y, -BF16_MOST, BF16_MOST);
+        const unsigned h = __builtin_bit_cast(unsigned, bf2g{(__bf16)hx, (__bf16)hy});
         x -= __uint_as_float(h << 16), y -= __uint_as_float(h & 0xffff0000u);
         const unsigned m = __builtin_bit_cast(unsigned, bf2g{(__bf16)x, (__bf16)y});
         x -= __uint_as_float(m << 16), y -= __uint_as_float(m & 0xffff0000u);

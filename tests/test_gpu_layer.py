@@ -627,3 +627,69 @@ def test_the_bounds_tell_mistakes_apart():
     for name, wrong in mistakes.items():
         wx, ww, wb = lo.behind_dz(e["x"], e["w"], wrong)
         assert not (((dx - wx).abs() <= bounds[0]).all() and ((dw - ww).abs() <= bounds[1]).all() and ((db - wb).abs() <= bounds[2]).all()), name
+
+
+# fp32 by each kernel: few rows, fp32 instructions, tiles of three bfloat16 parts on 16-byte pieces and off them, a small weight, a weight that is held
+RANGE = [(40, 512, 64), (200, 64, 72), (2048, 512, 2048), (4096, 1024, 4096), (3000, 1021, 1030), (4200, 64, 72), (131080, 40, 264), (131080, 59, 300)]
+
+
+@pytest.mark.parametrize("shape", RANGE, ids=lambda s: "P%dC%dO%d" % s)
+def test_the_largest_fp32_values(shape):
+    """Numbers up to the largest there is times small ones are finite.  A row has one value, so an element is one product: the one rounding of an fp32
+    instruction, or six products of parts, each added with 2 u of the sum, and 2^-24 for the parts left out: 14 u in all.  The gate's two
+    products count both, and one rounding."""
+    P, C, O = shape
+    g = torch.Generator(device=DEV).manual_seed(9)
+    sign = lambda *s: torch.randint(0, 2, s, generator=g, device=DEV) * 2 - 1
+    big = lambda n: (torch.randint(0x7f7f8000, 0x7f800000, (n,), generator=g, device=DEV, dtype=torch.int32).view(torch.float32) * sign(n)).float()
+    part = lambda *s: (torch.rand(s, generator=g, device=DEV) / 4 + 0.25) * sign(*s)
+    rows, k = torch.arange(P, device=DEV), torch.arange(P, device=DEV) % C
+    x, w = torch.zeros(P, C, device=DEV), part(O, C)
+    x[rows, k] = big(P)
+    x[0, 0], x[P - 1, k[P - 1]] = torch.finfo(torch.float32).max, torch.finfo(torch.float32).min
+    y = torch.empty(P, O, device=DEV)
+    sr.sr_layer_linear(x, w, None, lo.NONE, None, y)
+    want = x[rows, k].double()[:, None] * w.double().t()[k]
+    compare("y", y, want, 14 * U * want.abs())
+    both = torch.cat([w * 2.0 ** -60, part(O, C) * 2.0 ** -100])
+    sr.sr_layer_gated(x, both, None, lo.NONE, y)
+    want = want * 2.0 ** -60 * (x[rows, k].double()[:, None] * both[O:].double().t()[k])
+    compare("gated", y, want, 30 * U * want.abs())
+    n = min(P, O)
+    dy, x = torch.zeros(P, O, device=DEV), part(P, C)
+    dy[rows[:n], rows[:n]] = big(n)
+    dx, dw, db = torch.empty(P, C, device=DEV), torch.empty(O, C, device=DEV), torch.empty(O, device=DEV)
+    sr.sr_layer_linear_grad(x, w, None, lo.NONE, dy, dx, dw, db)
+    d = dy[rows[:n], rows[:n]]
+    for name, got, other in (("dx", dx, w), ("dweight", dw, x)):
+        want = d.double()[:, None] * other[:n].double()
+        compare(name, got[:n], want, 14 * U * want.abs())
+        assert not got[n:].any()
+    assert torch.equal(db[:n], d) and not db[n:].any()
+
+
+@pytest.mark.parametrize("shape", RANGE, ids=lambda s: "P%dC%dO%d" % s)
+def test_the_smallest_fp32_values(shape):
+    """Numbers down to the smallest there is times large ones: 14 u as above, and half of bfloat16's smallest number, 2^-134, of the other factor."""
+    P, C, O = shape
+    g = torch.Generator(device=DEV).manual_seed(10)
+    rows, k = torch.arange(P, device=DEV), torch.arange(P, device=DEV) % C
+    part = lambda *s: torch.rand(s, generator=g, device=DEV) + 1
+    small = (part(P).double() * 2.0 ** -(100 + rows % 50).double()).float()
+    assert float(small.min()) < 2.0 ** -(97 + min(P, 50)) and float(small.max()) > 2.0 ** -100
+    x, w, y = torch.zeros(P, C, device=DEV), part(O, C) * 2.0 ** 90, torch.empty(P, O, device=DEV)
+    x[rows, k] = small
+    sr.sr_layer_linear(x, w, None, lo.NONE, None, y)
+    other = w.double().t()[k]
+    want = small.double()[:, None] * other
+    compare("y", y, want, 14 * U * want.abs() + 2.0 ** -134 * other)
+    n = min(P, O)
+    dy, x = torch.zeros(P, O, device=DEV), part(P, C) * 2.0 ** 90
+    dy[rows[:n], rows[:n]] = small[:n]
+    dx, dw, db = torch.empty(P, C, device=DEV), torch.empty(O, C, device=DEV), torch.empty(O, device=DEV)
+    sr.sr_layer_linear_grad(x, w, None, lo.NONE, dy, dx, dw, db)
+    for name, got, other in (("dx", dx, w), ("dweight", dw, x)):
+        want = small[:n].double()[:, None] * other[:n].double()
+        compare(name, got[:n], want, 14 * U * want.abs() + 2.0 ** -134 * other[:n].double())
+        assert not got[n:].any()
+    assert torch.equal(db[:n], small[:n]) and not db[n:].any()
