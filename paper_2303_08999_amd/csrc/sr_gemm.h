@@ -55,6 +55,7 @@ struct GemmArgs {
     float* sums;               // RC_RC: [splits][m] sums of A over k, or null; SLOPE, GATED_SLOPE: [2 tiles_m][outputs] sums of the output over m, or null
     void* sums_out;            // RC_RC of one split: sums of A, [m] in the operands' type; and where launch_gemm_finish puts them
     int sum_rows;              // of sums, for launch_gemm_finish (0: splits)
+    float* exact;              // SLOPE, GATED_SLOPE by the kernel for few rows or of split sums: [m][outputs], the output before its rounding, or null
     int64_t out_lo;            // SLOPE, GATED_SLOPE: 0, or elements from `out` to where goes what its rounding leaves off (tiles 0 and 1)
     int64_t a_lo;              // KC_RC, RC_RC: 0, or elements from A to a second matrix that is added to it (tiles 0 and 1)
 };
@@ -408,6 +409,13 @@ template <typename T> __device__ __forceinline__ float gm_rest(float v) {
     const float f = gm_get(&t);
     return fabsf(f) == INFINITY ? 0.0f : v - f;
 }
+// 8 columns of a row of an output before its rounding, and of its second half
+template <bool GATED> __device__ __forceinline__ void gm_put_exact(const GemmArgs& g, int64_t row, int col, const float z[8], const float u[8]) {
+    if (!g.exact) return;
+    float* const p = g.exact + row * (GATED ? 2 * (int64_t)g.half : g.n) + col;
+    gm_put_some(p, g.n - col, z);
+    if constexpr (GATED) gm_put_some(p + g.half, g.n - col, u);
+}
 // 8 values of an output that comes in two parts
 template <typename T> __device__ __forceinline__ void gm_put_parts(T* p, int64_t lo, int count, const float v[8]) {
     gm_put_some(p, count, v);
@@ -463,6 +471,7 @@ __device__ __forceinline__ void gm_finish8(const GemmArgs& g, int64_t row, int c
         if constexpr (GATED) u[0][i] += bu[i];
     }
     gm_finish<GATED, 1>(g, z, u, e);
+    gm_put_exact<GATED>(g, row, col, z[0], u[0]);
     T* const out = (T*)g.out + row * g.ld_out + col;
     gm_put_parts(out, g.out_lo, count, z[0]);
     if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_parts(out + g.half, g.out_lo, count, u[0]);

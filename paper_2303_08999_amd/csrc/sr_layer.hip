@@ -120,8 +120,10 @@ template <typename F> hipError_t by_type(int d, F f) {
 }
 
 // Scratch for the sums of dz over the rows that the product which makes it leaves: two of them for each row of tiles, of 128 rows where the operands are
-// off 16-byte pieces; one for each group of rows of a workgroup that holds the weight
+// off 16-byte pieces; one for each group of rows of a workgroup that holds the weight; where the product is split or of few rows, dz itself in fp32
+bool leaves_rows(const Cut& c) { return c.tile == SKINNY || c.splits > 1; }
 size_t slope_sum_bytes(const Cut& c, const Layer& l) {
+    if (leaves_rows(c)) return up256((size_t)l.rows * l.wide * 4);
     const int64_t rows = gemm_tile_rows(c.tile > 1 ? 1 : c.tile);
     int64_t all = 2 * ((l.rows + rows - 1) / rows);
     if (c.rows) {
@@ -132,13 +134,18 @@ size_t slope_sum_bytes(const Cut& c, const Layer& l) {
 }
 
 // One product, split or not.  g: operands, sizes, mode and what the epilogue needs.  `ws`: partial_bytes of scratch (and, for RC_RC with sums_out but
-// no sums, of those).  A forward product of one split with g.sums says in *sum_rows how many rows of them it leaves.
+// no sums, of those).  A forward product with g.sums says in *sum_rows how many rows of them it leaves.
 hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hipStream_t st, int* sum_rows = nullptr) {
     const size_t es = layer_esize(dtype);
     const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
     const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda * es % 16 == 0 && g.ldb * es % 16 == 0;
     g.splits = c.splits;
     g.ksplit = c.ksplit ? c.ksplit : g.k;
+    if (sum_rows && leaves_rows(c)) {
+        g.exact = g.sums;
+        g.sums = nullptr;
+        *sum_rows = g.m;
+    }
     return by_type(dtype, [&](auto t) -> hipError_t {
         using T = std::remove_pointer_t<decltype(t)>;
         if (c.tile == SKINNY) return launch_skinny<T>(g, aligned, st);
@@ -154,7 +161,7 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         const int64_t width = gated ? 2 * (int64_t)g.n : g.n;
         g.tiles_m = (g.m + rows - 1) / rows;
         g.tiles_n = g.out ? (int)((width + cols - 1) / cols) : 1;      // without: the sums of dz alone
-        if (sum_rows) *sum_rows = 2 * g.tiles_m;
+        if (g.sums && sum_rows) *sum_rows = 2 * g.tiles_m;
         GemmArgs p = g;
         if (g.splits > 1) {
             p.mode = GEMM_PARTIAL;
@@ -241,7 +248,7 @@ GradPlan grad_plan(const Layer& l, int act) {
     size_t most = 0;
     if (again) {
         // fp32 loses nothing on the way; there it is only that the large tiles' sums beside dW cost their workgroups a sixth
-        p.slopes = p.parts == 1 && p.z.tile >= 0 && p.z.splits == 1 && (es == 2 || p.w.tile >= 2);
+        p.slopes = es == 2 ? p.parts == 1 : !leaves_rows(p.z) && p.w.tile >= 2;
         p.dz = up256((size_t)p.parts * l.rows * whole_row(l, l.wide) * es);
         p.sums = p.slopes ? slope_sum_bytes(p.z, l) : 0;
         most = partial_bytes(p.z, l.rows, l.wide);

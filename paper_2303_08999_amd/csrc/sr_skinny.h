@@ -91,6 +91,7 @@ __global__ __launch_bounds__(SKW * 64) void k_skinny(const GemmArgs g) {
     }
     if (g.extra) extra.values(e[0]);
     gm_finish<GATED, 1>(g, z, u, e);
+    gm_put_exact<GATED>(g, fm, col, z[0], u[0]);
     T* const out = (T*)g.out + fm * g.ld_out + col;
     gm_put_parts(out, g.out_lo, g.n - col, z[0]);
     if (GATED && g.mode == GEMM_GATED_SLOPE) gm_put_parts(out + g.half, g.out_lo, g.n - col, u[0]);

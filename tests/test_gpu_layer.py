@@ -693,3 +693,32 @@ def test_the_smallest_fp32_values(shape):
         compare(name, got[:n], want, 14 * U * want.abs() + 2.0 ** -134 * other[:n].double())
         assert not got[n:].any()
     assert torch.equal(db[:n], small[:n]) and not db[n:].any()
+
+
+# products of which z's is split, and z of few rows
+@pytest.mark.parametrize("shape", [(64, 4096, 4096), (256, 4096, 4096), (512, 4096, 1024), (33, 4104, 8200), (250, 4099, 2052)], ids=str)
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["linear", "gated"])
+def test_bias_gradients_of_few_rows_are_summed_before_their_rounding(gated, t, shape):
+    """Where z's gradient is rounded once, the bias's gradient is the exact sum of what it was before, rounded: the error in norm of that rounding,
+    and a fifth for scatter."""
+    d = inputs(*shape, t, gated, 33)
+    assert 2 * shape[0] * shape[1] * d["w"].shape[0] > 2e9
+    e = wide64(d)
+    dz = (lo.gated_dz if gated else lo.linear_dz)(e["x"], e["w"], e["b"], lo.GELU, e["dy"])
+    want = dz.sum(0)
+    every = run_grad(d, t, lo.GELU, gated)
+    rounding = (want.to(DT[t]).double() - want).norm()
+    assert (every[2].double() - want).norm() <= 1.2 * rounding
+    for name, got, exact in zip(("dx", "dweight"), every, lo.behind_dz(e["x"], e["w"], dz)):
+        assert (got.double() - exact).norm() <= 1.7 * (exact.to(DT[t]).double() - exact).norm(), name
+    for ask in ((True, False, False), (False, True, False), (False, False, True)):
+        for a, b in zip(run_grad(d, t, lo.GELU, gated, want=ask), every):
+            assert a is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(64, 4096, 4096), (250, 4099, 2052)], ids=str)
+def test_the_workspace_of_few_rows_and_its_replays(shape):
+    for gated in (False, True):
+        test_a_workspace_of_the_size_asked_for_and_no_more(gated, "bf16", shape)
+    test_every_way_at_once_on_two_streams_and_replayed(shape)
