@@ -70,7 +70,10 @@ constexpr int64_t THIN_FROM = 4096;
 // of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  Each launch reads the
 // rows again (bfloat16, 131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427; fp32, 351576 rows of 64 to 1024 in two: 564 and 505).
 // fp32 of more than 64 features splits more values than it multiplies (351576 rows of 128 to 256: 200 us, tiles 196; 1048576: 530 and 581).
+// A residual, of which the plan knows nothing, can halve a launch's columns: up to as many launches as there may be without one (bfloat16, 131072 rows
+// of 256 to 2048: 460 us in eight, tiles 380; of 136 to 1024 206 in four, tiles 227; fp32, 1048576 rows of 64 to 512 1003 in two, tiles 1213).
 constexpr double ROWS_FROM = 26e6;
+constexpr int ROWS_LAUNCHES = 4;
 // A launch has less than 2^32 threads, 256 a tile: 2^31 rows of few columns need larger tiles than the smallest.
 constexpr int64_t LAUNCH_TILES = 1 << 24;
 // The cut that should take least.  Split sums cost a launch and their way, written and read in fp32, at 8 bytes a ps through the
@@ -105,7 +108,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     if (rows && layout != GEMM_RC_RC && best.splits == 1) {
         const RowsShape s = rows_shape(m, n, k, es, gated, slope);
         const double cols = gated ? 2.0 * s.cols : s.cols;
-        const int most = es == 2 ? slope ? 2 : 4 : gated && !slope ? 4 : 1;
+        const int most = es == 2 ? slope ? 2 : ROWS_LAUNCHES : gated && !slope ? ROWS_LAUNCHES : 1;
         const double from = ROWS_FROM * (k > cols ? (double)k / cols : 1.0) * (s.launches > 1 ? 2.0 : 1.0) * (es == 4 && k > 64 ? 4.0 : 1.0);
         best.rows = s.grid && s.launches <= most && (double)m * cols >= from;
     }
@@ -152,8 +155,10 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
         if (c.tile == THIN) return launch_thin<T>(g, layout, st);
         if (c.rows && (uintptr_t)g.a % 4 == 0 && g.lda * es % 4 == 0) {
             const RowsShape r = rows_shape(g.m, g.n, g.k, es, gated, g.extra);
-            if (sum_rows) *sum_rows = r.grid * r.wr;
-            if (r.grid) return launch_rows<T>(g, layout, st);
+            if (r.grid && r.launches <= ROWS_LAUNCHES) {
+                if (sum_rows) *sum_rows = r.grid * r.wr;
+                return launch_rows<T>(g, layout, st);
+            }
         }
         int tile = c.tile;
         if ((!aligned || g.a_lo || g.out_lo) && tile > 1) tile = 1;

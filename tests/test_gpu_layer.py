@@ -8,6 +8,7 @@ quotient and product one each: (1.75 |z| + 8) u relative; erf is within 4 u of 1
 z^2 / 2: (4 + 2 z^2 exp(-z^2 / 2)) u in all is below 8 u (|z| + 1).  One bound for all of them: a value is within u (1.75 |z| + 8) (|value| + |z| + 1), a
 slope the same with |slope| + 1.  Slopes are below 1.13, second derivatives below 0.8: z's own error counts that much.  A rounding to type t is off by
 eps_t / 2 of the value, or half of t's smallest step."""
+import ctypes
 import math
 
 import pytest
@@ -722,3 +723,29 @@ def test_the_workspace_of_few_rows_and_its_replays(shape):
     for gated in (False, True):
         test_a_workspace_of_the_size_asked_for_and_no_more(gated, "bf16", shape)
     test_every_way_at_once_on_two_streams_and_replayed(shape)
+
+
+def launches(call):
+    """How many kernels a call is made of: the nodes of its graph."""
+    hip = ctypes.CDLL("libamdhip64.so")
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    count = ctypes.c_size_t()
+    assert hip.hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(count)) == 0
+    return count.value
+
+
+def test_a_residual_does_not_multiply_the_launches():
+    """The kernel that holds the weight reads the rows again in each launch: there are four at most, with a residual as well."""
+    shape = (104000, 256, 2048)
+    for t in ("f16", "bf16"):
+        for residual in (False, True):
+            d = inputs(*shape, t, False, 19, residual=residual)
+            y = torch.empty(shape[0], shape[2], device=DEV, dtype=DT[t])
+            assert 1 <= launches(lambda: sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.GELU, d["res"], y)) <= 4
+            rows = torch.arange(0, shape[0], 37, device=DEV)
+            some = {k: v if v is None or v.shape[0] != shape[0] else v[rows] for k, v in d.items()}
+            compare("y", y[rows], *forward_bound(t, wide64(some), lo.GELU, False))
