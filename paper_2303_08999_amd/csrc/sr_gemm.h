@@ -72,16 +72,16 @@ template <typename T> hipError_t launch_pack(const void* from, int64_t rows, int
 // Few rows: one pass over the weights (layout KC_KC, every mode but PARTIAL)
 template <typename T> hipError_t launch_skinny(const GemmArgs& g, bool aligned, hipStream_t st);
 constexpr int SKINNY_ROWS = 64;
-// Many rows, a small weight (layouts KC_KC and KC_RC, every mode but PARTIAL; the output's rows without gaps): what a launch is made of, waves = 0 if
-// the case is none for it.  rows: that a wavefront takes at a time; group: tiles of 16 columns (of each half) that are made at a time; np: columns of a
+// Many rows, a small weight (layouts KC_KC and KC_RC, modes STORE and GATED; rows of the output and of what is added without gaps): what a launch is made of, waves = 0 if
+// the case is none for it.  outputs: that a wavefront is to have room for, of 1 that it takes.  rows: that a wavefront takes at a time; group: tiles of 16 columns (of each half) that are made at a time; np: columns of a
 // half in LDS; steps: of 64 bytes of k.  With fewer than 12 wavefronts on a compute unit the rows' way through memory is not hidden (500 000 rows of
 // 128 to 128, bfloat16, 6 wavefronts: 70 us, the tile kernel 47).
 struct ThinShape { int np, steps, waves, group, rows; };
-inline ThinShape thin_shape(int64_t n, int64_t k, size_t es, bool gated, bool both) {
+inline ThinShape thin_shape(int64_t n, int64_t k, size_t es, bool gated, int outputs = 1) {
     const int64_t group = n <= 16 ? 1 : 2, np = (n + 16 * group - 1) / (16 * group) * (16 * group), steps = (k * (int64_t)es + 63) / 64;
     if (steps < 1 || steps > 4 || n > 512) return {0, 0, 0, 0, 0};
     for (int rows = 32; rows >= 16; rows /= 2) {
-        const int64_t patch = (rows * (both ? 2 * n : n) * (int64_t)es + 15) / 16 * 16;
+        const int64_t patch = (rows * outputs * n * (int64_t)es + 15) / 16 * 16;
         const int64_t bytes = np * (gated ? 2 : 1) * (steps * 64 + 20) + 4 * patch;
         if (bytes <= 65536 && 163840 / bytes >= 3) return {(int)np, (int)steps, 4, (int)group, rows};
     }
@@ -430,16 +430,20 @@ template <typename T> __device__ __forceinline__ void gm_put_parts(T* p, int64_t
 // What a layer does to 8 U values of z, outputs in its place; e: of `extra`.  For the gated forms u is the same columns of the second half, and
 // becomes the second output.
 template <bool GATED, int U>
+__device__ __forceinline__ void gm_forward(int act, float (&z)[U][8], const float (&u)[U][8], const float (&e)[U][8]) {
+    act8<U>(act, z);
+#pragma unroll
+    for (int r = 0; r < U; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (GATED) z[r][i] *= u[r][i];
+            else z[r][i] += e[r][i];
+        }
+}
+template <bool GATED, int U>
 __device__ __forceinline__ void gm_finish(const GemmArgs& g, float (&z)[U][8], float (&u)[U][8], const float (&e)[U][8]) {
     if (g.mode == (GATED ? GEMM_GATED : GEMM_STORE)) {
-        act8<U>(g.act, z);
-#pragma unroll
-        for (int r = 0; r < U; ++r)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (GATED) z[r][i] *= u[r][i];
-                else z[r][i] += e[r][i];
-            }
+        gm_forward<GATED, U>(g.act, z, u, e);
     } else {
         float value[U][8];
         slope8<U>(g.act, z, value);

@@ -82,7 +82,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0, false};
     if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
-        const ThinShape s = thin_shape(n, k, es, gated, gated);
+        const ThinShape s = thin_shape(n, k, es, gated, gated ? 2 : 1);
         if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0, 0.0, false};
     }
     const int64_t nn = gated ? 2 * n : n;

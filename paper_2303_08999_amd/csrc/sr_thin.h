@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     float* const bias = (float*)(lds + (size_t)np * H * SB);
-    const int width = g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n;
+    const int width = g.n;
     const int patch_bytes = (THIN_ROWS * width * (int)sizeof(T) + 15) / 16 * 16;
     T* const patch = (T*)(lds + (size_t)np * H * (SB + 4) + wave * patch_bytes);
 
@@ -121,8 +121,7 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
 #pragma unroll
             for (int s = 0; s < KS; ++s) v[f][s] = gm_cut<T>(v[f][s], g.k - (s * 4 + q) * E);
     };
-    // What is added or multiplied comes as the piece that the output leaves as, and through the same place in LDS, where its rows are as long.
-    const bool linear = g.extra && g.ld_extra == width;
+    // What is added comes as the piece that the output leaves as, and through the same place in LDS.
     int block = blockIdx.x * waves + wave;
     if (block < blocks) load(block, next);
     for (; block < blocks; block += step) {
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
         cut(now);
         if (block + step < blocks) load(block + step, next);
         const int row0 = block * THIN_ROWS, rows = g.m - row0 < THIN_ROWS ? g.m - row0 : THIN_ROWS, count = rows * width;
-        if (linear) {
+        if (g.extra) {
             const T* const in = (const T*)g.extra + (int64_t)row0 * width;
             for (int i = lane * E; i < count; i += 4 * 64 * E) {
                 u32x4g v[4];
@@ -146,7 +145,7 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
             __builtin_amdgcn_wave_barrier();
         }
         for (int n0 = 0; n0 < g.n; n0 += NG * 16) {
-            // [NG][RF][4 columns] as rows of 8; what is added or multiplied is on its way while the products are made
+            // [NG][RF][4 columns] as rows of 8
             float z[U][8], u[U][8], e[U][8];
             if constexpr (NG * RF == 1) {
 #pragma unroll
@@ -158,10 +157,8 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
                 for (int f = 0; f < RF; ++f) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) e[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = 0.0f;
-                    const int n = n0 + j * 16 + q * 4, m = row0 + f * 16 + r;
-                    if (linear) {
-                        if (n < g.n) thin_get4(patch + (f * 16 + r) * width + n, g.n - n, e[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
-                    } else if (g.extra && m < g.m) thin_get4((const T*)g.extra + (int64_t)m * g.ld_extra + n, g.n - n, e[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
+                    const int n = n0 + j * 16 + q * 4;
+                    if (g.extra && n < g.n) thin_get4(patch + (f * 16 + r) * width + n, g.n - n, e[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
                 }
             f32x4g acc[H][NG][RF];
 #pragma unroll
@@ -189,7 +186,7 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
                         z[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = acc[0][j][f][i];
                         if constexpr (GATED) u[(j * RF + f) / 2][(j * RF + f) % 2 * 4 + i] = acc[H - 1][j][f][i];
                     }
-            gm_finish<GATED, U>(g, z, u, e);
+            gm_forward<GATED, U>(g.act, z, u, e);
 #pragma unroll
             for (int j = 0; j < NG; ++j)
 #pragma unroll
@@ -197,7 +194,6 @@ __global__ __launch_bounds__(256, (thin_waves<KS, GATED>)) void k_thin(const Gem
                     const int n = n0 + j * 16 + q * 4;
                     T* const p = patch + (f * 16 + r) * width + n;
                     thin_put4<T, FOURS>(p, g.n - n, z[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
-                    if (GATED && g.mode == GEMM_GATED_SLOPE) thin_put4<T, FOURS>(p + g.n, g.n - n, u[(j * RF + f) / 2] + (j * RF + f) % 2 * 4);
                 }
         }
         __builtin_amdgcn_wave_barrier();
@@ -230,10 +226,10 @@ hipError_t start_thin(const GemmArgs& g, bool rc, int np, int waves, size_t lds,
 
 template <typename T>
 hipError_t launch_thin(const GemmArgs& g, int layout, hipStream_t st) {
-    const bool gated = g.mode == GEMM_GATED || g.mode == GEMM_GATED_SLOPE;
-    const ThinShape s = thin_shape(g.n, g.k, sizeof(T), gated, g.mode == GEMM_GATED_SLOPE);
-    if (!s.waves) return hipErrorInvalidValue;
-    const size_t lds = thin_lds<T>(s.np, gated ? 2 : 1, s.steps, g.mode == GEMM_GATED_SLOPE ? 2 * g.n : g.n, s.waves, s.rows);
+    const bool gated = g.mode == GEMM_GATED;
+    const ThinShape s = thin_shape(g.n, g.k, sizeof(T), gated);
+    if (!s.waves || !(gated || g.mode == GEMM_STORE)) return hipErrorInvalidValue;
+    const size_t lds = thin_lds<T>(s.np, gated ? 2 : 1, s.steps, g.n, s.waves, s.rows);
     const bool rc = layout == GEMM_KC_RC;
     auto go = [&](auto ks) {
         constexpr int KS = decltype(ks)::value;
