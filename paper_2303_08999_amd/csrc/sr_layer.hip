@@ -66,6 +66,12 @@ double tile_time(int tile, int64_t c, int64_t steps, size_t es) {
 // From here on rows with a weight that fits go to the kernel for them; where that takes 16 at a time (500 000 of 128 to 128, bfloat16: 58 us, tiles 47), only
 // if the rows are no 16-byte pieces, which the tile kernels read by way of registers (351 576 of 27 to 121, fp32: 55 us, tiles 65).
 constexpr int64_t THIN_FROM = 4096;
+// A gated block goes there where LDS has room for its output, or, if its products take longer than its rows' way (rows of more than 192 bytes, fp32 64) or its
+// output's rows meet in the same banks of LDS (16 bits, multiples of 256 bytes), for twice that: bfloat16, 400 000 rows of 32 to 120 30 us, by other kernels 38, of 64
+// to 72 23 and 38; but of 32 to 128 57 and 35, 12 000 of 128 to 64 8.5 and 7.2; fp32, 400 000 of 16 to 64 33 and 41, but of 32 to 64 48 and 41.
+int thin_room(int64_t n, int64_t k, size_t es, bool gated) {
+    return gated && (k * (int64_t)es > (es == 2 ? 192 : 64) || (es == 2 && n * (int64_t)es % 256 == 0)) ? 2 : 1;
+}
 // From so many outputs on (of a launch; more where there is more to read, or several) the kernel that holds the weight is worth its start (bfloat16, 65536 rows
 // of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  Each launch reads the
 // rows again (bfloat16, 131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427; fp32, 351576 rows of 64 to 1024 in two: 564 and 505).
@@ -82,7 +88,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k, size_t es, int layout, bool gated, b
     const int64_t bk = 128 / (int64_t)es, steps = (k + bk - 1) / bk;
     if (layout == GEMM_KC_KC && m <= SKINNY_ROWS) return {SKINNY, 1, 0, 0.0, false};
     if (thin && layout != GEMM_RC_RC && m >= THIN_FROM) {
-        const ThinShape s = thin_shape(n, k, es, gated, gated ? 2 : 1);
+        const ThinShape s = thin_shape(n, k, es, gated, thin_room(n, k, es, gated));
         if (s.waves && (s.rows == 32 || k * (int64_t)es % 16)) return {THIN, 1, 0, 0.0, false};
     }
     const int64_t nn = gated ? 2 * n : n;

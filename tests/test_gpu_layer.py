@@ -725,8 +725,13 @@ def test_the_workspace_of_few_rows_and_its_replays(shape):
     test_every_way_at_once_on_two_streams_and_replayed(shape)
 
 
+class KernelNode(ctypes.Structure):
+    _fields_ = [("block", ctypes.c_uint * 3), ("extra", ctypes.c_void_p), ("func", ctypes.c_void_p), ("grid", ctypes.c_uint * 3), ("args", ctypes.c_void_p),
+                ("shared", ctypes.c_uint)]
+
+
 def launches(call):
-    """How many kernels a call is made of: the nodes of its graph."""
+    """The kernels that a call is made of: the nodes of its graph, as it launches them."""
     hip = ctypes.CDLL("libamdhip64.so")
     call()
     torch.cuda.synchronize()
@@ -735,7 +740,11 @@ def launches(call):
         call()
     count = ctypes.c_size_t()
     assert hip.hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(count)) == 0
-    return count.value
+    nodes, kernels = (ctypes.c_void_p * count.value)(), (KernelNode * count.value)()
+    assert hip.hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), nodes, ctypes.byref(count)) == 0
+    for node, kernel in zip(nodes, kernels):
+        assert hip.hipGraphKernelNodeGetParams(ctypes.c_void_p(node), ctypes.byref(kernel)) == 0
+    return list(kernels)
 
 
 def test_a_residual_does_not_multiply_the_launches():
@@ -745,7 +754,20 @@ def test_a_residual_does_not_multiply_the_launches():
         for residual in (False, True):
             d = inputs(*shape, t, False, 19, residual=residual)
             y = torch.empty(shape[0], shape[2], device=DEV, dtype=DT[t])
-            assert 1 <= launches(lambda: sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.GELU, d["res"], y)) <= 4
+            assert 1 <= len(launches(lambda: sr.sr_layer_linear(d["x"], d["w"], d["b"], lo.GELU, d["res"], y))) <= 4
             rows = torch.arange(0, shape[0], 37, device=DEV)
             some = {k: v if v is None or v.shape[0] != shape[0] else v[rows] for k, v in d.items()}
             compare("y", y[rows], *forward_bound(t, wide64(some), lo.GELU, False))
+
+
+@pytest.mark.parametrize("C,O,t,small", [(64, 72, "bf16", True), (48, 96, "f16", True), (32, 120, "bf16", True), (96, 64, "f16", True), (16, 64, "f32", True), (12, 48, "f32", True), (64, 64, "bf16", True),
+                                         (32, 128, "bf16", False), (128, 64, "f16", False), (48, 48, "f32", False), (64, 200, "bf16", False)], ids=str)
+def test_gated_blocks_of_many_rows_go_to_the_kernel_for_a_small_weight(C, O, t, small):
+    """... where its LDS has room for the weight and one output: what is asked for is what is launched.  It is the only one of a forward call
+    whose LDS is given at the launch."""
+    for P in (4100, 20011):
+        d = inputs(P, C, O, t, True, 23)
+        y = torch.empty(P, O, device=DEV, dtype=DT[t])
+        kernels = launches(lambda: sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.SILU, y))
+        assert all((k.shared > 0) == small for k in kernels) and (len(kernels) == 1 or not small)
+        check_forward(P, C, O, t, lo.SILU, True, shift=P % 2)
