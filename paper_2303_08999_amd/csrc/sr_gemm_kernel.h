@@ -79,13 +79,14 @@ struct Operand {
     static __device__ __forceinline__ bool other(int i, int wave) { return GATED && ((i * NW + wave) * 8 / MT & 1); }
     __device__ __forceinline__ const char* from(int i, int wave) const { return GATED && other(i, wave) ? base + second : base; }
     // Straight to LDS; the whole of it is there.  Written out, because the compiler lets every turning LDS read wait for all loads to LDS that it
-    // knows of, whatever they write: landed() is what waits for these.  The instruction takes the place from m0, a wait state behind
-    // its writing; the scalar move is that state, and what makes the base one that no vector instruction has just written (five states, which the compiler counts for
-    // its own instructions only; as s_nop: 16384 rows of 4096 to 4096, bfloat16, gelu and residual, 450 us, so 438).
+    // knows of, whatever they write: landed() is what waits for these.  The instruction takes the place from m0, a wait state behind its writing; the move of the base
+    // is that state.  Both moves are scalar and in here, so that no vector instruction has just written what the load reads (it would need five states, which
+    // the compiler counts for its own instructions only).
     __device__ __forceinline__ void fetch(char* lds, int wave, int i) const {
         uint64_t at;
-        asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0"
-                     : "=&s"(at) : "v"(off[i]), "s"(from(i, wave)), "{m0}"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024)) : "memory");
+        unsigned m0;
+        asm volatile("s_mov_b32 %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
+                     : "=&s"(at), "=&{m0}"(m0) : "v"(off[i]), "s"(from(i, wave)), "s"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024)) : "memory");
     }
     __device__ __forceinline__ void fetch(char* lds, int wave) const {
 #pragma unroll
@@ -111,8 +112,9 @@ struct Operand {
                     at = ((unsigned)k * (unsigned)ld + (unsigned)(r < last ? r : last)) * 4;
                 }
                 uint64_t base_at;
-                asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0"
-                             : "=&s"(base_at) : "v"(at), "s"(uniform), "{m0}"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024 + j * 256)) : "memory");
+                unsigned m0;
+                asm volatile("s_mov_b32 %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0"
+                             : "=&s"(base_at), "=&{m0}"(m0) : "v"(at), "s"(uniform), "s"((unsigned)(uintptr_t)(lds_void)(lds + (i * NW + wave) * 1024 + j * 256)) : "memory");
             }
         }
     }

@@ -82,7 +82,8 @@ __global__ __launch_bounds__(512, 2) void k_rows(const GemmArgs g, const int wn,
                 if (p >= pieces) p = pieces - 1;
                 const unsigned off = (unsigned)(row < last ? row : last) * (unsigned)(g.lda * (int)sizeof(T)) + p * 16;
                 uint64_t at;
-                asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(at) : "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 1024)) : "memory");
+                unsigned m0;
+                asm volatile("s_mov_b32 %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(at), "=&{m0}"(m0) : "v"(off), "s"(from), "s"((unsigned)(uintptr_t)(lds_void_r)(to + i * 1024)) : "memory");
             }
         } else {
             const int fours = (g.k * (int)sizeof(T) + 3) / 4;
@@ -92,7 +93,8 @@ __global__ __launch_bounds__(512, 2) void k_rows(const GemmArgs g, const int wn,
                 if (p >= fours) p = fours - 1;
                 const unsigned off = (unsigned)(row < last ? row : last) * (unsigned)(g.lda * (int)sizeof(T)) + p * 4;
                 uint64_t at;
-                asm volatile("s_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0" : "=&s"(at) : "v"(off), "s"(from), "{m0}"((unsigned)(uintptr_t)(lds_void_r)(to + i * 256)) : "memory");
+                unsigned m0;
+                asm volatile("s_mov_b32 %1, %4\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dword %2, %0" : "=&s"(at), "=&{m0}"(m0) : "v"(off), "s"(from), "s"((unsigned)(uintptr_t)(lds_void_r)(to + i * 256)) : "memory");
             }
         }
     };

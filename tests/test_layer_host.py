@@ -1,6 +1,7 @@
 """Refusals of the layers, their gradients and the clipping: every check runs on the host, nothing is launched."""
 import ctypes
 import os
+import re
 
 import pytest
 import torch
@@ -270,3 +271,17 @@ def test_lists_of_tensors_beyond_32_bits_are_described_whole():
     assert fields(torch.empty(3, 0)) == [(None, sr.SR_F32, 1, 1, 3, 0)]
     for data, dtype, n, c, h, w in fields(torch.empty((0, 1 << 32))):
         assert data is None and n * c * h * w == 0
+
+
+def test_loads_to_lds_in_assembly_read_what_scalar_moves_have_just_written():
+    """A load to LDS takes its base and m0 at once; a vector instruction that wrote one of them would have to be five wait states before it, which nothing counts
+    for assembly.  So each of these loads moves both by itself, and the base last: m0 is one wait state away then."""
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    found = 0
+    for name in sorted(os.listdir(csrc)):
+        with open(os.path.join(csrc, name)) as f:
+            for text, outs in re.findall(r'asm volatile\s*\(\s*"([^"]*global_load_lds[^"]*)"\s*:([^:]*):', f.read()):
+                assert re.fullmatch(r"s_mov_b32 %1, %4\\n\\ts_mov_b64 %0, %3\\n\\tglobal_load_lds_dword(x4)? %2, %0", text), (name, text)
+                assert re.fullmatch(r'\s*"=&s"\(\w+\), "=&\{m0\}"\(\w+\)\s*', outs), (name, outs)
+                found += 1
+    assert found == 4
