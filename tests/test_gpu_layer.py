@@ -771,3 +771,44 @@ def test_gated_blocks_of_many_rows_go_to_the_kernel_for_a_small_weight(C, O, t, 
         kernels = launches(lambda: sr.sr_layer_gated(d["x"], d["w"], d["b"], lo.SILU, y))
         assert all((k.shared > 0) == small for k in kernels) and (len(kernels) == 1 or not small)
         check_forward(P, C, O, t, lo.SILU, True, shift=P % 2)
+
+
+def tail_bounds(z):
+    """gelu and its slope as the kernels' formula has them, in 64 bits, and what fp32 may be off of that.  erfc(x) = P(t) exp(-x^2), t = 1 / (1 + p x),
+    x = |z| / sqrt 2, P = a1 t + ... + a5 t^5 by Abramowitz and Stegun 7.1.26.  t: the constant, the sum and two for the reciprocal, 4 u; P: each of five
+    steps rounds once, the constants and t's error to the fifth power come in, 5 + 1 + 20 = 26 u of the sum of magnitudes S.  exp: its argument is rounded three times, 3 u of
+    z^2 / 2, the instruction 2 u.  Products with it and z three more.  Where z > 0, 1 - P rounds once more."""
+    a = (0.254829592, -0.284496736, 1.421413741, -1.453152027, 1.061405429)
+    t, d = 1 / (1 + 0.3275911 * math.sqrt(0.5) * z.abs()), torch.exp(-z * z / 2)
+    P = sum(c * t ** (i + 1) for i, c in enumerate(a))
+    S = sum(abs(c) * t ** (i + 1) for i, c in enumerate(a))
+    q = P * d / 2
+    cdf = torch.where(z < 0, q, 1 - q)
+    e = S * d / 2 * (26 + 1.5 * z * z + 4) * U + torch.where(z < 0, torch.zeros_like(z), 2 * U * cdf)
+    bell = z.abs() * d / math.sqrt(2 * math.pi)
+    slope = cdf + torch.sign(z) * bell
+    return (z * cdf, z.abs() * e + U * (z * cdf).abs()), (slope, e + bell * (1.5 * z * z + 6) * U + 2 * U * slope.abs())
+
+
+@pytest.mark.parametrize("P", [37, 2000, 5000], ids=["few rows", "tiles", "small weight"])
+def test_activations_in_their_tails(P):
+    """By themselves, z being a feature times one: gelu as its formula, and that within 0.75e-7 |z|; silu and sigmoid within (1.75 |z| + 8) u of themselves."""
+    C = O = 8
+    z = torch.linspace(-12, 12, P * C, device=DEV).view(P, C)
+    w, y, dx = torch.eye(C, device=DEV), torch.empty(P, C, device=DEV), torch.empty(P, C, device=DEV)
+    v = z.double()
+    (want, bound), (want_slope, slope_bound) = tail_bounds(v)
+    assert ((want - lo.act(lo.GELU, v)).abs() <= 0.75e-7 * v.abs()).all()
+    sr.sr_layer_linear(z, w, None, lo.GELU, None, y)
+    compare("gelu", y, want, bound)
+    sr.sr_layer_linear_grad(z, w, None, lo.GELU, torch.ones_like(z), dx, None, None)
+    compare("slope", dx, want_slope, slope_bound)
+    for name, wrong in {"nothing": torch.zeros_like(want), "1 + erf in fp32": z.double() * 0.5 * (1 + torch.erf(z * math.sqrt(0.5))).double(), "half of it": want / 2}.items():
+        tail = (v < -4) & (v > -6)
+        assert ((wrong - y.double()).abs() > bound)[tail].any(), name
+    z = z * 6
+    v = z.double()
+    for kind in (lo.SILU, lo.SIGMOID):
+        sr.sr_layer_linear(z, w, None, kind, None, y)
+        want = lo.act(kind, v)
+        compare("silu or sigmoid", y, want, U * (1.75 * v.abs() + 8) * want.abs() + 2.0 ** -126)
