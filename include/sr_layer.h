@@ -123,17 +123,17 @@ size_t sr_grad_clip_workspace_bytes(int tensors);
  *     norm = sqrt(sum over all elements of g^2)    factor = max_norm / norm if norm is finite and above max_norm, else 1
  *     out = factor g
  *
- *   grads     HOST array of `tensors` descriptors, any sizes (none too), each f32, f16 or bf16; the same tensor
- *             twice counts twice
+ *   grads     HOST array of `tensors` descriptors, any sizes (none too; 2^40 elements at most), each f32, f16 or bf16; the same tensor
+ *             twice counts twice.  Where no axes hold its elements (more than 2^31 - 1 in one), a tensor is described as several
  *   outs      HOST array of as many, each with its gradient's type and sizes; a gradient's own memory (in place) or
  *             memory that no gradient and no other output overlaps; or NULL: the norm alone
  *   max_norm  not negative; infinity: nothing is scaled
  *   norm      DEVICE, 2 floats, written: norm, factor
  *   workspace, workspace_bytes   DEVICE scratch, 16-byte aligned
  *
- * The squares are summed so that no finite gradients overflow or vanish (the norm itself may be beyond fp32: infinity then).  A norm that is
- * not finite says that the gradients hold infinities or NaN: they are left as they are, so that a program may skip its
- * step.  1 <= tensors <= SR_MAX_GRADS.  Both arrays are read before the call returns.
+ * The squares are summed so that no finite gradients overflow or vanish.  A norm that is finite but beyond fp32 is written as infinity, with the factor
+ * that it has.  Gradients that hold infinities or NaN are left as they are, with a norm that is not finite and a factor of 1, so that a program
+ * may skip its step.  1 <= tensors <= SR_MAX_GRADS.  Both arrays are read before the call returns.
  */
 int sr_grad_clip(const sr_tensor* grads, const sr_tensor* outs, int tensors, double max_norm, float* norm,
                  void* workspace, size_t workspace_bytes, void* stream);

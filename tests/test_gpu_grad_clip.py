@@ -208,3 +208,16 @@ def test_a_tensor_of_more_elements_than_32_bits_count(shape, t):
     if len(shape) == 1 and n % (1 << 30):
         with pytest.raises(ValueError, match="another size"):
             sr.sr_grad_clip(grads, [flat[:1 << 30], small], 1.0, stats)
+
+
+@pytest.mark.parametrize("most", [1.0, 1e30, 1e38, 2e39])
+def test_a_norm_beyond_fp32(most):
+    """Written as infinity; the factor is that of the norm itself, in fp32, whose smallest step 2^-149 it has where it is subnormal."""
+    g = [torch.full((100,), 3e38, device=DEV), torch.full((7,), -1e38, device=DEV, dtype=torch.bfloat16)]
+    outs, stats = [torch.empty_like(v) for v in g], torch.empty(2, device=DEV)
+    want, norm, factor = lo.clip([v.double() for v in g], most)
+    assert norm > torch.finfo(torch.float32).max and factor < 1
+    sr.sr_grad_clip(g, outs, most, stats)
+    assert float(stats[0]) == math.inf and abs(float(stats[1]) - factor) <= 2 * U * factor + 2.0 ** -150
+    for v, o, w, eps in zip(g, outs, want, (U, 2.0 ** -8)):
+        assert ((o.double() - w).abs() <= (3 * U + eps) * w.abs() + 2.0 ** -150 * v.double().abs()).all()
