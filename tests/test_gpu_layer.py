@@ -812,3 +812,26 @@ def test_activations_in_their_tails(P):
         sr.sr_layer_linear(z, w, None, kind, None, y)
         want = lo.act(kind, v)
         compare("silu or sigmoid", y, want, U * (1.75 * v.abs() + 8) * want.abs() + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("shape", [(40, 4096, 256), (300, 4096, 264), (2048, 4096, 2048), (4096, 1024, 4096), (3000, 2045, 1030), (8200, 2047, 2049), (66000, 64, 72), (131080, 64, 264), (131080, 100, 264)],
+                         ids=str)
+@pytest.mark.parametrize("one_sign", [True, False], ids=["one_sign", "both"])
+def test_errors_of_fp32_in_norm(shape, one_sign):
+    """A product of K terms is at most n = K / 2 sums one after the other (two products a fp32 instruction; six parts of 16 an instruction are fewer), the i-th of them i / n of
+    the whole where all have one sign.  Roundings to nearest add up like sqrt(n / 3) of them at most, each below u; in norm that is below u sqrt(K / 2), with the result's own
+    rounding, u, beside it.  Sums that were cut off would be off by n / 2 steps of 2 u / 2 each: 1024 u for 45 at K = 4096.  Operands of both signs make smaller partial
+    sums of a smaller whole, and stay below that as well.  dbias: one more sum a row, K of them."""
+    P, C, O = shape
+    g = torch.Generator(device=DEV).manual_seed(41)
+    make = lambda *s: torch.rand(s, generator=g, device=DEV) if one_sign else torch.randn(s, generator=g, device=DEV)
+    x, w, dy, y = make(P, C), make(O, C), make(P, O), torch.empty(P, O, device=DEV)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(O, device=DEV)
+    sr.sr_layer_linear(x, w, None, lo.NONE, None, y)
+    sr.sr_layer_linear_grad(x, w, None, lo.NONE, dy, dx, dw, db)
+    exact = lo.behind_dz(x.double(), w.double(), dy.double())
+    for name, got, want, n in zip(("y", "dx", "dweight", "dbias"), (y, dx, dw, db), (lo.affine(x.double(), w.double(), None), *exact), (C / 2, O / 2, P / 2, P)):
+        off = got.double() - want
+        assert off.norm() <= U * (math.sqrt(n) + 1) * want.norm(), name
+        if one_sign:
+            assert abs(float((off / want).mean())) <= U * (math.sqrt(n) + 1) / 4, (name, "the same way everywhere")
