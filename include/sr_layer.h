@@ -11,19 +11,22 @@
  *     linear   z = x W^T + b                     y = act(z) + residual
  *     gated    g = x Wg^T + bg, u = x Wu^T + bu  y = act(g) u         (W = Wg on top of Wu, b = bg, bu)
  *
- * All tensors of a call have one type, f32, f16 or bf16.  Products are summed in fp32 or better; those of
- * 16-bit values are exact, those of f32 values are within 2^-24 of themselves (large calls hold an f32 value below 2^-110 to 2^-134, as
- * three bfloat16 numbers).  Bias, activation and the rest are fp32; each output is rounded once.  Silu and sigmoid are within (1.75 |z| + 8) 2^-24
- * of themselves, gelu within 0.75e-7 |z| (Abramowitz and Stegun 7.1.26), which in its tail shrinks with it: 5e-5 of its value at z = -3, 2e-3 at -5, 3e-2 at
- * -8.  z's gradient, where an activation or a gate makes it, is an operand of two more
- * products: f16 and bf16 calls of up to 2e9 operations a product (2 rows x in x rows of the weight) hold it in two numbers of
- * their type, to 2^-17 of itself or better (f16: or 2^-25), larger ones round it once, as the next layer of a training step does
- * with what it is given; the bias's gradient is summed before that where it is rounded once.  An f16 gradient of z beyond 65504 is an infinity on that
- * way.  Infinities and NaN in the inputs stay in the rows and columns to which the formulas take them; what an infinity makes
- * there may be NaN.
+ * All tensors of a call have one type, f32, f16 or bf16.  Products are summed in fp32 or better; those of 16-bit values
+ * are exact, those of f32 values are within 2^-24 of themselves (large calls hold an f32 value below 2^-110 to 2^-134, as
+ * three bfloat16 numbers).  Bias, activation and the rest are fp32; each output is rounded once.  Silu and sigmoid are within
+ * (1.75 |z| + 8) 2^-24 of themselves, gelu within 0.75e-7 |z| (Abramowitz and Stegun 7.1.26), in its tail 5e-5 of its value at
+ * z = -3, 2e-3 at -5, 3e-2 at -8.
  *
- * All rules of sr_dict.h hold: contiguous device memory of the caller at any address aligned to its elements,
- * every check on the host before anything is launched, its statuses, no allocation, no synchronisation, work
+ * z's gradient, where an activation or a gate makes it, is an operand of two more products: f16 and bf16 calls of up to
+ * 2e9 operations a product (2 rows x in x rows of the weight) hold it in two numbers of their type, to 2^-17 of itself or better
+ * (f16: or 2^-25), larger ones round it once, as the next layer of a training step does with what it is given; the
+ * bias's gradient is summed before that where it is rounded once.  An f16 gradient of z beyond 65504 is an infinity on that
+ * way.  Infinities and NaN in the inputs stay in the rows and columns to which the formulas take them; what an infinity
+ * makes there may be NaN.
+ *
+ * All rules of sr_dict.h hold: contiguous device memory of the caller at any address aligned to its elements (off 16-byte
+ * boundaries large layers of 16 bits take some twice as long), every check on the host before anything is launched, its
+ * statuses, no allocation, no synchronisation, work
  * enqueued on `stream` of the current device.  Outputs and workspace must not overlap inputs or one
  * another (but see sr_grad_clip).  The result of a call does not change from run to run: every sum has a
  * fixed order.  Calls that are in flight together need workspaces of their own (so do captured graphs

@@ -73,9 +73,10 @@ int thin_room(int64_t n, int64_t k, size_t es, bool gated) {
     return gated && (k * (int64_t)es > (es == 2 ? 192 : 64) || (es == 2 && n * (int64_t)es % 256 == 0)) ? 2 : 1;
 }
 // From so many outputs on (of a launch; more where there is more to read, or several) the kernel that holds the weight is worth its start (bfloat16, 65536 rows
-// of 64 to 512: 20 us, tiles 23, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 232 and 413, of 136 to 200 200 and 360).  Each launch reads the
+// of 64 to 512: 21 us, tiles 25, of 256 to 256 26 and 22; 1048576 rows of 64 to 512: 231 and 415, of 136 to 200 202 and 360).  Each launch reads the
 // rows again (bfloat16, 131072 rows of 256 to 1024 in four launches, gradient: 446 us, tiles 427; fp32, 351576 rows of 64 to 1024 in two: 564 and 505).
-// fp32 of more than 64 features splits more values than it multiplies (351576 rows of 128 to 256: 200 us, tiles 196; 1048576: 530 and 581).
+// fp32 of more than 64 features splits more values than it multiplies (351576 rows of 128 to 256: 200 us, tiles 196; 1048576: 530 and 581; all fp32 figures here are some 4 %
+// more on both sides since h is kept finite).
 // A residual, of which the plan knows nothing, can halve a launch's columns: up to as many launches as there may be without one (bfloat16, 131072 rows
 // of 256 to 2048: 460 us in eight, tiles 380; of 136 to 1024 206 in four, tiles 227; fp32, 1048576 rows of 64 to 512 1003 in two, tiles 1213).
 constexpr double ROWS_FROM = 26e6;
@@ -192,13 +193,13 @@ hipError_t product(GemmArgs g, const Cut& c, int dtype, int layout, void* ws, hi
 }
 
 // Rows on 16-byte pieces: dz, and copies of tensors that are not, where the products gain more than the copies take.  16-bit types: the tile kernels read other rows by way
-// of registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1106 us, so 527).  fp32 goes to LDS by 4 bytes (500 rows of 333 to 555: 16
+// of registers and take 2.2 times as long (gradient of 16207 rows of 1754 to 1183, gated, fp16: 1087 us, so 508).  fp32 goes to LDS by 4 bytes (500 rows of 333 to 555: 16
 // us, by registers 21); copies have the larger tiles to gain.
 int64_t whole_row(const Layer& l, int64_t cols) { const int64_t e = 16 / (int64_t)layer_esize(l.dtype); return (cols + e - 1) / e * e; }
 bool whole(const Layer& l, int64_t cols) { return whole_row(l, cols) == cols; }
 size_t copy_bytes(const Layer& l, int64_t rows, int64_t cols) { return up256((size_t)rows * whole_row(l, cols) * layer_esize(l.dtype)); }
 constexpr int TILES_OFF_PIECES = 2;
-constexpr double OFF_PIECES = 1.1;          // what these take there, of what tile_time says (8192 rows of 4095 to 4097, fp32: 1828 us, with copies 1722)
+constexpr double OFF_PIECES = 1.1;          // what these take there, of what tile_time says (8192 rows of 4095 to 4097, fp32: 1817 us, with copies 1713)
 bool copies_pay(double gain, size_t bytes, int copies) { return gain > 4.0 * copies + 2.0 * (double)bytes / 4.5e6; }
 hipError_t copy_rows(const Layer& l, const void* from, int64_t rows, int cols, void* to, hipStream_t st) {
     return by_type(l.dtype, [&](auto t) { return launch_pack<std::remove_pointer_t<decltype(t)>>(from, rows, cols, to, st); });

@@ -1,4 +1,5 @@
-// Products of very many rows whose weight fits the registers of a compute unit (sr_gemm.h): 16-bit types.
+// Products of very many rows whose weight fits the registers of a compute unit (sr_gemm.h): 16-bit types, and fp32 as three bfloat16 parts; rows on 16-byte pieces, or on
+// four bytes.
 //
 // A workgroup has a compute unit to itself and keeps the whole weight in registers as matrix operands, a wavefront NT tiles of 16 columns for all
 // k.  Rows come to LDS a block at a time, straight from memory, while the block before is worked on; every wavefront reads them as the other operand.  So
@@ -7,7 +8,8 @@
 // behind the next wait for rows, so that no wait is for stores just begun; a register that did not fit would be read again behind the rows on
 // their way, so each form takes only what fits (1048576 rows of 512 to 128, bfloat16: 430 us with three of them outside, 254 without).
 //
-// Bound by memory: 1048576 rows of 128 to 256, bfloat16, 180 us, of 136 to 200 200 us, gated 128 to 256 224 us; the tile kernel 220, 360, 389.
+// Bound by memory: 1048576 rows of 128 to 256, bfloat16, 184 us, of 136 to 200 202 us, gated 128 to 256 230 us; the tile kernel 221, 360, 426.  fp32, of 64 to 512
+// 545 us, of 100 to 200 506 us; the tile kernel 805, 667.
 #pragma once
 #include "sr_gemm.h"
 
